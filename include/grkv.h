@@ -61,6 +61,7 @@ extern "C" {
 #define GRKV_ERR_NUMERIC             -6  /* device: Cholesky pivot <= 0 (lambda ~ 0) */
 #define GRKV_ERR_TIMEOUT             -7  /* device: a bounded wait expired        */
 #define GRKV_ERR_BOUNDS              -8  /* device, GRKV_CHECKS: idx breaks its contract */
+#define GRKV_ERR_NO_PAGES            -9  /* device: a reserve found too few free pages */
 
 #define GRKV_F32  0
 #define GRKV_BF16 1
@@ -264,9 +265,123 @@ int grkv_transfer_check(const grkv_params* p, int32_t held, const void* q_win,
  * them.  scores and idx are device pointers laid out as for grkv_select. */
 int grkv_select_noalloc(const grkv_params* p, const float* scores, int32_t* idx, void* stream);
 
+/* ------------------------------------------------------------ paged cache
+ * The paper has no counterpart below: it is what a serving loop does with the
+ * compressed caches.  Their units have lengths of their own (budgets per unit,
+ * sequences of a batch), share prefixes and grow by a token a step, so they live
+ * in pages of one pool, and decoding attends over those.
+ *
+ *   k_pages, v_pages [P][page][d]      the pool, dtype elements; page = 16, 32, 64 or 128
+ *   table [U][max_pages]       int32   slots c page .. c page + page - 1 of unit u are in
+ *                                      pool page table[u][c]; negative: no page
+ *   len   [U]                  int32   slots in use, 0 <= len <= max_pages page
+ *   refs  [P]                  int32   table entries that hold a page; 0: free
+ *
+ * Several units (beams, forks of a sequence) may hold a page together as long as
+ * none of them writes to it; grkv_cache_reserve gives a unit pages of its own where it
+ * is about to write.  A pool may serve several tables; refs counts the entries of all.
+ * Row data and the workspace must be 16-byte aligned, the integer arrays (and lse) as
+ * their elements are, so that a slice of a table (one layer's units) is a table.  The
+ * arrays of one call must not overlap, except as stated.
+ *
+ * Faults found on the device go to the status word (grkv_status): GRKV_ERR_INVALID_ARG
+ * for a length, count, index, page or parent outside its range, which is clamped
+ * (lengths, counts), read as page 0 (attention), taken as no parent, or skipped (rows
+ * that would move), and never read or written through.  A call's other results
+ * stand.  Every call takes a workspace of grkv_cache_workspace_size bytes; calls that
+ * may overlap on the GPU need workspaces of their own. */
+typedef struct {
+  int32_t units;      /* U >= 0                                                       */
+  int32_t group;      /* g: query heads per KV head, 1..64                            */
+  int32_t d;          /* head dimension; 128 only                                     */
+  int32_t pages;      /* P >= 1: pages of the pool                                    */
+  int32_t page;       /* slots per page: 16, 32, 64 or 128                            */
+  int32_t max_pages;  /* columns of a table row; max_pages page <= 2^28               */
+  int32_t tokens;     /* t >= 1: rows per unit of q, new rows or idx (1); U g t <= 2^28 */
+  int32_t window;     /* W >= 0: slots a row sees behind it, itself included; 0: all  */
+  int32_t n_sink;     /* s >= 0: first slots that a window leaves visible (4)         */
+  float   scale;      /* logit scale; 0 -> fp32(1/sqrt(d))                            */
+  int32_t dtype;      /* GRKV_BF16 or GRKV_F32 for rows, queries and outputs          */
+  uint32_t flags;     /* GRKV_FORCE_SIMT                                              */
+} grkv_cache_params;
+
+/* Fills `p` with the defaults above for the given sizes (bf16, one token, no window). */
+void grkv_cache_params_init(grkv_cache_params* p, int32_t units, int32_t group, int32_t pages,
+                            int32_t page, int32_t max_pages);
+int grkv_cache_workspace_size(const grkv_cache_params* p, size_t* bytes);
+
+/* Pages for the slots [len[u], want[u]) of every unit (none if want <= len), each held by
+ * that unit alone: missing ones are taken from the pool, one that other entries hold
+ * too is replaced, its slots below len copied.  table and refs are updated, len is not.
+ * Free pages are taken from the lowest, for units and then columns ascending; pages that the
+ * call itself sets free are not used by it.  Too few: GRKV_ERR_NO_PAGES, and
+ * nothing changes. */
+int grkv_cache_reserve(const grkv_cache_params* p, int32_t* table, const int32_t* len,
+                       const int32_t* want, int32_t* refs, void* k_pages, void* v_pages,
+                       void* ws, size_t ws_bytes, void* stream);
+
+/* Unit u of table_out holds the pages of unit src[u] of table_in (units_in rows), or none
+ * for src[u] = -1: forks sequences, reorders beams.  No row is copied: refs gains
+ * one per entry written.  len_out[u] = len_in[src[u]].  table_out is overwritten, entries
+ * behind the length with -1; it must hold no page (grkv_cache_trim to 0 first). */
+int grkv_cache_fork(const grkv_cache_params* p, int32_t units_in, const int32_t* src,
+                    const int32_t* table_in, const int32_t* len_in, int32_t* table_out,
+                    int32_t* len_out, int32_t* refs, void* ws, size_t ws_bytes, void* stream);
+
+/* Gives back the pages that lie wholly behind len[u] (all of them for 0): entries become
+ * -1, refs loses one per entry. */
+int grkv_cache_trim(const grkv_cache_params* p, int32_t* table, const int32_t* len, int32_t* refs,
+                    void* ws, size_t ws_bytes, void* stream);
+
+/* Writes new rows to the last count[u] (NULL: t) of the len[u] slots of every unit: len is
+ * the length with the new rows.  Row i of unit u is row u t + i of k_new, v_new
+ * [U][t][d], or, with first_row, row first_row[u] + i (the packed outputs of
+ * grkv_compress_ragged). */
+int grkv_cache_append(const grkv_cache_params* p, const void* k_new, const void* v_new,
+                      const int64_t* first_row, const int32_t* count, const int32_t* table,
+                      const int32_t* len, void* k_pages, void* v_pages, void* ws, size_t ws_bytes,
+                      void* stream);
+
+/* Moves kept rows together: slot first[u] + i (first NULL: 0) of table_out takes slot
+ * idx[u][i] of table_in, i < keep[u] (NULL: t); idx [U][t], slots below len_in[u].
+ * Either table_out is another table whose written pages hold nothing that the call reads, or
+ * it is table_in itself, and then idx[u][i] >= first[u] + i (any ascending choice of slots
+ * from first[u] on) and the pages written must be the unit's own.  Serves a retained set
+ * (grkv_select's idx) and the accepted path of a draft.  Lengths and pages stay: call
+ * grkv_cache_trim with the new lengths. */
+int grkv_cache_compact(const grkv_cache_params* p, const int32_t* idx, const int32_t* keep,
+                       const int32_t* first, const int32_t* table_in, const int32_t* len_in,
+                       const int32_t* table_out, void* k_pages, void* v_pages, void* ws,
+                       size_t ws_bytes, void* stream);
+
+/* Attention of the last q_len[u] (NULL: t) slots of every unit over its cache, those slots
+ * included (append first).  Query row i is at slot p = len[u] - q_len[u] + i and sees the
+ * slots j <= p that are within its window, j > p - W (W = 0: all), or sinks, j < s:
+ *   out = sum_j softmax_j(scale q.k_j) v_j,  lse = ln sum_j exp(scale q.k_j)
+ * q, out [U][g][t][d]; lse [U][g][t] fp32, or NULL.  A row that sees nothing (p < 0,
+ * or only logits of -inf) gives out = 0 and lse = -inf.  Rows from q_len[u] on are left as
+ * they were.  Slots that a row does not see do not reach it, whatever they hold,
+ * and a page without a slot that some row of its unit sees is not read: its entry may be negative.
+ * t = 1 is decoding, larger t a chunk of prefill.  bf16 rounds the unnormalised
+ * probabilities to bf16 for the product with V (fp32 sums); results do not change from
+ * run to run. */
+int grkv_attend(const grkv_cache_params* p, const void* q, const void* k_pages, const void* v_pages,
+                const int32_t* table, const int32_t* len, const int32_t* q_len, void* out,
+                float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* grkv_attend for drafted trees, t <= 256: the last q_len[u] slots hold the nodes of a tree,
+ * parent[u][i] (int32 [U][t]) < i is node i's parent, -1 the cache before it.  A node sees that
+ * cache, its ancestors and itself.  With base = len[u] - q_len[u], a node of depth a
+ * (roots 0) is at position base + a, a cached slot j at j; window and sinks go by
+ * positions. */
+int grkv_attend_tree(const grkv_cache_params* p, const void* q, const void* k_pages,
+                     const void* v_pages, const int32_t* table, const int32_t* len,
+                     const int32_t* q_len, const int32_t* parent, void* out, float* lse, void* ws,
+                     size_t ws_bytes, void* stream);
+
 /* Synchronises `stream`, then stores in *device_status the device-side
- * status of the most recent call that used `ws` (GRKV_OK, GRKV_ERR_NUMERIC or
- * GRKV_ERR_TIMEOUT).  Returns GRKV_ERR_CUDA if the stream reports an error. */
+ * status of the most recent call that used `ws` (GRKV_OK or one of the codes marked
+ * "device" above).  Returns GRKV_ERR_CUDA if the stream reports an error. */
 int grkv_status(const void* ws, int* device_status, void* stream);
 
 /* Static description of an error code. */

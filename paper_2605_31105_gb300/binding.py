@@ -22,6 +22,7 @@ GRKV_ERR_CUDA = -5
 GRKV_ERR_NUMERIC = -6
 GRKV_ERR_TIMEOUT = -7
 GRKV_ERR_BOUNDS = -8
+GRKV_ERR_NO_PAGES = -9
 
 GRKV_F32 = 0
 GRKV_BF16 = 1
@@ -37,7 +38,10 @@ GRKV_TEST_TIMEOUT = 0x80000000
 EXPORTS = ("grkv_params_init", "grkv_workspace_size", "grkv_score", "grkv_select", "grkv_merge",
            "grkv_compress", "grkv_status", "grkv_strerror", "grkv_launch_count",
            "grkv_select_noalloc", "grkv_transfer_workspace_size", "grkv_transfer_check",
-           "grkv_compress_ragged_workspace_size", "grkv_compress_ragged")
+           "grkv_compress_ragged_workspace_size", "grkv_compress_ragged",
+           "grkv_cache_params_init", "grkv_cache_workspace_size", "grkv_cache_reserve",
+           "grkv_cache_fork", "grkv_cache_trim", "grkv_cache_append", "grkv_cache_compact",
+           "grkv_attend", "grkv_attend_tree")
 
 
 class grkv_params(ctypes.Structure):
@@ -49,6 +53,15 @@ class grkv_params(ctypes.Structure):
         ("lambda_k", ctypes.c_float), ("scale", ctypes.c_float), ("causal", ctypes.c_int32),
         ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("cg_iters", ctypes.c_int32),
         ("cg_tol", ctypes.c_float), ("steps", ctypes.c_int32), ("step_tol", ctypes.c_float),
+    ]
+
+
+class grkv_cache_params(ctypes.Structure):
+    _fields_ = [
+        ("units", ctypes.c_int32), ("group", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("pages", ctypes.c_int32), ("page", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+        ("tokens", ctypes.c_int32), ("window", ctypes.c_int32), ("n_sink", ctypes.c_int32),
+        ("scale", ctypes.c_float), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
     ]
 
 
@@ -99,6 +112,17 @@ def load():
                  "grkv_transfer_check", "grkv_compress_ragged_workspace_size",
                  "grkv_compress_ragged"):
         getattr(lib, name).restype = ctypes.c_int
+    _cp, _sz, _i = ctypes.POINTER(grkv_cache_params), ctypes.c_size_t, ctypes.c_int32
+    lib.grkv_cache_params_init.argtypes = [_cp, _i, _i, _i, _i, _i]
+    lib.grkv_cache_params_init.restype = None
+    lib.grkv_cache_workspace_size.argtypes = [_cp, ctypes.POINTER(_sz)]
+    for name, lead in (("grkv_cache_reserve", [_vp] * 6), ("grkv_cache_trim", [_vp] * 3),
+                       ("grkv_cache_fork", [_i] + [_vp] * 6), ("grkv_cache_append", [_vp] * 8),
+                       ("grkv_cache_compact", [_vp] * 8), ("grkv_attend", [_vp] * 8),
+                       ("grkv_attend_tree", [_vp] * 9)):
+        getattr(lib, name).argtypes = [_cp, *lead, _vp, _sz, _vp]
+        getattr(lib, name).restype = ctypes.c_int
+    lib.grkv_cache_workspace_size.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -227,6 +251,153 @@ def grkv_compress_ragged(p, budgets, q, k, v, k_out, v_out, idx, ws, ws_bytes=No
                                      _ptr(v), _ptr(k_out), _ptr(v_out), _ptr(idx), _ptr(ws),
                                      ws_bytes, _stream(stream))
     return _check(rc, "grkv_compress_ragged", check)
+
+
+# ------------------------------------------------------------------ paged cache
+def cache_params(units, group, pages, page, max_pages, **kw) -> grkv_cache_params:
+    """grkv_cache_params with the library defaults, then any field overridden by name
+    (dtype may be given as "bf16" / "f32")."""
+    p = grkv_cache_params()
+    load().grkv_cache_params_init(ctypes.byref(p), units, group, pages, page, max_pages)
+    for key, val in kw.items():
+        if key == "dtype" and isinstance(val, str):
+            val = {"bf16": GRKV_BF16, "f32": GRKV_F32}[val]
+        setattr(p, key, val)
+    return p
+
+
+_DTYPES = {GRKV_BF16: "torch.bfloat16", GRKV_F32: "torch.float32"}
+
+
+def _args(p, ws, rows, words):
+    """Checks the tensors of a cache call (addresses given as ints pass): row data of the
+    call's type, integer arrays of 32 bits (64 where the name starts with first_row), all
+    contiguous, on the device of the workspace, as large as the call reads or writes."""
+    import torch
+    dev = None if isinstance(ws, int) else ws.device
+    if dev is not None and (dev.type != "cuda" or dev.index != torch.cuda.current_device()):
+        raise ValueError("the workspace is not on the current CUDA device")
+    for kind, group in (("row", rows), ("word", words)):
+        for name, (t, need) in group.items():
+            if t is None or isinstance(t, int):
+                continue
+            want = _DTYPES.get(p.dtype) if kind == "row" else (
+                "torch.float32" if name == "lse" else
+                "torch.int64" if name == "first_row" else "torch.int32")
+            if str(t.dtype) != want:
+                raise ValueError(f"{name} is {t.dtype}, the call takes {want}")
+            if dev is not None and t.device != dev:
+                raise ValueError(f"{name} is on {t.device}, the workspace on {dev}")
+            if not t.is_contiguous():
+                raise ValueError(f"{name} is not contiguous")
+            if t.numel() < need:
+                raise ValueError(f"{name} holds {t.numel()} elements, the call takes {need}")
+
+
+def _pool_args(p, k_pages, v_pages):
+    n = p.pages * p.page * p.d
+    return {"k_pages": (k_pages, n), "v_pages": (v_pages, n)}
+
+
+def _table_args(p, lens, **tables):
+    return {**{k: (t, p.units * p.max_pages) for k, t in tables.items()}, "lens": (lens, p.units)}
+
+
+def _nbytes(ws, ws_bytes):
+    return ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+
+
+def grkv_cache_workspace_size(p: grkv_cache_params) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().grkv_cache_workspace_size(ctypes.byref(p), ctypes.byref(n)),
+           "grkv_cache_workspace_size", True)
+    return n.value
+
+
+def grkv_cache_reserve(p, table, lens, want, refs, k_pages, v_pages, ws, ws_bytes=None,
+                       stream=None, check=True):
+    """Own pages for slots [lens, want) of every unit."""
+    _args(p, ws, _pool_args(p, k_pages, v_pages),
+          {**_table_args(p, lens, table=table), "want": (want, p.units), "refs": (refs, p.pages)})
+    rc = load().grkv_cache_reserve(ctypes.byref(p), _ptr(table), _ptr(lens), _ptr(want),
+                                   _ptr(refs), _ptr(k_pages), _ptr(v_pages), _ptr(ws),
+                                   _nbytes(ws, ws_bytes), _stream(stream))
+    return _check(rc, "grkv_cache_reserve", check)
+
+
+def grkv_cache_fork(p, src, table_in, lens_in, table_out, lens_out, refs, ws, units_in=None,
+                    ws_bytes=None, stream=None, check=True):
+    """Unit u of table_out shares the pages of unit src[u] of table_in (-1: none)."""
+    if units_in is None:
+        units_in = lens_in.numel()
+    _args(p, ws, {}, {"src": (src, p.units), "table_in": (table_in, units_in * p.max_pages),
+                      "lens_in": (lens_in, units_in),
+                      "table_out": (table_out, p.units * p.max_pages),
+                      "lens_out": (lens_out, p.units), "refs": (refs, p.pages)})
+    rc = load().grkv_cache_fork(ctypes.byref(p), units_in, _ptr(src), _ptr(table_in),
+                                _ptr(lens_in), _ptr(table_out), _ptr(lens_out), _ptr(refs),
+                                _ptr(ws), _nbytes(ws, ws_bytes), _stream(stream))
+    return _check(rc, "grkv_cache_fork", check)
+
+
+def grkv_cache_trim(p, table, lens, refs, ws, ws_bytes=None, stream=None, check=True):
+    """Gives back the pages behind lens."""
+    _args(p, ws, {}, {**_table_args(p, lens, table=table), "refs": (refs, p.pages)})
+    rc = load().grkv_cache_trim(ctypes.byref(p), _ptr(table), _ptr(lens), _ptr(refs), _ptr(ws),
+                                _nbytes(ws, ws_bytes), _stream(stream))
+    return _check(rc, "grkv_cache_trim", check)
+
+
+def grkv_cache_append(p, k_new, v_new, k_pages, v_pages, table, lens, ws, count=None,
+                      first_row=None, ws_bytes=None, stream=None, check=True):
+    """New rows to the last `count` of the `lens` slots of every unit."""
+    need = 0 if first_row is not None else p.units * p.tokens * p.d
+    _args(p, ws, {**_pool_args(p, k_pages, v_pages), "k_new": (k_new, need),
+                  "v_new": (v_new, need)},
+          {**_table_args(p, lens, table=table), "count": (count, p.units),
+           "first_row": (first_row, p.units)})
+    rc = load().grkv_cache_append(ctypes.byref(p), _ptr(k_new), _ptr(v_new), _ptr(first_row),
+                                  _ptr(count), _ptr(table), _ptr(lens), _ptr(k_pages),
+                                  _ptr(v_pages), _ptr(ws), _nbytes(ws, ws_bytes), _stream(stream))
+    return _check(rc, "grkv_cache_append", check)
+
+
+def grkv_cache_compact(p, idx, k_pages, v_pages, table_in, lens_in, table_out, ws, keep=None,
+                       first=None, ws_bytes=None, stream=None, check=True):
+    """Slot first + i of table_out takes slot idx[u][i] of table_in."""
+    _args(p, ws, _pool_args(p, k_pages, v_pages),
+          {**_table_args(p, lens_in, table_in=table_in, table_out=table_out),
+           "idx": (idx, p.units * p.tokens), "keep": (keep, p.units), "first": (first, p.units)})
+    rc = load().grkv_cache_compact(ctypes.byref(p), _ptr(idx), _ptr(keep), _ptr(first),
+                                   _ptr(table_in), _ptr(lens_in), _ptr(table_out),
+                                   _ptr(k_pages), _ptr(v_pages), _ptr(ws),
+                                   _nbytes(ws, ws_bytes), _stream(stream))
+    return _check(rc, "grkv_cache_compact", check)
+
+
+def grkv_attend(p, q, k_pages, v_pages, table, lens, out, ws, q_lens=None, lse=None,
+                ws_bytes=None, stream=None, check=True):
+    """Attention of the last q_lens slots of every unit over its pages."""
+    n = p.units * p.group * p.tokens
+    _args(p, ws, {**_pool_args(p, k_pages, v_pages), "q": (q, n * p.d), "out": (out, n * p.d)},
+          {**_table_args(p, lens, table=table), "q_lens": (q_lens, p.units), "lse": (lse, n)})
+    rc = load().grkv_attend(ctypes.byref(p), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(table),
+                            _ptr(lens), _ptr(q_lens), _ptr(out), _ptr(lse), _ptr(ws),
+                            _nbytes(ws, ws_bytes), _stream(stream))
+    return _check(rc, "grkv_attend", check)
+
+
+def grkv_attend_tree(p, q, k_pages, v_pages, table, lens, parent, out, ws, q_lens=None, lse=None,
+                     ws_bytes=None, stream=None, check=True):
+    """grkv_attend for trees of drafted tokens: parent [U][t], -1 for roots."""
+    n = p.units * p.group * p.tokens
+    _args(p, ws, {**_pool_args(p, k_pages, v_pages), "q": (q, n * p.d), "out": (out, n * p.d)},
+          {**_table_args(p, lens, table=table), "q_lens": (q_lens, p.units), "lse": (lse, n),
+           "parent": (parent, p.units * p.tokens)})
+    rc = load().grkv_attend_tree(ctypes.byref(p), _ptr(q), _ptr(k_pages), _ptr(v_pages),
+                                 _ptr(table), _ptr(lens), _ptr(q_lens), _ptr(parent), _ptr(out),
+                                 _ptr(lse), _ptr(ws), _nbytes(ws, ws_bytes), _stream(stream))
+    return _check(rc, "grkv_attend_tree", check)
 
 
 def grkv_launch_count() -> int:

@@ -1,0 +1,298 @@
+// Attention over the paged cache: what the portable and the tensor-core kernel share.
+// The visible slots of a row, the work items, their split over the CTAs, and the
+// partial results that k_attend_join adds up.
+//
+// A work item is one unit and a block of its tokens: `nq` row tiles of T tokens x g
+// query heads, which read the same keys.  Its keys come in tiles of 128 slots: those
+// that hold sinks, then those of the rows' windows.  The items' tiles in a row
+// are cut into equal runs, one per CTA, whatever item they belong to: lengths that
+// differ, causal triangles, few units with many keys and many units with few all
+// leave every CTA the same work, and only the device needs to know the lengths.  A CTA
+// that holds only part of an item's tiles leaves a partial (reference, sum, output).
+#pragma once
+
+#include "cache_args.cuh"
+#include "sm100.cuh"
+
+namespace grkv {
+
+constexpr int kSlotTile = 128;   // slots per key tile
+
+struct AttendRec {
+  int u, qb, last, err;   // the split item that starts in this CTA (u < 0: none), its last CTA
+};
+
+struct AttendArgs {
+  const void *q, *k, *v;
+  const int32_t *table, *len, *qlen, *parent;
+  void* out;
+  float* lse;
+  int U, g, t, P, shift, cols, W, s;
+  int T;       // tokens of a row tile
+  int nq;      // row tiles of an item
+  int QB;      // items of a unit
+  int rows;    // rows of an item, nq * T * g
+  float sl2;   // scale * log2(e)
+  AttendRec* rec;
+  float2* pml;
+  float* po;
+  int* status;
+};
+
+// One item: tokens [tok0, tok0 + ntok) of unit u; the slots that its rows see are in
+// [0, sink_end) and [lo, hi); its tile k is slot tile k < ns ? k : lo_tile + k - ns.
+struct Item {
+  int u, tok0, ntok, base, L;
+  int sink_end, lo, hi, ns, lo_tile, nt;
+  __device__ int tile(int k) const { return k < ns ? k : lo_tile + k - ns; }
+  // Slots [a, b) hold one that some row of the item sees.
+  __device__ bool wanted(int a, int b) const { return a < sink_end || (a < hi && b > lo); }
+};
+
+__device__ __forceinline__ Item make_item(const AttendArgs& a, int item) {
+  Item it;
+  it.u = item / a.QB;
+  const int L = a.len[it.u], cap = a.cols << a.shift;
+  it.L = min(max(L, 0), cap);
+  const int T = a.qlen ? min(max(a.qlen[it.u], 0), a.t) : a.t;
+  it.base = it.L - T;
+  it.tok0 = (item - it.u * a.QB) * a.nq * a.T;
+  it.ntok = max(0, min(T - it.tok0, a.nq * a.T));
+  const bool tree = a.parent != nullptr;
+  const int p0 = it.base + (tree ? 0 : it.tok0);   // the first position of a row
+  it.hi = max(0, it.base + it.tok0 + it.ntok);
+  it.lo = a.W ? min(max(0, p0 - a.W + 1), it.hi) : 0;
+  it.sink_end = a.W ? min(a.s, it.lo) : 0;
+  it.lo_tile = it.lo / kSlotTile;
+  it.ns = min((it.sink_end + kSlotTile - 1) / kSlotTile, it.lo_tile);
+  it.nt = it.ns + (it.hi + kSlotTile - 1) / kSlotTile - it.lo_tile;
+  if (it.ntok == 0) it.nt = 0;
+  else if (it.nt < 1) it.nt = 1;   // rows that see nothing are written by a tile without slots
+  return it;
+}
+
+// Whether every row of tokens [t0, t0 + n) of the item sees the whole slot tile.
+__device__ __forceinline__ bool tile_full(const AttendArgs& a, const Item& it, int t0, int n, int tile) {
+  const int x = tile * kSlotTile, y = x + kSlotTile;
+  const bool tree = a.parent != nullptr;
+  const int first_hi = tree ? it.base : it.base + t0 + 1;
+  if (y > first_hi) return false;
+  if (!a.W || y <= a.s) return true;
+  return x >= it.base + t0 + n - a.W;   // a node's depth is at most its index
+}
+
+// Bits 0..n-1 (n clamped to 0..32).
+__device__ __forceinline__ uint32_t low_bits(int n) {
+  return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+}
+// Bit e: slot a + e is in [x, y).
+__device__ __forceinline__ uint32_t range_bits(int a, int x, int y) {
+  return low_bits(y - a) & ~low_bits(x - a);
+}
+
+// What one row sees: slots below end_s or in [lo, hi), and, in a tree, the drafted
+// slots base + b whose bit b is set in anc.
+struct RowVis {
+  int end_s, lo, hi, base;
+  const uint32_t* anc;   // kMaxTree bits, or null
+  // Bit e: slot a + e (a a multiple of 32).
+  __device__ uint32_t word(int a) const {
+    uint32_t m = range_bits(a, 0, end_s) | range_bits(a, lo, hi);
+    if (anc) {
+      const int o = a - base, i = o >> 5, sh = o & 31;   // arithmetic shift: floor
+      const uint32_t w0 = (unsigned)i < kMaxTree / 32 ? anc[i] : 0u;
+      const uint32_t w1 = (unsigned)(i + 1) < kMaxTree / 32 ? anc[i + 1] : 0u;
+      m |= __funnelshift_r(w0, w1, sh);
+    }
+    return m;
+  }
+};
+
+// The slots that token i of the item's unit sees (live: the row exists).  In a tree the row's
+// ancestor bits go to anc, 8 words that only this thread writes; a bad parent sets
+// *err and counts as none.
+__device__ __forceinline__ RowVis row_vis(const AttendArgs& a, const Item& it, int i, bool live,
+                                          uint32_t* anc, int* err) {
+  RowVis r{0, 0, 0, it.base, nullptr};
+  if (a.parent) {
+#pragma unroll
+    for (int w = 0; w < kMaxTree / 32; ++w) anc[w] = 0;
+    r.anc = anc;
+  }
+  if (!live) return r;
+  int p = it.base + i;
+  r.hi = p + 1;
+  if (a.parent) {
+    const int32_t* par = a.parent + (size_t)it.u * a.t;
+    int depth = 0;
+    for (int x = i;;) {
+      const int y = par[x];
+      if (y < -1 || y >= x) *err = GRKV_ERR_INVALID_ARG;
+      if (y < 0 || y >= x) break;
+      x = y;
+      ++depth;
+    }
+    p = it.base + depth;
+    for (int x = i, k = 0; k <= depth; ++k) {   // the ancestor k steps up is at position p - k
+      if (!a.W || k < a.W || p - k < a.s) anc[x >> 5] |= 1u << (x & 31);
+      x = par[x];
+    }
+    r.hi = it.base;
+  }
+  r.hi = max(r.hi, 0);
+  r.lo = a.W ? min(max(0, p - a.W + 1), r.hi) : 0;
+  r.end_s = min(a.s, r.lo);
+  return r;
+}
+
+// The CTA's run of tiles.
+struct Run {
+  long long total;   // tiles of all items
+  int G;             // CTAs that have any
+  int item, off;     // first item and its first tile here
+  int left;          // tiles of the run
+  __device__ long long start(int c) const { return total * c / G; }
+  __device__ int owner(long long t) const { return (int)(((t + 1) * G + total - 1) / total) - 1; }
+};
+
+// The fewest tiles worth a CTA of their own: a tile takes about 1 us and joining a
+// partial result about as long.
+constexpr int kMinRun = 1;
+
+struct PlanSmem {
+  Run run;
+  AttendRec rec;
+  long long warp_sum[32];
+  int err;
+};
+
+// Every thread of the block takes part (n threads, a multiple of 32).  Afterwards ps->run
+// holds the CTA's run (left == 0: none), ps->rec the split item that starts in it, and
+// ps->err any fault of the lengths.
+__device__ __forceinline__ void plan_run(const AttendArgs& a, PlanSmem* ps, int n) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int items = a.U * a.QB;
+  const int per = (items + n - 1) / n, i0 = min(items, tid * per), i1 = min(items, i0 + per);
+  if (tid == 0) {
+    ps->err = 0;
+    ps->run = Run{0, 1, 0, 0, 0};
+    ps->rec = AttendRec{-1, 0, 0, 0};
+  }
+  __syncthreads();
+  long long mine = 0;
+  for (int i = i0; i < i1; ++i) {
+    const Item it = make_item(a, i);
+    mine += it.nt;
+    if (it.L != a.len[it.u] || (a.qlen && (a.qlen[it.u] < 0 || a.qlen[it.u] > a.t)))
+      ps->err = GRKV_ERR_INVALID_ARG;
+  }
+  long long scan = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long x = __shfl_up_sync(0xffffffffu, scan, d);
+    if (lane >= d) scan += x;
+  }
+  if (lane == 31) ps->warp_sum[warp] = scan;
+  __syncthreads();
+  long long before = 0, total = 0;
+  for (int w = 0; w < n / 32; ++w) {
+    const long long x = ps->warp_sum[w];
+    if (w < warp) before += x;
+    total += x;
+  }
+  before += scan - mine;
+  if (total > 0) {
+    Run r;
+    r.total = total;
+    r.G = (int)min((long long)gridDim.x, max(1ll, total / kMinRun));
+    const int c = blockIdx.x;
+    const long long t0 = r.start(c);
+    const long long t1 = r.start(c + 1);
+    // the first and the last tile are each in the items of one thread
+    const bool first = before <= t0 && t0 < before + mine;
+    const bool last = before < t1 && t1 <= before + mine;
+    if (c < r.G && (first || last)) {
+      long long at = before;
+      for (int i = i0; i < i1; ++i) {
+        const int nt = make_item(a, i).nt;
+        if (at <= t0 && t0 < at + nt) {
+          r.item = i;
+          r.off = (int)(t0 - at);
+          r.left = (int)(t1 - t0);
+          ps->run = r;
+        }
+        if (t0 <= at && at < t1 && t1 < at + nt)
+          ps->rec = AttendRec{i / a.QB, i % a.QB, r.owner(at + nt - 1), 0};
+        at += nt;
+        if (at >= t1) break;
+      }
+    }
+  }
+  __syncthreads();
+}
+
+// A CTA's segments in order: each is a run of tiles of one item.
+struct Segments {
+  Item it;
+  int item, off, cnt, left;
+  __device__ Segments(const AttendArgs& a, const Run& r)
+      : item(r.item), off(r.off), left(r.left) {
+    if (left > 0) load(a);
+  }
+  __device__ void load(const AttendArgs& a) {
+    it = make_item(a, item);
+    cnt = min(left, it.nt - off);
+  }
+  __device__ bool more() const { return left > 0; }
+  __device__ bool whole() const { return off == 0 && cnt == it.nt; }
+  __device__ int slot(int cta) const { return off == 0 ? 2 * cta + 1 : 2 * cta; }
+  __device__ void next(const AttendArgs& a) {
+    left -= cnt;
+    off = 0;
+    ++item;
+    if (left <= 0) return;
+    load(a);
+    while (it.nt == 0) {   // items without rows; left > 0 says that one with rows follows
+      ++item;
+      load(a);
+    }
+  }
+};
+
+// The page entry of table column c of unit u, and the page to read: an entry outside the
+// pool sets *err and stands for page 0.
+__device__ __forceinline__ int page_of(const AttendArgs& a, int u, int c, int* err) {
+  const int e = __ldg(a.table + (size_t)u * a.cols + c);
+  if ((unsigned)e < (unsigned)a.P) return e;
+  *err = GRKV_ERR_INVALID_ARG;
+  return 0;
+}
+
+// Row r of row tile w of an item: its head and token; false for rows that are padding.
+__device__ __forceinline__ bool row_of(const AttendArgs& a, const Item& it, int w, int r, int* h,
+                                       int* i) {
+  *h = r / a.T;
+  const int x = w * a.T + r - *h * a.T;
+  *i = it.tok0 + x;
+  return *h < a.g && x < it.ntok;
+}
+
+// What a partial result with reference m weighs against reference M.
+__device__ __forceinline__ float weight_of(float m, float M) {
+  return m == -INFINITY ? 0.f : sm100::fast_exp2(m - M);
+}
+
+// ln of a row's sum of exponentials; -inf for a row that sees nothing.
+__device__ __forceinline__ float row_lse(float m, float l) {
+  return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+__device__ __forceinline__ void store_row4(float* p, float4 x) { *(float4*)p = x; }
+__device__ __forceinline__ void store_row4(__nv_bfloat16* p, float4 x) {
+  uint2 v;
+  v.x = sm100::pack_bf16(x.x, x.y);
+  v.y = sm100::pack_bf16(x.z, x.w);
+  *(uint2*)p = v;
+}
+
+}  // namespace grkv

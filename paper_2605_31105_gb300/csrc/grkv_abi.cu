@@ -317,6 +317,7 @@ const char* grkv_strerror(int code) {
     case GRKV_ERR_NUMERIC: return "non-positive Cholesky pivot";
     case GRKV_ERR_TIMEOUT: return "bounded device wait expired";
     case GRKV_ERR_BOUNDS: return "idx breaks its contract (GRKV_CHECKS)";
+    case GRKV_ERR_NO_PAGES: return "too few free pages in the pool";
     default: return "unknown error";
   }
 }

@@ -1,0 +1,325 @@
+// Attention over the paged cache on CUDA cores, for fp32 and (GRKV_FORCE_SIMT) bf16.
+//
+// A row tile is up to 64 rows (T tokens x g query heads).  Its keys come in
+// sub-tiles of 64 slots, two buffers deep, copied page by page to shared memory.  A thread
+// of 256 holds 4 rows x 4 slots of the logits and then 4 rows x 8 columns of the
+// output; the softmax is online: reference (running maximum, log2 units) and sum per row,
+// the output rescaled when the reference grows.  Slots that a row does not see carry p = -1
+// and are left out of its sums by comparison, so whatever lies there (a NaN, an infinity)
+// does not reach the row.
+#include <algorithm>
+
+#include "attend_plan.cuh"
+
+namespace grkv {
+namespace {
+
+using namespace sm100;
+
+constexpr int kRowTile = 64;   // rows of a tile
+constexpr int kSub = 64;       // slots of a sub-tile
+constexpr int kThreads = 256;
+constexpr int kQStride = kD + 4;        // floats
+constexpr int kPStride = kSub + 4;
+
+template <typename T>
+struct SimtLayout {
+  static constexpr int kStride = kD + 16 / (int)sizeof(T);      // elements of a K or V row
+  static constexpr uint32_t kSubBytes = kSub * kStride * sizeof(T);
+  static constexpr uint32_t kOffQ = 0;
+  static constexpr uint32_t kOffKv = kOffQ + kRowTile * kQStride * 4;   // [2][K, V]
+  static constexpr uint32_t kOffP = kOffKv + 4 * kSubBytes;
+  static constexpr uint32_t kOffAnc = kOffP + kRowTile * kPStride * 4;
+  static constexpr uint32_t kOffMask = kOffAnc + kRowTile * (kMaxTree / 8);
+  static constexpr uint32_t kOffPlan = kOffMask + 2 * kRowTile * 8;
+  static constexpr uint32_t kBytes = kOffPlan + ((sizeof(PlanSmem) + 15) & ~15);
+};
+static_assert(SimtLayout<float>::kBytes <= 227 * 1024, "smem");
+
+__device__ __forceinline__ float4 ld4(const float* p) { return *(const float4*)p; }
+__device__ __forceinline__ float4 ld4(const __nv_bfloat16* p) {
+  const uint2 v = *(const uint2*)p;
+  return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u),
+                     __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 1) k_attend_simt(AttendArgs a) {
+  using Lay = SimtLayout<T>;
+  extern __shared__ __align__(16) uint8_t sm[];
+  float* qs = (float*)(sm + Lay::kOffQ);
+  float* ps = (float*)(sm + Lay::kOffP);
+  uint32_t(*anc)[kMaxTree / 32] = (uint32_t(*)[kMaxTree / 32])(sm + Lay::kOffAnc);
+  uint32_t(*masks)[2] = (uint32_t(*)[2])(sm + Lay::kOffMask);   // [2][rows]
+  PlanSmem* plan = (PlanSmem*)(sm + Lay::kOffPlan);
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  plan_run(a, plan, kThreads);
+  const Run run = plan->run;
+  int err = 0;
+
+  for (Segments sg(a, run); sg.more(); sg.next(a)) {
+    const Item& it = sg.it;
+    auto kv = [&](int buf, int which) {
+      return (T*)(sm + Lay::kOffKv + (2 * buf + which) * Lay::kSubBytes);
+    };
+    // sub-tiles of the segment: two per slot tile
+    auto load = [&](int n) {
+      const int x = it.tile(sg.off + (n >> 1)) * kSlotTile + (n & 1) * kSub;
+      constexpr int kChunks = kD * (int)sizeof(T) / 16;
+      for (int e = tid; e < kSub * kChunks; e += kThreads) {
+        const int row = e / kChunks, ch = e % kChunks, slot = x + row, c = slot >> a.shift;
+        if (!it.wanted(c << a.shift, (c + 1) << a.shift)) continue;
+        const size_t at =
+            (((size_t)page_of(a, it.u, c, &err) << a.shift) + (slot & ((1 << a.shift) - 1))) * kD;
+        const int off = ch * (16 / (int)sizeof(T));
+        cp_async16(smem_u32(kv(n & 1, 0) + row * Lay::kStride + off), (const T*)a.k + at + off);
+        cp_async16(smem_u32(kv(n & 1, 1) + row * Lay::kStride + off), (const T*)a.v + at + off);
+      }
+    };
+    const int subs = 2 * sg.cnt;
+    load(0);
+    // the item's queries; rows that do not exist are zero
+    for (int e = tid; e < kRowTile * (kD / 4); e += kThreads) {
+      const int r = e / (kD / 4), d = e % (kD / 4) * 4;
+      int h, i;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (row_of(a, it, 0, r, &h, &i))
+        x = ld4((const T*)a.q + (((size_t)it.u * a.g + h) * a.t + i) * kD + d);
+      *(float4*)(qs + r * kQStride + d) = x;
+    }
+    RowVis vis{};
+    if (tid < kRowTile) {
+      int h, i;
+      const bool live = row_of(a, it, 0, tid, &h, &i);
+      vis = row_vis(a, it, i, live, anc[tid], &err);
+    }
+    float m[4], l[4], acc[4][8];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      m[r] = -INFINITY;
+      l[r] = 0.f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) acc[r][c] = 0.f;
+    }
+    for (int n = 0; n < subs; ++n) {
+      cp_async_wait_all();
+      const int tile = it.tile(sg.off + (n >> 1)), x = tile * kSlotTile + (n & 1) * kSub;
+      const bool full = tile_full(a, it, it.tok0, it.ntok, tile);
+      uint32_t(*mask)[2] = masks + (n & 1) * kRowTile;
+      if (tid < kRowTile) {
+        mask[tid][0] = vis.word(x);
+        mask[tid][1] = vis.word(x + 32);
+      }
+      __syncthreads();   // the sub-tile and the masks are there; the last one has been read
+      if (n + 1 < subs) load(n + 1);
+      const T *ks = kv(n & 1, 0), *vs = kv(n & 1, 1);
+      float sc[4][4] = {};
+      for (int d = 0; d < kD; d += 4) {
+        float4 q4[4], k4[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) q4[r] = ld4(qs + (ty * 4 + r) * kQStride + d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k4[j] = ld4(ks + (tx + 16 * j) * Lay::kStride + d);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            sc[r][j] = fmaf(q4[r].x, k4[j].x, sc[r][j]);
+            sc[r][j] = fmaf(q4[r].y, k4[j].y, sc[r][j]);
+            sc[r][j] = fmaf(q4[r].z, k4[j].z, sc[r][j]);
+            sc[r][j] = fmaf(q4[r].w, k4[j].w, sc[r][j]);
+          }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = ty * 4 + r;
+        const uint32_t w0 = mask[row][0], w1 = mask[row][1];
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w = j < 2 ? w0 : w1;
+          const bool see = (w >> ((tx + 16 * j) & 31)) & 1;
+          sc[r][j] = see ? sc[r][j] * a.sl2 : -INFINITY;
+          top = fmaxf(top, sc[r][j]);
+        }
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const float M = fmaxf(m[r], top), ref = M == -INFINITY ? 0.f : M;
+        const float keep = fast_exp2(m[r] - ref);
+        m[r] = M;
+        l[r] *= keep;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[r][c] *= keep;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w = j < 2 ? w0 : w1;
+          const bool see = (w >> ((tx + 16 * j) & 31)) & 1;
+          const float p = fast_exp2(sc[r][j] - ref);
+          if (see) l[r] += p;
+          ps[row * kPStride + tx + 16 * j] = see ? p : -1.f;
+        }
+      }
+      __syncwarp();   // a warp writes and reads its own 8 rows
+      for (int j = 0; j < kSub; j += 4) {
+        float4 p4[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p4[r] = ld4(ps + (ty * 4 + r) * kPStride + j);
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) {
+          const float4 va = ld4(vs + (j + jj) * Lay::kStride + tx * 4);
+          const float4 vb = ld4(vs + (j + jj) * Lay::kStride + 64 + tx * 4);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float p = jj == 0 ? p4[r].x : jj == 1 ? p4[r].y : jj == 2 ? p4[r].z : p4[r].w;
+            if (full || !(p < 0.f)) {
+              acc[r][0] = fmaf(p, va.x, acc[r][0]);
+              acc[r][1] = fmaf(p, va.y, acc[r][1]);
+              acc[r][2] = fmaf(p, va.z, acc[r][2]);
+              acc[r][3] = fmaf(p, va.w, acc[r][3]);
+              acc[r][4] = fmaf(p, vb.x, acc[r][4]);
+              acc[r][5] = fmaf(p, vb.y, acc[r][5]);
+              acc[r][6] = fmaf(p, vb.z, acc[r][6]);
+              acc[r][7] = fmaf(p, vb.w, acc[r][7]);
+            }
+          }
+        }
+      }
+    }
+    const bool whole = sg.whole();
+    const size_t part = (size_t)sg.slot(blockIdx.x) * a.rows;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int row = ty * 4 + r;
+#pragma unroll
+      for (int d = 8; d >= 1; d >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+      int h, i;
+      if (!row_of(a, it, 0, row, &h, &i)) continue;
+      float4 x0 = make_float4(acc[r][0], acc[r][1], acc[r][2], acc[r][3]);
+      float4 x1 = make_float4(acc[r][4], acc[r][5], acc[r][6], acc[r][7]);
+      if (whole) {
+        const size_t o = ((size_t)it.u * a.g + h) * a.t + i;
+        const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
+        x0 = make_float4(x0.x * inv, x0.y * inv, x0.z * inv, x0.w * inv);
+        x1 = make_float4(x1.x * inv, x1.y * inv, x1.z * inv, x1.w * inv);
+        store_row4((T*)a.out + o * kD + tx * 4, x0);
+        store_row4((T*)a.out + o * kD + 64 + tx * 4, x1);
+        if (a.lse && tx == 0) a.lse[o] = row_lse(m[r], l[r]);
+      } else {
+        store_row4(a.po + (part + row) * kD + tx * 4, x0);
+        store_row4(a.po + (part + row) * kD + 64 + tx * 4, x1);
+        if (tx == 0) a.pml[part + row] = make_float2(m[r], l[r]);
+      }
+    }
+    __syncthreads();   // the next segment overwrites the queries and both buffers
+  }
+  if (err) plan->err = err;
+  __syncthreads();
+  if (tid == 0) {
+    AttendRec rec = plan->rec;
+    rec.err = plan->err;
+    a.rec[blockIdx.x] = rec;
+  }
+}
+
+// Adds up the partial results of the split items, and writes the call's status.  Block
+// (c, y) takes 8 rows of the item that starts in CTA c, a warp each.
+template <typename T>
+__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int G) {
+  chain_wait();
+  const int c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (c == 0 && blockIdx.y == 0 && warp == 0) {
+    int err = 0;
+    for (int x = lane; x < G; x += 32) err = min(err, a.rec[x].err);
+    err = __reduce_min_sync(0xffffffffu, err);
+    if (lane == 0) *a.status = err;
+  }
+  const AttendRec rec = a.rec[c];
+  const int row = blockIdx.y * 8 + warp;
+  if (rec.u < 0 || row >= a.rows) return;
+  const Item it = make_item(a, rec.u * a.QB + rec.qb);
+  const int per = a.T * a.g, w = row / per;
+  int h, i;
+  if (!row_of(a, it, w, row - w * per, &h, &i)) return;
+  float M = -INFINITY;
+  // part 0 is in the CTA's second slot, the others in the first of the CTAs after it
+  auto at = [&](int x) { return (size_t)(x == c ? 2 * c + 1 : 2 * x) * a.rows + row; };
+  for (int x = c + lane; x <= rec.last; x += 32) M = fmaxf(M, a.pml[at(x)].x);
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int x = c; x <= rec.last; ++x) {
+    const float2 ml = a.pml[at(x)];
+    const float f = weight_of(ml.x, M);
+    const float4 p = ((const float4*)(a.po + at(x) * kD))[lane];
+    l += f * ml.y;
+    o.x = fmaf(f, p.x, o.x);
+    o.y = fmaf(f, p.y, o.y);
+    o.z = fmaf(f, p.z, o.z);
+    o.w = fmaf(f, p.w, o.w);
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const size_t dst = ((size_t)it.u * a.g + h) * a.t + i;
+  store_row4((T*)a.out + dst * kD + lane * 4,
+             make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  if (a.lse && lane == 0) a.lse[dst] = row_lse(M, l);
+}
+
+int simt_tokens(const CacheShape& s) { return std::min(s.t, kRowTile / s.g); }
+
+template <typename T>
+cudaError_t launch_simt(const AttendArgs& a, int G, cudaStream_t st) {
+  auto kern = k_attend_simt<T>;
+  const uint32_t smem = SimtLayout<T>::kBytes;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  count_launches(1);
+  return launch_kernel(false, 1, kern, dim3(G), kThreads, smem, st, a);
+}
+
+}  // namespace
+
+int attend_rows(const CacheShape& s, bool) { return simt_tokens(s) * s.g; }
+
+cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, const CacheWs& L,
+                          cudaStream_t st) {
+  AttendArgs a{};
+  a.q = io.q;
+  a.k = io.k;
+  a.v = io.v;
+  a.table = io.table;
+  a.len = io.len;
+  a.qlen = io.qlen;
+  a.parent = io.parent;
+  a.out = io.out;
+  a.lse = io.lse;
+  a.U = s.U;
+  a.g = s.g;
+  a.t = s.t;
+  a.P = s.P;
+  a.shift = s.shift;
+  a.cols = s.cols;
+  a.W = s.W;
+  a.s = s.s;
+  a.sl2 = (float)((double)s.scale * 1.4426950408889634);
+  a.rec = (AttendRec*)(ws + L.rec);
+  a.pml = (float2*)(ws + L.pml);
+  a.po = (float*)(ws + L.po);
+  a.status = (int*)(ws + L.status);
+  a.T = simt_tokens(s);
+  a.nq = 1;
+  a.QB = (s.t + a.T - 1) / a.T;
+  a.rows = a.T * s.g;
+  const int G = sm_count();
+  if (G <= 0 || G > kMaxAttendCtas) return cudaErrorInvalidDevice;
+  const bool f32 = s.dtype == GRKV_F32;
+  cudaError_t e = f32 ? launch_simt<float>(a, G, st) : launch_simt<__nv_bfloat16>(a, G, st);
+  if (e != cudaSuccess) return e;
+  count_launches(1);
+  const dim3 grid(G, (a.rows + 7) / 8);
+  return f32 ? launch_kernel(true, 1, k_attend_join<float>, grid, 256, 0, st, a, G)
+             : launch_kernel(true, 1, k_attend_join<__nv_bfloat16>, grid, 256, 0, st, a, G);
+}
+
+}  // namespace grkv
