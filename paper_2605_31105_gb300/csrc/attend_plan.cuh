@@ -295,4 +295,6 @@ __device__ __forceinline__ void store_row4(__nv_bfloat16* p, float4 x) {
   *(uint2*)p = v;
 }
 
+cudaError_t launch_attend_tc(const CacheShape& s, const AttendArgs& a, int G, cudaStream_t st);
+
 }  // namespace grkv

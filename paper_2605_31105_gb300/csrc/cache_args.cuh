@@ -35,7 +35,7 @@ struct CacheWs {
   size_t total;
 };
 
-int attend_rows(const CacheShape& s, bool tree);   // rows of a work item
+int attend_rows(const CacheShape& s);   // rows of a work item
 cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, const CacheWs& L,
                           cudaStream_t st);
 

@@ -266,8 +266,6 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int G) {
   if (a.lse && lane == 0) a.lse[dst] = row_lse(M, l);
 }
 
-int simt_tokens(const CacheShape& s) { return std::min(s.t, kRowTile / s.g); }
-
 template <typename T>
 cudaError_t launch_simt(const AttendArgs& a, int G, cudaStream_t st) {
   auto kern = k_attend_simt<T>;
@@ -280,7 +278,20 @@ cudaError_t launch_simt(const AttendArgs& a, int G, cudaStream_t st) {
 
 }  // namespace
 
-int attend_rows(const CacheShape& s, bool) { return simt_tokens(s) * s.g; }
+// Tokens and row tiles of an item.  bf16 goes to the tensor cores: tiles of 128 rows, two to
+// an item where a unit has more rows than one tile holds.
+static void plan_rows(const CacheShape& s, int* T, int* nq) {
+  const bool tc = s.dtype == GRKV_BF16 && !s.simt;
+  const int most = (tc ? 128 : kRowTile) / s.g;
+  *T = std::min(s.t, most);
+  *nq = tc && s.t > most ? 2 : 1;
+}
+
+int attend_rows(const CacheShape& s) {
+  int T, nq;
+  plan_rows(s, &T, &nq);
+  return T * nq * s.g;
+}
 
 cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, const CacheWs& L,
                           cudaStream_t st) {
@@ -307,14 +318,15 @@ cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, con
   a.pml = (float2*)(ws + L.pml);
   a.po = (float*)(ws + L.po);
   a.status = (int*)(ws + L.status);
-  a.T = simt_tokens(s);
-  a.nq = 1;
-  a.QB = (s.t + a.T - 1) / a.T;
-  a.rows = a.T * s.g;
+  plan_rows(s, &a.T, &a.nq);
+  a.QB = (s.t + a.nq * a.T - 1) / (a.nq * a.T);
+  a.rows = a.nq * a.T * s.g;
   const int G = sm_count();
   if (G <= 0 || G > kMaxAttendCtas) return cudaErrorInvalidDevice;
   const bool f32 = s.dtype == GRKV_F32;
-  cudaError_t e = f32 ? launch_simt<float>(a, G, st) : launch_simt<__nv_bfloat16>(a, G, st);
+  cudaError_t e = f32      ? launch_simt<float>(a, G, st)
+                  : s.simt ? launch_simt<__nv_bfloat16>(a, G, st)
+                           : launch_attend_tc(s, a, G, st);
   if (e != cudaSuccess) return e;
   count_launches(1);
   const dim3 grid(G, (a.rows + 7) / 8);

@@ -76,7 +76,7 @@ CacheWs plan_cache_ws(const CacheShape& s) {
     off = align256(off + bytes);
     return at;
   };
-  const size_t rows = (size_t)std::max(attend_rows(s, false), attend_rows(s, true));
+  const size_t rows = (size_t)attend_rows(s);
   L.status = take(256);
   L.rec = take((size_t)kMaxAttendCtas * 16);
   L.pml = take(2 * (size_t)kMaxAttendCtas * rows * sizeof(float2));

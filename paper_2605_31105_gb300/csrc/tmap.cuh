@@ -10,10 +10,10 @@
 namespace grkv {
 
 // 3-D bf16 tensor [dim2][dim1][dim0] (dim0 contiguous) read in boxes of
-// box0 x box1 x 1 with the 128-byte swizzle; out-of-range cells read as 0.
+// box0 x box1 x box2 with the 128-byte swizzle; out-of-range cells read as 0.
 // Returns false if the driver rejects the description.
 inline bool encode_bf16_3d(CUtensorMap* map, const void* base, uint64_t dim0, uint64_t dim1,
-                           uint64_t dim2, uint32_t box0, uint32_t box1) {
+                           uint64_t dim2, uint32_t box0, uint32_t box1, uint32_t box2 = 1) {
   static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
   if (!fn) {
     cudaDriverEntryPointQueryResult q;
@@ -26,7 +26,7 @@ inline bool encode_bf16_3d(CUtensorMap* map, const void* base, uint64_t dim0, ui
   }
   const cuuint64_t dims[3] = {dim0, dim1, dim2};
   const cuuint64_t strides[2] = {dim0 * 2, dim0 * dim1 * 2};   // bytes, dims 1 and 2
-  const cuuint32_t box[3] = {box0, box1, 1};
+  const cuuint32_t box[3] = {box0, box1, box2};
   const cuuint32_t elem[3] = {1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box,
             elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
