@@ -266,45 +266,58 @@ def cache_params(units, group, pages, page, max_pages, **kw) -> grkv_cache_param
     return p
 
 
-_DTYPES = {GRKV_BF16: "torch.bfloat16", GRKV_F32: "torch.float32"}
+def _fault(name, t, dtype, dev, need):
+    if t.dtype != dtype:
+        return f"{name} is {t.dtype}, the call takes {dtype}"
+    if t.get_device() != dev:
+        return f"{name} is on {t.device}, the workspace on device {dev}"
+    if not t.is_contiguous():
+        return f"{name} is not contiguous"
+    return f"{name} holds {t.numel()} elements, the call takes {need}"
 
 
-def _args(p, ws, rows, words):
-    """Checks the tensors of a cache call (addresses given as ints pass): row data of the
-    call's type, integer arrays of 32 bits (64 where the name starts with first_row), all
-    contiguous, on the device of the workspace, as large as the call reads or writes."""
+def _addresses(p, ws, ws_bytes, stream, rows, words, lse=None):
+    """The addresses of a cache call's tensors, the workspace's address and bytes, and the
+    stream.  Tensors are checked: row data of the call's type, 32-bit integer arrays (64 bits for
+    first_row), contiguous, on the current device like the workspace, as large as the call reads
+    or writes.  Addresses given as ints pass as they are, None where the call allows it."""
     import torch
-    dev = None if isinstance(ws, int) else ws.device
-    if dev is not None and (dev.type != "cuda" or dev.index != torch.cuda.current_device()):
-        raise ValueError("the workspace is not on the current CUDA device")
-    for kind, group in (("row", rows), ("word", words)):
-        for name, (t, need) in group.items():
-            if t is None or isinstance(t, int):
-                continue
-            want = _DTYPES.get(p.dtype) if kind == "row" else (
-                "torch.float32" if name == "lse" else
-                "torch.int64" if name == "first_row" else "torch.int32")
-            if str(t.dtype) != want:
-                raise ValueError(f"{name} is {t.dtype}, the call takes {want}")
-            if dev is not None and t.device != dev:
-                raise ValueError(f"{name} is on {t.device}, the workspace on {dev}")
-            if not t.is_contiguous():
-                raise ValueError(f"{name} is not contiguous")
-            if t.numel() < need:
-                raise ValueError(f"{name} holds {t.numel()} elements, the call takes {need}")
-
-
-def _pool_args(p, k_pages, v_pages):
-    n = p.pages * p.page * p.d
-    return {"k_pages": (k_pages, n), "v_pages": (v_pages, n)}
-
-
-def _table_args(p, lens, **tables):
-    return {**{k: (t, p.units * p.max_pages) for k, t in tables.items()}, "lens": (lens, p.units)}
-
-
-def _nbytes(ws, ws_bytes):
-    return ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    if isinstance(ws, int):
+        dev = None
+    else:
+        dev = ws.get_device()
+        if dev < 0 or dev != torch.cuda.current_device():
+            raise ValueError("the workspace is not on the current CUDA device")
+        if not ws.is_contiguous():
+            raise ValueError("the workspace is not contiguous")
+    row = torch.bfloat16 if p.dtype == GRKV_BF16 else torch.float32
+    out = []
+    for dtype, group in ((row, rows), (torch.int32, words)):
+        for name, t, need in group:
+            if t is not None and not isinstance(t, int):
+                want = torch.int64 if name == "first_row" else dtype
+                at = t.get_device() if dev is None else dev
+                if (t.dtype != want or t.get_device() != at or not t.is_contiguous()
+                        or t.numel() < need):
+                    raise ValueError(_fault(name, t, want, at, need))
+                t = t.data_ptr()
+            out.append(t)
+    if lse is not None:
+        t, need = lse
+        if t is not None and not isinstance(t, int):
+            at = t.get_device() if dev is None else dev
+            if (t.dtype != torch.float32 or t.get_device() != at or not t.is_contiguous()
+                    or t.numel() < need):
+                raise ValueError(_fault("lse", t, torch.float32, at, need))
+            t = t.data_ptr()
+        out.append(t)
+    if stream is None:
+        stream = torch.cuda.current_stream().cuda_stream
+    elif not isinstance(stream, int):
+        stream = stream.cuda_stream
+    if ws_bytes is None:
+        ws_bytes = ws.numel() * ws.element_size()
+    return out, (ws if dev is None else ws.data_ptr()), ws_bytes, stream
 
 
 def grkv_cache_workspace_size(p: grkv_cache_params) -> int:
@@ -317,11 +330,12 @@ def grkv_cache_workspace_size(p: grkv_cache_params) -> int:
 def grkv_cache_reserve(p, table, lens, want, refs, k_pages, v_pages, ws, ws_bytes=None,
                        stream=None, check=True):
     """Own pages for slots [lens, want) of every unit."""
-    _args(p, ws, _pool_args(p, k_pages, v_pages),
-          {**_table_args(p, lens, table=table), "want": (want, p.units), "refs": (refs, p.pages)})
-    rc = load().grkv_cache_reserve(ctypes.byref(p), _ptr(table), _ptr(lens), _ptr(want),
-                                   _ptr(refs), _ptr(k_pages), _ptr(v_pages), _ptr(ws),
-                                   _nbytes(ws, ws_bytes), _stream(stream))
+    u, n = p.units, p.pages * p.page * p.d
+    (k, v, t, le, wa, r), w, nb, st = _addresses(
+        p, ws, ws_bytes, stream, (("k_pages", k_pages, n), ("v_pages", v_pages, n)),
+        (("table", table, u * p.max_pages), ("lens", lens, u), ("want", want, u),
+         ("refs", refs, p.pages)))
+    rc = load().grkv_cache_reserve(ctypes.byref(p), t, le, wa, r, k, v, w, nb, st)
     return _check(rc, "grkv_cache_reserve", check)
 
 
@@ -330,73 +344,79 @@ def grkv_cache_fork(p, src, table_in, lens_in, table_out, lens_out, refs, ws, un
     """Unit u of table_out shares the pages of unit src[u] of table_in (-1: none)."""
     if units_in is None:
         units_in = lens_in.numel()
-    _args(p, ws, {}, {"src": (src, p.units), "table_in": (table_in, units_in * p.max_pages),
-                      "lens_in": (lens_in, units_in),
-                      "table_out": (table_out, p.units * p.max_pages),
-                      "lens_out": (lens_out, p.units), "refs": (refs, p.pages)})
-    rc = load().grkv_cache_fork(ctypes.byref(p), units_in, _ptr(src), _ptr(table_in),
-                                _ptr(lens_in), _ptr(table_out), _ptr(lens_out), _ptr(refs),
-                                _ptr(ws), _nbytes(ws, ws_bytes), _stream(stream))
+    u, m = p.units, p.max_pages
+    (s, ti, li, to, lo, r), w, nb, st = _addresses(
+        p, ws, ws_bytes, stream, (),
+        (("src", src, u), ("table_in", table_in, units_in * m), ("lens_in", lens_in, units_in),
+         ("table_out", table_out, u * m), ("lens_out", lens_out, u), ("refs", refs, p.pages)))
+    rc = load().grkv_cache_fork(ctypes.byref(p), units_in, s, ti, li, to, lo, r, w, nb, st)
     return _check(rc, "grkv_cache_fork", check)
 
 
 def grkv_cache_trim(p, table, lens, refs, ws, ws_bytes=None, stream=None, check=True):
     """Gives back the pages behind lens."""
-    _args(p, ws, {}, {**_table_args(p, lens, table=table), "refs": (refs, p.pages)})
-    rc = load().grkv_cache_trim(ctypes.byref(p), _ptr(table), _ptr(lens), _ptr(refs), _ptr(ws),
-                                _nbytes(ws, ws_bytes), _stream(stream))
+    (t, le, r), w, nb, st = _addresses(
+        p, ws, ws_bytes, stream, (),
+        (("table", table, p.units * p.max_pages), ("lens", lens, p.units), ("refs", refs, p.pages)))
+    rc = load().grkv_cache_trim(ctypes.byref(p), t, le, r, w, nb, st)
     return _check(rc, "grkv_cache_trim", check)
 
 
 def grkv_cache_append(p, k_new, v_new, k_pages, v_pages, table, lens, ws, count=None,
                       first_row=None, ws_bytes=None, stream=None, check=True):
     """New rows to the last `count` of the `lens` slots of every unit."""
-    need = 0 if first_row is not None else p.units * p.tokens * p.d
-    _args(p, ws, {**_pool_args(p, k_pages, v_pages), "k_new": (k_new, need),
-                  "v_new": (v_new, need)},
-          {**_table_args(p, lens, table=table), "count": (count, p.units),
-           "first_row": (first_row, p.units)})
-    rc = load().grkv_cache_append(ctypes.byref(p), _ptr(k_new), _ptr(v_new), _ptr(first_row),
-                                  _ptr(count), _ptr(table), _ptr(lens), _ptr(k_pages),
-                                  _ptr(v_pages), _ptr(ws), _nbytes(ws, ws_bytes), _stream(stream))
+    u, n = p.units, p.pages * p.page * p.d
+    need = 0 if first_row is not None else u * p.tokens * p.d
+    (kn, vn, k, v, t, le, c, f), w, nb, st = _addresses(
+        p, ws, ws_bytes, stream, (("k_new", k_new, need), ("v_new", v_new, need),
+                                  ("k_pages", k_pages, n), ("v_pages", v_pages, n)),
+        (("table", table, u * p.max_pages), ("lens", lens, u), ("count", count, u),
+         ("first_row", first_row, u)))
+    rc = load().grkv_cache_append(ctypes.byref(p), kn, vn, f, c, t, le, k, v, w, nb, st)
     return _check(rc, "grkv_cache_append", check)
 
 
 def grkv_cache_compact(p, idx, k_pages, v_pages, table_in, lens_in, table_out, ws, keep=None,
                        first=None, ws_bytes=None, stream=None, check=True):
     """Slot first + i of table_out takes slot idx[u][i] of table_in."""
-    _args(p, ws, _pool_args(p, k_pages, v_pages),
-          {**_table_args(p, lens_in, table_in=table_in, table_out=table_out),
-           "idx": (idx, p.units * p.tokens), "keep": (keep, p.units), "first": (first, p.units)})
-    rc = load().grkv_cache_compact(ctypes.byref(p), _ptr(idx), _ptr(keep), _ptr(first),
-                                   _ptr(table_in), _ptr(lens_in), _ptr(table_out),
-                                   _ptr(k_pages), _ptr(v_pages), _ptr(ws),
-                                   _nbytes(ws, ws_bytes), _stream(stream))
+    u, n = p.units, p.pages * p.page * p.d
+    (k, v, i, ti, li, to, ke, f), w, nb, st = _addresses(
+        p, ws, ws_bytes, stream, (("k_pages", k_pages, n), ("v_pages", v_pages, n)),
+        (("idx", idx, u * p.tokens), ("table_in", table_in, u * p.max_pages),
+         ("lens_in", lens_in, u), ("table_out", table_out, u * p.max_pages), ("keep", keep, u),
+         ("first", first, u)))
+    rc = load().grkv_cache_compact(ctypes.byref(p), i, ke, f, ti, li, to, k, v, w, nb, st)
     return _check(rc, "grkv_cache_compact", check)
+
+
+def _attend(fn, p, q, k_pages, v_pages, table, lens, q_lens, parent, out, lse, ws, ws_bytes, stream):
+    u, n = p.units, p.pages * p.page * p.d
+    rows = u * p.group * p.tokens
+    words = [("table", table, u * p.max_pages), ("lens", lens, u), ("q_lens", q_lens, u)]
+    if parent is not None:
+        words.append(("parent", parent, u * p.tokens))
+    (q, k, v, o, *rest, ls), w, nb, st = _addresses(
+        p, ws, ws_bytes, stream,
+        (("q", q, rows * p.d), ("k_pages", k_pages, n), ("v_pages", v_pages, n),
+         ("out", out, rows * p.d)), words, (lse, rows))
+    return fn(ctypes.byref(p), q, k, v, *rest, o, ls, w, nb, st)
 
 
 def grkv_attend(p, q, k_pages, v_pages, table, lens, out, ws, q_lens=None, lse=None,
                 ws_bytes=None, stream=None, check=True):
     """Attention of the last q_lens slots of every unit over its pages."""
-    n = p.units * p.group * p.tokens
-    _args(p, ws, {**_pool_args(p, k_pages, v_pages), "q": (q, n * p.d), "out": (out, n * p.d)},
-          {**_table_args(p, lens, table=table), "q_lens": (q_lens, p.units), "lse": (lse, n)})
-    rc = load().grkv_attend(ctypes.byref(p), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(table),
-                            _ptr(lens), _ptr(q_lens), _ptr(out), _ptr(lse), _ptr(ws),
-                            _nbytes(ws, ws_bytes), _stream(stream))
+    rc = _attend(load().grkv_attend, p, q, k_pages, v_pages, table, lens, q_lens, None, out, lse,
+                 ws, ws_bytes, stream)
     return _check(rc, "grkv_attend", check)
 
 
 def grkv_attend_tree(p, q, k_pages, v_pages, table, lens, parent, out, ws, q_lens=None, lse=None,
                      ws_bytes=None, stream=None, check=True):
     """grkv_attend for trees of drafted tokens: parent [U][t], -1 for roots."""
-    n = p.units * p.group * p.tokens
-    _args(p, ws, {**_pool_args(p, k_pages, v_pages), "q": (q, n * p.d), "out": (out, n * p.d)},
-          {**_table_args(p, lens, table=table), "q_lens": (q_lens, p.units), "lse": (lse, n),
-           "parent": (parent, p.units * p.tokens)})
-    rc = load().grkv_attend_tree(ctypes.byref(p), _ptr(q), _ptr(k_pages), _ptr(v_pages),
-                                 _ptr(table), _ptr(lens), _ptr(q_lens), _ptr(parent), _ptr(out),
-                                 _ptr(lse), _ptr(ws), _nbytes(ws, ws_bytes), _stream(stream))
+    if parent is None:
+        parent = 0
+    rc = _attend(load().grkv_attend_tree, p, q, k_pages, v_pages, table, lens, q_lens, parent,
+                 out, lse, ws, ws_bytes, stream)
     return _check(rc, "grkv_attend_tree", check)
 
 

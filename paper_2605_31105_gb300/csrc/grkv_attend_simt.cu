@@ -222,10 +222,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_simt(AttendArgs a) {
 }
 
 // Adds up the partial results of the split items, and writes the call's status.  Block
-// (c, y) takes 8 rows of the item that starts in CTA c, a warp each.
-template <typename T>
+// (c, y) takes rows of the item that starts in CTA c: a warp each, or, where items have few
+// rows and so may have many parts, one row whose parts go round the eight warps.
+template <typename T, bool kFewRows>
 __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int G) {
   chain_wait();
+  __shared__ float4 sum_o[8][32];
+  __shared__ float sum_l[8];
   const int c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (c == 0 && blockIdx.y == 0 && warp == 0) {
     int err = 0;
@@ -234,7 +237,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int G) {
     if (lane == 0) *a.status = err;
   }
   const AttendRec rec = a.rec[c];
-  const int row = blockIdx.y * 8 + warp;
+  const int row = kFewRows ? blockIdx.y : blockIdx.y * 8 + warp;
   if (rec.u < 0 || row >= a.rows) return;
   const Item it = make_item(a, rec.u * a.QB + rec.qb);
   const int per = a.T * a.g, w = row / per;
@@ -249,7 +252,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int G) {
   float l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int x = c; x <= rec.last; ++x) {
+  for (int x = c + (kFewRows ? warp : 0); x <= rec.last; x += kFewRows ? 8 : 1) {
     const float2 ml = a.pml[at(x)];
     const float f = weight_of(ml.x, M);
     const float4 p = ((const float4*)(a.po + at(x) * kD))[lane];
@@ -259,11 +262,34 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int G) {
     o.z = fmaf(f, p.z, o.z);
     o.w = fmaf(f, p.w, o.w);
   }
+  if (kFewRows) {
+    sum_o[warp][lane] = o;
+    if (lane == 0) sum_l[warp] = l;
+    __syncthreads();   // the block has one row: all of its warps are here
+    if (warp > 0) return;
+#pragma unroll
+    for (int x = 1; x < 8; ++x) {
+      const float4 p = sum_o[x][lane];
+      l += sum_l[x];
+      o.x += p.x;
+      o.y += p.y;
+      o.z += p.z;
+      o.w += p.w;
+    }
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const size_t dst = ((size_t)it.u * a.g + h) * a.t + i;
   store_row4((T*)a.out + dst * kD + lane * 4,
              make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
   if (a.lse && lane == 0) a.lse[dst] = row_lse(M, l);
+}
+
+template <typename T>
+cudaError_t launch_join(const AttendArgs& a, int G, cudaStream_t st) {
+  count_launches(1);
+  if (a.rows <= 16)
+    return launch_kernel(true, 1, k_attend_join<T, true>, dim3(G, a.rows), 256, 0, st, a, G);
+  return launch_kernel(true, 1, k_attend_join<T, false>, dim3(G, (a.rows + 7) / 8), 256, 0, st, a, G);
 }
 
 template <typename T>
@@ -328,10 +354,7 @@ cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, con
                   : s.simt ? launch_simt<__nv_bfloat16>(a, G, st)
                            : launch_attend_tc(s, a, G, st);
   if (e != cudaSuccess) return e;
-  count_launches(1);
-  const dim3 grid(G, (a.rows + 7) / 8);
-  return f32 ? launch_kernel(true, 1, k_attend_join<float>, grid, 256, 0, st, a, G)
-             : launch_kernel(true, 1, k_attend_join<__nv_bfloat16>, grid, 256, 0, st, a, G);
+  return f32 ? launch_join<float>(a, G, st) : launch_join<__nv_bfloat16>(a, G, st);
 }
 
 }  // namespace grkv

@@ -12,6 +12,7 @@
 // on one row tile (two-tile items) or one slot tile (one-tile items) while the softmax
 // works on the other.  Warps 4-7 (and 8-11 for the second row tile) do the softmax: a
 // thread owns one row, one TMEM lane, and holds the tile's 128 logits in registers.
+// Warps 2-3 search the V of masked tiles (below).
 //
 // The reference of a row is its maximum so far, but it is only moved when the tile's maximum is
 // more than 8 above it in log2 units: P stays below 2^8 (bf16 keeps its relative
@@ -36,7 +37,7 @@ using namespace sm100;
 
 constexpr int kRows = 128;                                    // rows of a tile, TMEM lanes
 constexpr uint32_t kTileBytes = kSlotTile * kD * 2;           // 32 KB
-constexpr int kRing = 4;                                      // K and V tiles in flight
+constexpr int kRing = 4;   // tiles in flight: K in the even slots, V in the odd ones
 constexpr long long kWaitBudget = 1ll << 32;                  // cycles (~2 s)
 constexpr int kMaxEdges = 16;   // masked tiles of a segment: at most 4 at each end of the
                                 // window (256 tokens) and one at the sinks' end
@@ -61,7 +62,7 @@ struct TcBars {
   uint64_t ring_full[kRing], ring_empty[kRing];
   uint64_t q_full[2], q_empty[2];
   uint64_t s_full[2], p_full[2], pv_done[2];
-  uint64_t searched[4];   // V of a masked tile has been searched
+  uint64_t searched[4];   // V of a masked tile has been searched (uses in turn)
   uint64_t drain;
   uint32_t tmem;
   int abort;
@@ -79,6 +80,17 @@ struct Ring {
   }
 };
 
+// With two row tiles the softmax threads, which hold 128 logits each, get registers of the
+// other warpgroup: 128 x 72 + 256 x 208 = 62464 of the 384 x 168 = 64512 at launch.
+template <int NQ>
+__device__ __forceinline__ void fewer_regs() {
+  if (NQ == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+}
+template <int NQ>
+__device__ __forceinline__ void more_regs() {
+  if (NQ == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+}
+
 __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort, kWaitBudget));
 }
@@ -95,32 +107,28 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 
 __device__ __forceinline__ bool nonfinite16(uint32_t h) { return (h & 0x7f80u) == 0x7f80u; }
 
-// Searches one row of a V tile (two 128-byte halves) for non-finite elements and zeroes them.
+// Searches one row of a V tile (two 128-byte halves) for non-finite elements and zeroes
+// them.  x 0 + sum stays zero over finite elements and NaN from the first other one on.
 __device__ __forceinline__ bool clean_row(uint8_t* tile, int row) {
-  bool found = false;
-#pragma unroll 1
-  for (int h = 0; h < 2; ++h) {
-    uint4* p = (uint4*)(tile + h * (kTileBytes / 2) + row * 128);
+  uint32_t sum = 0;
 #pragma unroll
-    for (int c0 = 0; c0 < 8; ++c0) {
-      const int c = (c0 + row) & 7;   // lanes on different banks
-      uint4 x = p[c];
-      uint32_t* w = (uint32_t*)&x;
-      bool any = false;
+  for (int c0 = 0; c0 < 16; ++c0) {
+    const int c = ((c0 & 7) + row) & 7;   // lanes on different banks
+    const uint4 x = *(const uint4*)(tile + (c0 >> 3) * (kTileBytes / 2) + row * 128 + c * 16);
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) any |= nonfinite16(w[i]) || nonfinite16(w[i] >> 16);
-      if (any) {
-        found = true;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (nonfinite16(w[i])) w[i] &= 0xffff0000u;
-          if (nonfinite16(w[i] >> 16)) w[i] &= 0x0000ffffu;
-        }
-        p[c] = x;
-      }
-    }
+    for (int i = 0; i < 4; ++i)
+      asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(w[i]), "r"(0u));
   }
-  return found;
+  if (!nonfinite16(sum) && !nonfinite16(sum >> 16)) return false;
+  for (int c = 0; c < 64; ++c) {
+    uint32_t* w = (uint32_t*)(tile + (c >> 5) * (kTileBytes / 2) + row * 128) + (c & 31);
+    uint32_t x = *w;
+    if (nonfinite16(x)) x &= 0xffff0000u;
+    if (nonfinite16(x >> 16)) x &= 0x0000ffffu;
+    *w = x;
+  }
+  return true;
 }
 
 // Adds to columns [c0, c0 + 32) of a row's output the non-finite values of the slots that it sees.
@@ -164,7 +172,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
   if (tid == 0) {
     for (int i = 0; i < kRing; ++i) {
       mbar_init(&bars->ring_full[i], 1);
-      mbar_init(&bars->ring_empty[i], 1);
+      mbar_init(&bars->ring_empty[i], i & 1 ? 3 : 1);   // V: the product and both searchers
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars->q_full[i], 1);
@@ -173,7 +181,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
       mbar_init(&bars->p_full[i], 4);
       mbar_init(&bars->pv_done[i], 1);
     }
-    for (int i = 0; i < 4; ++i) mbar_init(&bars->searched[i], 4);
+    for (int i = 0; i < 4; ++i) mbar_init(&bars->searched[i], 2);
     mbar_init(&bars->drain, 1);
     bars->abort = 0;
     fence_mbar_init();
@@ -191,6 +199,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
 
   if (warp == 0) {
     // -------------------------------------------------------------- producer
+    fewer_regs<NQ>();
     if (lane == 0) {
       prefetch_tensormap(&tmQ);
       prefetch_tensormap(&tmK);
@@ -251,6 +260,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
     __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------- MMA issuer
+    fewer_regs<NQ>();
     // Job n is row tile w of a slot tile; it uses S buffer n & 1.
     constexpr uint32_t id_s = idesc_bf16(kRows, kSlotTile, 0, 0);   // S = Q K^T, both K-major
     constexpr uint32_t id_o = idesc_bf16(kRows, kD, 0, 1);          // O += P V, V MN-major
@@ -263,6 +273,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
     vp.add(1);
     uint32_t qn = 0, vn = 0;   // jobs whose S / output products have been issued
     int qk = 0, qseg = 0, vk = 0, vseg = 0;
+    uint32_t edges = 0;
     bool ok = true;
     auto issue_s = [&]() -> bool {   // the next slot tile's S products: NQ jobs, or one of them
       const int w = NQ == 2 ? (int)(qn & 1) : 0, b = qseg % Lay::kQBufs;
@@ -292,7 +303,14 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
     while (ok && vs.more()) {
       const int w = NQ == 2 ? (int)(vn & 1) : 0;
       ok = wait_warp(&bars->p_full[vn & 1], (vn >> 1) & 1, abort_flag);
-      if (ok && w == 0) ok = wait_warp(&bars->ring_full[vp.slot], vp.phase, abort_flag);
+      if (ok && w == 0) {
+        ok = wait_warp(&bars->ring_full[vp.slot], vp.phase, abort_flag);
+        const Item& it = vs.it;
+        if (ok && !tile_full(a, it, it.tok0, it.ntok, it.tile(vs.off + vk))) {
+          ok = wait_warp(&bars->searched[edges & 3], (edges >> 2) & 1, abort_flag);
+          ++edges;
+        }
+      }
       if (!ok) break;
       tc_fence_after();
       const int o = NQ == 2 ? w : vseg & 1;
@@ -316,15 +334,51 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
     volatile int no_abort = 0;
     mbar_wait(&bars->drain, 0, &no_abort, kWaitBudget);
     __syncwarp();
-  } else if (warp >= 4) {
+  } else if (warp < 4) {
+    // --------------------------------------------------- search of masked tiles' V
+    fewer_regs<NQ>();
+    // Two warps, two rows a lane.  They pass every V tile in turn, masked or not, and a V slot is
+    // not filled again before they have: so a parity always means the use that they are at,
+    // and they are ahead of the softmax by at most the ring's two V tiles, which four marks
+    // and four segments' words cover.
+    uint32_t edges = 0;
+    int seg = 0;
+    Ring vp;
+    vp.add(1);
+    bool ok = true;
+    for (Segments sg(a, run); ok && sg.more(); sg.next(a), ++seg) {
+      const Item& it = sg.it;
+      int e = 0;
+      for (int k = 0; ok && k < sg.cnt; ++k, vp.add(2)) {
+        ok = wait_warp(&bars->ring_full[vp.slot], vp.phase, abort_flag);
+        if (!ok) break;
+        if (tile_full(a, it, it.tok0, it.ntok, it.tile(sg.off + k))) {
+          if (lane == 0) mbar_arrive(&bars->ring_empty[vp.slot]);
+          continue;
+        }
+        uint8_t* tile = sm + Lay::kOffRing + vp.slot * kTileBytes;
+        uint32_t* words = (uint32_t*)(bad_all + (seg & 3) * kMaxEdges + e);
+#pragma unroll 1
+        for (int r = 0; r < 2; ++r) {
+          const int q = (warp - 2) * 2 + r;
+          const uint32_t bits = __ballot_sync(0xffffffffu, clean_row(tile, q * 32 + lane));
+          if (lane == 0 && e < kMaxEdges) words[q] = bits;
+          if (bits) fence_proxy_async_smem();
+        }
+        arrive_warp(&bars->searched[edges & 3], lane);
+        if (lane == 0) mbar_arrive(&bars->ring_empty[vp.slot]);
+        ++edges;
+        ++e;
+      }
+    }
+  } else {
     // ---------------------------------------------------------------- softmax
+    more_regs<NQ>();
     const int w = (warp - 4) >> 2, q = warp & 3, row = q * 32 + lane;
     const uint32_t lane_addr = tmem + ((uint32_t)(q * 32) << 16);
     uint32_t* anc = (uint32_t*)(sm + Lay::kOffAnc) + (w * kRows + row) * (kMaxTree / 32);
     uint32_t n = w, edges = 0;
     int seg = 0;
-    Ring vp;
-    vp.add(1);
     bool ok = true;
     for (Segments sg(a, run); ok && sg.more(); sg.next(a), ++seg) {
       const Item& it = sg.it;
@@ -342,27 +396,10 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
       auto done = [&](uint32_t job) {
         return wait_warp(&bars->pv_done[job & 1], (job >> 1) & 1, abort_flag);
       };
-      for (int k = 0; k < sg.cnt; ++k, n += NQ, vp.add(2)) {
+      for (int k = 0; k < sg.cnt; ++k, n += NQ) {
         const int tile = it.tile(sg.off + k);
         const bool edge = !tile_full(a, it, it.tok0, it.ntok, tile);
         const uint32_t scol = (n & 1) * kSlotTile;
-        if (edge) {
-          if (w == 0) {
-            ok = wait_warp(&bars->ring_full[vp.slot], vp.phase, abort_flag);
-            if (!ok) break;
-            const bool found = clean_row(sm + Lay::kOffRing + vp.slot * kTileBytes, row);
-            const uint32_t bits = __ballot_sync(0xffffffffu, found);
-            if (lane == 0 && e < kMaxEdges) ((uint32_t*)(bad + e))[q] = bits;
-            if (bits) fence_proxy_async_smem();
-            arrive_warp(&bars->searched[edges & 3], lane);
-          }
-          ok = wait_warp(&bars->searched[edges & 3], (edges >> 2) & 1, abort_flag);
-          if (!ok) break;
-          const uint4 b = bad[min(e, kMaxEdges - 1)];
-          any_bad |= (b.x | b.y | b.z | b.w) != 0;
-          ++e;
-          ++edges;
-        }
         ok = wait_warp(&bars->s_full[n & 1], (n >> 1) & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
@@ -376,6 +413,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
               const uint32_t m = vis.word(tile * kSlotTile + 32 * c);
+              if (__all_sync(0xffffffffu, m == 0xffffffffu)) continue;
 #pragma unroll
               for (int x = 0; x < 32; ++x)
                 if (!((m >> x) & 1)) v[32 * c + x] = -INFINITY;
@@ -437,6 +475,14 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
         }
         tc_fence_before();
         arrive_warp(&bars->p_full[n & 1], lane);
+        if (edge) {   // after the arrival: the product with V waits for the search as well
+          ok = wait_warp(&bars->searched[edges & 3], (edges >> 2) & 1, abort_flag);
+          if (!ok) break;
+          const uint4 b = bad[min(e, kMaxEdges - 1)];
+          any_bad |= (b.x | b.y | b.z | b.w) != 0;
+          ++e;
+          ++edges;
+        }
       }
       if (!ok) break;
       // ------------------------------------------------------------ the rows' results
