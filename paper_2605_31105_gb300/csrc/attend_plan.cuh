@@ -49,14 +49,13 @@ struct Item {
   __device__ bool wanted(int a, int b) const { return a < sink_end || (a < hi && b > lo); }
 };
 
-__device__ __forceinline__ Item make_item(const AttendArgs& a, int item) {
+// Item qb of a unit whose length and tokens (clamped) are known.
+__device__ __forceinline__ Item make_item(const AttendArgs& a, int u, int qb, int L, int T) {
   Item it;
-  it.u = item / a.QB;
-  const int L = a.len[it.u], cap = a.cols << a.shift;
-  it.L = min(max(L, 0), cap);
-  const int T = a.qlen ? min(max(a.qlen[it.u], 0), a.t) : a.t;
-  it.base = it.L - T;
-  it.tok0 = (item - it.u * a.QB) * a.nq * a.T;
+  it.u = u;
+  it.L = L;
+  it.base = L - T;
+  it.tok0 = qb * a.nq * a.T;
   it.ntok = max(0, min(T - it.tok0, a.nq * a.T));
   const bool tree = a.parent != nullptr;
   const int p0 = it.base + (tree ? 0 : it.tok0);   // the first position of a row
@@ -69,6 +68,16 @@ __device__ __forceinline__ Item make_item(const AttendArgs& a, int item) {
   if (it.ntok == 0) it.nt = 0;
   else if (it.nt < 1) it.nt = 1;   // rows that see nothing are written by a tile without slots
   return it;
+}
+
+__device__ __forceinline__ int unit_len(const AttendArgs& a, int u) {
+  return min(max(__ldg(a.len + u), 0), a.cols << a.shift);
+}
+__device__ __forceinline__ int unit_tokens(const AttendArgs& a, int u) {
+  return a.qlen ? min(max(__ldg(a.qlen + u), 0), a.t) : a.t;
+}
+__device__ __forceinline__ Item make_item(const AttendArgs& a, int u, int qb) {
+  return make_item(a, u, qb, unit_len(a, u), unit_tokens(a, u));
 }
 
 // Whether every row of tokens [t0, t0 + n) of the item sees the whole slot tile.
@@ -149,7 +158,7 @@ __device__ __forceinline__ RowVis row_vis(const AttendArgs& a, const Item& it, i
 struct Run {
   long long total;   // tiles of all items
   int G;             // CTAs that have any
-  int item, off;     // first item and its first tile here
+  int u, qb, off;    // first item and its first tile here
   int left;          // tiles of the run
   __device__ long long start(int c) const { return total * c / G; }
   __device__ int owner(long long t) const { return (int)(((t + 1) * G + total - 1) / total) - 1; }
@@ -175,16 +184,23 @@ __device__ __forceinline__ void plan_run(const AttendArgs& a, PlanSmem* ps, int 
   const int per = (items + n - 1) / n, i0 = min(items, tid * per), i1 = min(items, i0 + per);
   if (tid == 0) {
     ps->err = 0;
-    ps->run = Run{0, 1, 0, 0, 0};
+    ps->run = Run{0, 1, 0, 0, 0, 0};
     ps->rec = AttendRec{-1, 0, 0, 0};
   }
   __syncthreads();
+  const int first_u = i0 / a.QB, first_qb = i0 - first_u * a.QB;
   long long mine = 0;
-  for (int i = i0; i < i1; ++i) {
-    const Item it = make_item(a, i);
-    mine += it.nt;
-    if (it.L != a.len[it.u] || (a.qlen && (a.qlen[it.u] < 0 || a.qlen[it.u] > a.t)))
-      ps->err = GRKV_ERR_INVALID_ARG;
+  for (int i = i0, u = first_u, qb = first_qb, L = 0, T = 0; i < i1; ++i) {
+    if (i == i0 || qb == 0) {
+      L = unit_len(a, u);
+      T = unit_tokens(a, u);
+      if (L != __ldg(a.len + u) || (a.qlen && T != __ldg(a.qlen + u))) ps->err = GRKV_ERR_INVALID_ARG;
+    }
+    mine += make_item(a, u, qb, L, T).nt;
+    if (++qb == a.QB) {
+      qb = 0;
+      ++u;
+    }
   }
   long long scan = mine;
 #pragma unroll
@@ -213,18 +229,23 @@ __device__ __forceinline__ void plan_run(const AttendArgs& a, PlanSmem* ps, int 
     const bool last = before < t1 && t1 <= before + mine;
     if (c < r.G && (first || last)) {
       long long at = before;
-      for (int i = i0; i < i1; ++i) {
-        const int nt = make_item(a, i).nt;
+      for (int i = i0, u = first_u, qb = first_qb; i < i1; ++i) {
+        const int nt = make_item(a, u, qb).nt;
         if (at <= t0 && t0 < at + nt) {
-          r.item = i;
+          r.u = u;
+          r.qb = qb;
           r.off = (int)(t0 - at);
           r.left = (int)(t1 - t0);
           ps->run = r;
         }
         if (t0 <= at && at < t1 && t1 < at + nt)
-          ps->rec = AttendRec{i / a.QB, i % a.QB, r.owner(at + nt - 1), 0};
+          ps->rec = AttendRec{u, qb, r.owner(at + nt - 1), 0};
         at += nt;
         if (at >= t1) break;
+        if (++qb == a.QB) {
+          qb = 0;
+          ++u;
+        }
       }
     }
   }
@@ -234,13 +255,20 @@ __device__ __forceinline__ void plan_run(const AttendArgs& a, PlanSmem* ps, int 
 // A CTA's segments in order: each is a run of tiles of one item.
 struct Segments {
   Item it;
-  int item, off, cnt, left;
-  __device__ Segments(const AttendArgs& a, const Run& r)
-      : item(r.item), off(r.off), left(r.left) {
-    if (left > 0) load(a);
+  int qb, off, cnt, left, L, T;
+  __device__ Segments(const AttendArgs& a, const Run& r) : qb(r.qb), off(r.off), left(r.left) {
+    it.u = r.u;
+    if (left > 0) {
+      unit(a);
+      load(a);
+    }
+  }
+  __device__ void unit(const AttendArgs& a) {
+    L = unit_len(a, it.u);
+    T = unit_tokens(a, it.u);
   }
   __device__ void load(const AttendArgs& a) {
-    it = make_item(a, item);
+    it = make_item(a, it.u, qb, L, T);
     cnt = min(left, it.nt - off);
   }
   __device__ bool more() const { return left > 0; }
@@ -249,13 +277,15 @@ struct Segments {
   __device__ void next(const AttendArgs& a) {
     left -= cnt;
     off = 0;
-    ++item;
     if (left <= 0) return;
-    load(a);
-    while (it.nt == 0) {   // items without rows; left > 0 says that one with rows follows
-      ++item;
+    do {   // items without rows are passed; left > 0 says that one with rows follows
+      if (++qb == a.QB) {
+        qb = 0;
+        ++it.u;
+        unit(a);
+      }
       load(a);
-    }
+    } while (it.nt == 0);
   }
 };
 

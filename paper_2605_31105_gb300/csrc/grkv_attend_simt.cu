@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int G) {
   const AttendRec rec = a.rec[c];
   const int row = kFewRows ? blockIdx.y : blockIdx.y * 8 + warp;
   if (rec.u < 0 || row >= a.rows) return;
-  const Item it = make_item(a, rec.u * a.QB + rec.qb);
+  const Item it = make_item(a, rec.u, rec.qb);
   const int per = a.T * a.g, w = row / per;
   int h, i;
   if (!row_of(a, it, w, row - w * per, &h, &i)) return;

@@ -54,7 +54,8 @@ struct TcLayout {
   static constexpr uint32_t kOffBad = kOffAnc + NQ * kRows * (kMaxTree / 8);
   static constexpr uint32_t kOffBar = kOffBad + 4 * kMaxEdges * 16;
   static constexpr uint32_t kOffPlan = kOffBar + 512;
-  static constexpr uint32_t kBytes = kOffPlan + 1024 + 1024;   // + alignment slack
+  static constexpr uint32_t kOffStage = kOffPlan + 1024;   // 2 KB a softmax warp
+  static constexpr uint32_t kBytes = kOffStage + NQ * 4 * 2048 + 1024;   // + alignment slack
 };
 static_assert(TcLayout<2>::kBytes <= 227 * 1024 && sizeof(PlanSmem) <= 1024, "smem");
 
@@ -105,6 +106,54 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
+__device__ __forceinline__ float max128(const float* v) {
+  float m[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    m[c] = max3(v[c], v[4 + c], v[8 + c]);
+#pragma unroll
+    for (int x = 12; x < 124; x += 8) m[c] = max3(m[c], v[x + c], v[x + 4 + c]);
+    m[c] = fmaxf(m[c], v[124 + c]);
+  }
+  return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+}
+
+// exp2(v sl2 - ref) of 64 logits as bf16 pairs; the sum (two partial ones) is of the
+// values before rounding.  A row that has seen nothing has v = ref = -inf and gets zeros.
+__device__ __forceinline__ uint64_t half_exp(const float* v, float sl2, float ref, uint32_t pk[2][16]) {
+  const float r = ref == -INFINITY ? 0.f : ref;
+  const uint64_t s2 = pack2(sl2, sl2), m2 = pack2(-r, -r);
+  uint64_t acc[2] = {0, 0};
+#pragma unroll
+  for (int x = 0; x < 32; ++x) {
+    float p0, p1;
+    unpack2(fma2(pack2(v[2 * x], v[2 * x + 1]), s2, m2), p0, p1);
+    p0 = fast_exp2(p0);
+    p1 = fast_exp2(p1);
+    acc[x & 1] = add2(acc[x & 1], pack2(p0, p1));
+    pk[x >> 4][x & 15] = pack_bf16(p0, p1);
+  }
+  return add2(acc[0], acc[1]);
+}
+
+// Stores 64 bytes of each of a warp's 32 rows, x this lane's, through shared memory so that four
+// lanes write a row's 64 bytes together (a lane to a row, every store touches 32 lines:
+// an item's end took 8 K cycles of the load-store unit).  rows[j] is the index of row
+// 8 j + lane / 4 in the array at base, or negative.
+__device__ __forceinline__ void store_rows(uint8_t* stage, int lane, const uint4* x, const int* rows,
+                                           uint8_t* base, size_t row_bytes) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) *(uint4*)(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = x[c];
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int r = 8 * j + (lane >> 2), c = lane & 3;
+    const uint4 y = *(const uint4*)(stage + r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
+    if (rows[j] >= 0) *(uint4*)(base + (size_t)rows[j] * row_bytes + c * 16) = y;
+  }
+  __syncwarp();
+}
+
 __device__ __forceinline__ bool nonfinite16(uint32_t h) { return (h & 0x7f80u) == 0x7f80u; }
 
 // Searches one row of a V tile (two 128-byte halves) for non-finite elements and zeroes
@@ -131,29 +180,41 @@ __device__ __forceinline__ bool clean_row(uint8_t* tile, int row) {
   return true;
 }
 
-// Adds to columns [c0, c0 + 32) of a row's output the non-finite values of the slots that it sees.
+// Adds the non-finite values of the slots that a row sees to its output in TMEM (all lanes of the
+// warp).  A function of its own: the epilogue's registers stay registers.
 __device__ __noinline__ void add_bad(const AttendArgs& a, const Item& it, int off, int cnt,
-                                     const RowVis& vis, const uint4* bad, int c0, float* o) {
-  int e = 0, err = 0;
-  for (int k = 0; k < cnt; ++k) {
-    const int tile = it.tile(off + k);
-    if (tile_full(a, it, it.tok0, it.ntok, tile)) continue;
-    const uint4 words = bad[min(e, kMaxEdges - 1)];
-    const uint32_t w[4] = {words.x, words.y, words.z, words.w};
-    ++e;
-    for (int i = 0; i < 4; ++i) {
-      const int x = tile * kSlotTile + 32 * i;
-      for (uint32_t m = w[i] & vis.word(x); m; m &= m - 1) {
-        const int slot = x + __ffs(m) - 1, c = slot >> a.shift;
-        const size_t row = ((size_t)page_of(a, it.u, c, &err) << a.shift) + (slot & ((1 << a.shift) - 1));
-        const __nv_bfloat16* v = (const __nv_bfloat16*)a.v + row * kD + c0;
-        for (int j = 0; j < 32; ++j) {
-          const float y = __bfloat162float(v[j]);
-          if (!isfinite(y)) o[j] += y;
+                                     const RowVis& vis, const uint4* bad, bool live, uint32_t taddr) {
+  int err = 0;
+  for (int c0 = 0; c0 < kD; c0 += 32) {
+    float o[32];
+    tmem_ld32f(taddr + c0, o);
+    tmem_wait32(o);
+    int e = 0;
+    for (int k = 0; live && k < cnt; ++k) {
+      const int tile = it.tile(off + k);
+      if (tile_full(a, it, it.tok0, it.ntok, tile)) continue;
+      const uint4 words = bad[min(e, kMaxEdges - 1)];
+      const uint32_t w[4] = {words.x, words.y, words.z, words.w};
+      ++e;
+      for (int i = 0; i < 4; ++i) {
+        const int x = tile * kSlotTile + 32 * i;
+        for (uint32_t m = w[i] & vis.word(x); m; m &= m - 1) {
+          const int slot = x + __ffs(m) - 1, c = slot >> a.shift;
+          const size_t row =
+              ((size_t)page_of(a, it.u, c, &err) << a.shift) + (slot & ((1 << a.shift) - 1));
+          const __nv_bfloat16* v = (const __nv_bfloat16*)a.v + row * kD + c0;
+          for (int j = 0; j < 32; ++j) {
+            const float y = __bfloat162float(v[j]);
+            if (!isfinite(y)) o[j] += y;
+          }
         }
       }
     }
+    __syncwarp();
+    tmem_st16(taddr + c0, (uint32_t*)o);
+    tmem_st16(taddr + c0 + 16, (uint32_t*)o + 16);
   }
+  tmem_st_wait();
 }
 
 template <int NQ>
@@ -313,9 +374,9 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
       }
       if (!ok) break;
       tc_fence_after();
-      const int o = NQ == 2 ? w : vseg & 1;
-      mma8_ts<id_o, false>(tmem + kColO + o * kD, tmem + (vn & 1) * kSlotTile,
-                           v_desc + vp.slot * kTileDesc, vk > 0);
+      const uint32_t o = tmem + kColO + (NQ == 2 ? w : vseg & 1) * kD, p = tmem + (vn & 1) * kSlotTile;
+      const uint64_t v = v_desc + vp.slot * kTileDesc;
+      mma8_ts<id_o, false>(o, p, v, vk > 0);
       mma_commit_elect(&bars->pv_done[vn & 1]);
       ++vn;
       if (w == NQ - 1) {
@@ -419,57 +480,36 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
                 if (!((m >> x) & 1)) v[32 * c + x] = -INFINITY;
             }
           }
-          float t4[4];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            t4[c] = max3(v[c], v[4 + c], v[8 + c]);
-#pragma unroll
-            for (int x = 12; x < 124; x += 8) t4[c] = max3(t4[c], v[x + c], v[x + 4 + c]);
-            t4[c] = fmaxf(t4[c], v[124 + c]);
-          }
-          const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * a.sl2;
-          if (k == 0) {
-            ref = top;
-          } else {
-            const bool move = live && top > ref + kSlack;
-            if (__any_sync(0xffffffffu, move)) {
-              ok = done(n - NQ);
-              if (!ok) break;
-              tc_fence_after();
-              const float f = move ? fast_exp2(ref - top) : 1.f;
-              l *= f;
-              if (move) ref = top;
+          const float top = max128(v) * a.sl2;
+          if (k == 0) ref = top;
+          const bool move = live && top > ref + kSlack;
+          if (__any_sync(0xffffffffu, move)) {
+            ok = done(n - NQ);
+            if (!ok) break;
+            tc_fence_after();
+            const float f = move ? fast_exp2(ref - top) : 1.f;
+            l *= f;
+            if (move) ref = top;
 #pragma unroll 1
-              for (int c = 0; c < 4; ++c) {
-                float o[32];
-                tmem_ld32f(lane_addr + ocol + 32 * c, o);
-                tmem_wait32(o);
+            for (int c = 0; c < 4; ++c) {
+              float o[32];
+              tmem_ld32f(lane_addr + ocol + 32 * c, o);
+              tmem_wait32(o);
 #pragma unroll
-                for (int x = 0; x < 32; ++x) o[x] *= f;
-                tmem_st16(lane_addr + ocol + 32 * c, (uint32_t*)o);
-                tmem_st16(lane_addr + ocol + 32 * c + 16, (uint32_t*)o + 16);
-              }
+              for (int x = 0; x < 32; ++x) o[x] *= f;
+              tmem_st16(lane_addr + ocol + 32 * c, (uint32_t*)o);
+              tmem_st16(lane_addr + ocol + 32 * c + 16, (uint32_t*)o + 16);
             }
           }
-          const float r = ref == -INFINITY ? 0.f : ref;
-          const uint64_t s2 = pack2(a.sl2, a.sl2), m2 = pack2(-r, -r);
-          uint64_t acc[2] = {0, 0};
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t pk[16];
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              float p0, p1;
-              unpack2(fma2(pack2(v[32 * c + 2 * x], v[32 * c + 2 * x + 1]), s2, m2), p0, p1);
-              p0 = fast_exp2(p0);
-              p1 = fast_exp2(p1);
-              acc[x & 1] = add2(acc[x & 1], pack2(p0, p1));
-              pk[x] = pack_bf16(p0, p1);
-            }
-            tmem_st16(lane_addr + scol + 32 * c, pk);
-          }
+          uint32_t pk[2][16];
+          uint64_t sum = half_exp(v, a.sl2, ref, pk);
+          tmem_st16(lane_addr + scol, pk[0]);
+          tmem_st16(lane_addr + scol + 32, pk[1]);
+          sum = add2(sum, half_exp(v + 64, a.sl2, ref, pk));
+          tmem_st16(lane_addr + scol + 64, pk[0]);
+          tmem_st16(lane_addr + scol + 96, pk[1]);
           float l0, l1;
-          unpack2(add2(acc[0], acc[1]), l0, l1);
+          unpack2(sum, l0, l1);
           l += l0 + l1;
           tmem_st_wait();
         }
@@ -490,35 +530,45 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
       if (!ok) break;
       tc_fence_after();
       if (!warp_live) continue;
+      if (__any_sync(0xffffffffu, any_bad))
+        add_bad(a, it, sg.off, sg.cnt, vis, bad, live, lane_addr + ocol);
       const bool whole = sg.whole();
       const float f = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
-      const size_t dst = ((size_t)it.u * a.g + h) * a.t + i;
-      const size_t part = (size_t)sg.slot(blockIdx.x) * a.rows + w * a.T * a.g + row;
+      // rows of out and lse, or of the CTA's part; both counts fit 32 bits
+      const int dst = whole ? ((it.u * a.g + h) * a.t + i)
+                            : sg.slot(blockIdx.x) * a.rows + w * a.T * a.g + row;
+      int rows[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        rows[j] = __shfl_sync(0xffffffffu, live ? dst : -1, 8 * j + (lane >> 2));
+      uint8_t* stage = sm + Lay::kOffStage + (warp - 4) * 2048;
 #pragma unroll 1
       for (int c = 0; c < 4; ++c) {
         float o[32];
         tmem_ld32f(lane_addr + ocol + 32 * c, o);
         tmem_wait32(o);
-        if (live && any_bad) add_bad(a, it, sg.off, sg.cnt, vis, bad, 32 * c, o);
-        if (live && whole) {
-          uint4* p = (uint4*)((__nv_bfloat16*)a.out + dst * kD + 32 * c);
+        uint4 x[4];
+        if (whole) {
 #pragma unroll
-          for (int x = 0; x < 4; ++x)
-            p[x] = make_uint4(pack_bf16(o[8 * x] * f, o[8 * x + 1] * f),
-                              pack_bf16(o[8 * x + 2] * f, o[8 * x + 3] * f),
-                              pack_bf16(o[8 * x + 4] * f, o[8 * x + 5] * f),
-                              pack_bf16(o[8 * x + 6] * f, o[8 * x + 7] * f));
-        } else if (live) {
-          float4* p = (float4*)(a.po + part * kD + 32 * c);
+          for (int y = 0; y < 4; ++y)
+            x[y] = make_uint4(pack_bf16(o[8 * y] * f, o[8 * y + 1] * f),
+                              pack_bf16(o[8 * y + 2] * f, o[8 * y + 3] * f),
+                              pack_bf16(o[8 * y + 4] * f, o[8 * y + 5] * f),
+                              pack_bf16(o[8 * y + 6] * f, o[8 * y + 7] * f));
+          store_rows(stage, lane, x, rows, (uint8_t*)a.out + 64 * c, kD * 2);
+        } else {
 #pragma unroll
-          for (int x = 0; x < 8; ++x)
-            p[x] = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+          for (int hh = 0; hh < 2; ++hh) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              x[y] = *(const uint4*)(o + 16 * hh + 4 * y);
+            store_rows(stage, lane, x, rows, (uint8_t*)a.po + 128 * c + 64 * hh, kD * 4);
+          }
         }
-        __syncwarp();   // the next TMEM load is the whole warp's
       }
       if (live) {
         if (!whole)
-          a.pml[part] = make_float2(ref, l);
+          a.pml[dst] = make_float2(ref, l);
         else if (a.lse)
           a.lse[dst] = row_lse(ref, l);
       }

@@ -322,6 +322,37 @@ def test_faulty_tables_lengths_and_parents_are_reported(grkv_lib, dtype, flags):
         assert status(parent=pr) == b.GRKV_ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("units,g,t,n,window", [(3, 4, 1500, 5000, 0), (2, 3, 3001, 3001, 500),
+                                                (5, 1, 2100, 4500, 1000), (40, 8, 33, 2900, 700),
+                                                (1, 8, 1024, 20000, 0)])
+def test_long_chunks_agree_between_the_kernels(grkv_lib, units, g, t, n, window):
+    """Runs of many slot tiles and many items to a CTA, where rings and parities wrap many
+    times: tensor cores against CUDA cores, each within the bounds of its own arithmetic."""
+    page = 32
+    cols = R.pages_of(n, page)
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=gen).bfloat16()
+    k, v, q = rnd(units * cols, page, D), rnd(units * cols, page, D), rnd(units, g, t, D)
+    table = torch.randperm(units * cols, device="cuda", generator=gen).int().view(units, cols)
+    lens = torch.tensor([n - 7 * u for u in range(units)], dtype=torch.int32, device="cuda")
+    res = []
+    for flags in (0, b.GRKV_FORCE_SIMT):
+        p = b.cache_params(units, g, units * cols, page, cols, tokens=t, window=window, flags=flags)
+        ws, out = workspace(p), torch.zeros_like(q)
+        lse = torch.zeros(units, g, t, device="cuda")
+        for _ in range(2):
+            b.grkv_attend(p, q, k, v, table, lens, out, ws, lse=lse)
+            assert b.grkv_status(ws) == b.GRKV_OK
+        res.append((out.float(), lse))
+    (o1, l1), (o2, l2) = res
+    # A = sum_j p_j |v_j| is a mean of |v|, at most max |v| < 6 (few slots seen): both kernels
+    # round the output (2^-8 |o| each), one rounds P (2^-8 A); the fp32 terms are below 2^-10 A
+    mass = v.abs().max().item()
+    assert ((o1 - o2).abs() <= 2.0 ** -7 * o2.abs() + (2.0 ** -8 + 2.0 ** -10) * mass).all()
+    assert torch.equal(l1 == -math.inf, l2 == -math.inf)      # rows in front of a shorter cache
+    assert (torch.where(l1 == l2, 0.0, l1 - l2).abs() <= 2.0 ** -9).all()
+
+
 def test_no_units(grkv_lib):
     p = b.cache_params(0, 1, 4, 16, 1)
     ws = workspace(p)
