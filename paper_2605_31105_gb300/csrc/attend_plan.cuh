@@ -80,15 +80,18 @@ __device__ __forceinline__ Item make_item(const AttendArgs& a, int u, int qb) {
   return make_item(a, u, qb, unit_len(a, u), unit_tokens(a, u));
 }
 
-// Whether every row of tokens [t0, t0 + n) of the item sees the whole slot tile.
-__device__ __forceinline__ bool tile_full(const AttendArgs& a, const Item& it, int t0, int n, int tile) {
-  const int x = tile * kSlotTile, y = x + kSlotTile;
-  const bool tree = a.parent != nullptr;
-  const int first_hi = tree ? it.base : it.base + t0 + 1;
-  if (y > first_hi) return false;
-  if (!a.W || y <= a.s) return true;
-  return x >= it.base + t0 + n - a.W;   // a node's depth is at most its index
-}
+// The slot tiles that every row of tokens [t0, t0 + n) of an item sees whole: those that end
+// by the first row's last slot and are sinks or start in the last row's window (in a tree a
+// node's depth is at most its index).
+struct FullTiles {
+  int end, sinks, window;
+  __device__ FullTiles(const AttendArgs& a, const Item& it, int t0, int n) {
+    end = max(0, a.parent ? it.base : it.base + t0 + 1) / kSlotTile;
+    sinks = a.W ? a.s / kSlotTile : 0;
+    window = a.W ? (max(0, it.base + t0 + n - a.W) + kSlotTile - 1) / kSlotTile : 0;
+  }
+  __device__ bool has(int tile) const { return tile < end && (tile < sinks || tile >= window); }
+};
 
 // Bits 0..n-1 (n clamped to 0..32).
 __device__ __forceinline__ uint32_t low_bits(int n) {

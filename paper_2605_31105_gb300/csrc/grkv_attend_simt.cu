@@ -59,6 +59,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_simt(AttendArgs a) {
 
   for (Segments sg(a, run); sg.more(); sg.next(a)) {
     const Item& it = sg.it;
+    const FullTiles full_tiles(a, it, it.tok0, it.ntok);
     auto kv = [&](int buf, int which) {
       return (T*)(sm + Lay::kOffKv + (2 * buf + which) * Lay::kSubBytes);
     };
@@ -104,7 +105,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_simt(AttendArgs a) {
     for (int n = 0; n < subs; ++n) {
       cp_async_wait_all();
       const int tile = it.tile(sg.off + (n >> 1)), x = tile * kSlotTile + (n & 1) * kSub;
-      const bool full = tile_full(a, it, it.tok0, it.ntok, tile);
+      const bool full = full_tiles.has(tile);
       uint32_t(*mask)[2] = masks + (n & 1) * kRowTile;
       if (tid < kRowTile) {
         mask[tid][0] = vis.word(x);

@@ -14,18 +14,21 @@
 // thread owns one row, one TMEM lane, and holds the tile's 128 logits in registers.
 // Warps 2-3 search the V of masked tiles (below).
 //
-// The reference of a row is its maximum so far, but it is only moved when the tile's maximum is
-// more than 8 above it in log2 units: P stays below 2^8 (bf16 keeps its relative
-// precision, the fp32 sums have room) and the output, which has to be rescaled in TMEM when
-// the reference moves, is hardly ever touched.  P is rounded to bf16 for the product
-// with V: a relative 2^-8 a term, of the size of the output's own rounding; the
-// sum of a row is taken in fp32 before it.
+// The reference of a row is the maximum of the first tile in which it sees a slot, and stays:
+// P, O and the sum are floating point, so what counts is only that nothing leaves their
+// range.  The first tile's largest P is 1, so no sum underflows; and where a later tile's sum
+// exceeds 2^60 the row takes that tile's maximum, the tile is done again and the output
+// scaled in TMEM.  A running maximum costs 64 three-operand maxima per row and tile in front of
+// the exponentials (half their time), and now and then the output's rescaling.  P is rounded to bf16 for the product with V: a
+// relative 2^-8 a term, of the size of the output's own rounding; the sum of a row is taken
+// in fp32 before it.
 //
 // Slot tiles that every row sees whole take no masks.  In the others the masks of a row are
 // four words, and V is searched for non-finite elements first: they are set to zero
 // in shared memory (0 x NaN would reach rows that do not see the slot; what was
 // never loaded is there too) and added again, at the end, to the rows that do see them.
 #include <algorithm>
+#include <type_traits>
 
 #include "attend_plan.cuh"
 #include "tmap.cuh"
@@ -41,7 +44,7 @@ constexpr int kRing = 4;   // tiles in flight: K in the even slots, V in the odd
 constexpr long long kWaitBudget = 1ll << 32;                  // cycles (~2 s)
 constexpr int kMaxEdges = 16;   // masked tiles of a segment: at most 4 at each end of the
                                 // window (256 tokens) and one at the sinks' end
-constexpr float kSlack = 8.f;   // how far a tile's maximum may exceed the reference (log2)
+constexpr float kMaxSum = 0x1p60f;   // of a row's P over one tile
 constexpr uint32_t kColO = 256; // TMEM: two S buffers, then two outputs
 
 template <int NQ>
@@ -62,7 +65,8 @@ static_assert(TcLayout<2>::kBytes <= 227 * 1024 && sizeof(PlanSmem) <= 1024, "sm
 struct TcBars {
   uint64_t ring_full[kRing], ring_empty[kRing];
   uint64_t q_full[2], q_empty[2];
-  uint64_t s_full[2], p_full[2], pv_done[2];
+  uint64_t s_full[2], p_full[2], o_done[2];
+  uint64_t v_ok[2];       // V of the slot has been passed by both searchers
   uint64_t searched[4];   // V of a masked tile has been searched (uses in turn)
   uint64_t drain;
   uint32_t tmem;
@@ -93,6 +97,7 @@ __device__ __forceinline__ void more_regs() {
 }
 
 __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort, kWaitBudget));
 }
 __device__ __forceinline__ void arrive_warp(uint64_t* bar, int lane) {
@@ -118,22 +123,37 @@ __device__ __forceinline__ float max128(const float* v) {
   return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
 
-// exp2(v sl2 - ref) of 64 logits as bf16 pairs; the sum (two partial ones) is of the
-// values before rounding.  A row that has seen nothing has v = ref = -inf and gets zeros.
-__device__ __forceinline__ uint64_t half_exp(const float* v, float sl2, float ref, uint32_t pk[2][16]) {
-  const float r = ref == -INFINITY ? 0.f : ref;
+// exp2(v sl2 - r) of 128 logits as bf16 pairs; returns the sum of the values before rounding.
+__device__ __forceinline__ float exp128(const float* v, float sl2, float r, uint32_t* pk) {
   const uint64_t s2 = pack2(sl2, sl2), m2 = pack2(-r, -r);
-  uint64_t acc[2] = {0, 0};
+  uint64_t acc[4] = {0, 0, 0, 0};
 #pragma unroll
-  for (int x = 0; x < 32; ++x) {
+  for (int x = 0; x < 64; ++x) {
     float p0, p1;
     unpack2(fma2(pack2(v[2 * x], v[2 * x + 1]), s2, m2), p0, p1);
     p0 = fast_exp2(p0);
     p1 = fast_exp2(p1);
-    acc[x & 1] = add2(acc[x & 1], pack2(p0, p1));
-    pk[x >> 4][x & 15] = pack_bf16(p0, p1);
+    acc[x & 3] = add2(acc[x & 3], pack2(p0, p1));
+    pk[x] = pack_bf16(p0, p1);
   }
-  return add2(acc[0], acc[1]);
+  float s0, s1;
+  unpack2(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), s0, s1);
+  return s0 + s1;
+}
+
+// Multiplies a row's output by f (all lanes of the warp; rare, so not in line).
+__device__ __noinline__ void scale_row(uint32_t o_addr, float f) {
+  tc_fence_after();
+  for (int c = 0; c < kD; c += 32) {
+    float o[32];
+    tmem_ld32f(o_addr + c, o);
+    tmem_wait32(o);
+#pragma unroll
+    for (int x = 0; x < 32; ++x) o[x] *= f;
+    tmem_st16(o_addr + c, (uint32_t*)o);
+    tmem_st16(o_addr + c + 16, (uint32_t*)o + 16);
+  }
+  tmem_st_wait();
 }
 
 // Stores 64 bytes of each of a warp's 32 rows, x this lane's, through shared memory so that four
@@ -190,9 +210,10 @@ __device__ __noinline__ void add_bad(const AttendArgs& a, const Item& it, int of
     tmem_ld32f(taddr + c0, o);
     tmem_wait32(o);
     int e = 0;
+    const FullTiles full(a, it, it.tok0, it.ntok);
     for (int k = 0; live && k < cnt; ++k) {
       const int tile = it.tile(off + k);
-      if (tile_full(a, it, it.tok0, it.ntok, tile)) continue;
+      if (full.has(tile)) continue;
       const uint4 words = bad[min(e, kMaxEdges - 1)];
       const uint32_t w[4] = {words.x, words.y, words.z, words.w};
       ++e;
@@ -233,14 +254,15 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
   if (tid == 0) {
     for (int i = 0; i < kRing; ++i) {
       mbar_init(&bars->ring_full[i], 1);
-      mbar_init(&bars->ring_empty[i], i & 1 ? 3 : 1);   // V: the product and both searchers
+      mbar_init(&bars->ring_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars->q_full[i], 1);
       mbar_init(&bars->q_empty[i], 1);
       mbar_init(&bars->s_full[i], 1);
       mbar_init(&bars->p_full[i], 4);
-      mbar_init(&bars->pv_done[i], 1);
+      mbar_init(&bars->o_done[i], 1);
+      mbar_init(&bars->v_ok[i], 2);
     }
     for (int i = 0; i < 4; ++i) mbar_init(&bars->searched[i], 2);
     mbar_init(&bars->drain, 1);
@@ -321,74 +343,116 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
     __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------- MMA issuer
+    // One warp feeds the tensor cores through some forty dependent instructions a product; with
+    // the masks' tests and general ring positions in it, it was what bound the kernel (3.7 K
+    // cycles for two row tiles of 2 K cycles of MMAs).  So tiles go two to a round: slots and
+    // S buffers are constants, parities one bit; a segment only shows where its count ends.
     fewer_regs<NQ>();
-    // Job n is row tile w of a slot tile; it uses S buffer n & 1.
     constexpr uint32_t id_s = idesc_bf16(kRows, kSlotTile, 0, 0);   // S = Q K^T, both K-major
     constexpr uint32_t id_o = idesc_bf16(kRows, kD, 0, 1);          // O += P V, V MN-major
     constexpr uint32_t kTileDesc = kTileBytes >> 4;
     const uint64_t q_desc = sw128_desc(smem_u32(sm + Lay::kOffQ), 16, 1024);
     const uint64_t k_desc = sw128_desc(smem_u32(sm + Lay::kOffRing), 16, 1024);
-    const uint64_t v_desc = sw128_desc(smem_u32(sm + Lay::kOffRing), kTileBytes / 2, 1024);
-    Segments qs(a, run), vs(a, run);
-    Ring kp, vp;
-    vp.add(1);
-    uint32_t qn = 0, vn = 0;   // jobs whose S / output products have been issued
-    int qk = 0, qseg = 0, vk = 0, vseg = 0;
-    uint32_t edges = 0;
-    bool ok = true;
-    auto issue_s = [&]() -> bool {   // the next slot tile's S products: NQ jobs, or one of them
-      const int w = NQ == 2 ? (int)(qn & 1) : 0, b = qseg % Lay::kQBufs;
-      if (w == 0) {
-        if (qk == 0 && !wait_warp(&bars->q_full[b], (qseg / Lay::kQBufs) & 1, abort_flag)) return false;
-        if (!wait_warp(&bars->ring_full[kp.slot], kp.phase, abort_flag)) return false;
+    const uint64_t v_desc = sw128_desc(smem_u32(sm + Lay::kOffRing + kTileBytes), kTileBytes / 2, 1024);
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return wait_warp(bar, parity, abort_flag); };
+    // segments: the S products' (ahead), and the lengths of those the output's have yet to start
+    Segments qs(a, run);
+    int q_left = 0, q_seg = -1, v_left = 0, v_seg = -1, next1 = 0, next2 = 0;
+    uint32_t qb = 0;
+    bool v_first = false;
+    auto q_begin = [&]() -> bool {   // before a slot tile's S products
+      if (q_left > 0) return true;
+      if (q_seg >= 0) qs.next(a);
+      ++q_seg;
+      q_left = qs.cnt;
+      if (next1 == 0) next1 = q_left;
+      else next2 = q_left;
+      qb = q_seg % Lay::kQBufs;
+      return wait(&bars->q_full[qb], (q_seg / Lay::kQBufs) & 1);
+    };
+    auto q_end = [&]() {
+      if (--q_left == 0) mma_commit_elect(&bars->q_empty[qb]);
+    };
+    auto v_begin = [&]() {   // before a slot tile's output products
+      v_first = v_left == 0;
+      if (v_first) {
+        ++v_seg;
+        v_left = next1;
+        next1 = next2;
+        next2 = 0;
       }
+      --v_left;
+    };
+    auto issue_s = [&](int buf, int w, int slot) {
+      mma8_ss<id_s>(tmem + buf * kSlotTile, q_desc + (qb * NQ + w) * kTileDesc,
+                    k_desc + slot * 2 * kTileDesc);
+    };
+    auto issue_o = [&](int buf, int o, int slot) {
       tc_fence_after();
-      mma8_ss<id_s>(tmem + (qn & 1) * kSlotTile, q_desc + (b * NQ + w) * kTileDesc,
-                    k_desc + kp.slot * kTileDesc);
-      mma_commit_elect(&bars->s_full[qn & 1]);
-      ++qn;
-      if (w == NQ - 1) {
-        mma_commit_elect(&bars->ring_empty[kp.slot]);
-        kp.add(2);
-        if (++qk == qs.cnt) {
-          mma_commit_elect(&bars->q_empty[b]);
-          qk = 0;
-          ++qseg;
-          qs.next(a);
+      mma8_ts<id_o, false>(tmem + kColO + o * kD, tmem + buf * kSlotTile,
+                           v_desc + slot * 2 * kTileDesc, !v_first);
+    };
+    const int tiles = run.left;
+    // Slot tile t, in slot B = t & 1; ph = (t >> 1) & 1.  With two row tiles everything but P is
+    // waited for first, so that nothing stands between a product with V and the S product
+    // over its P, and one signal says that both are done; the output's own is for a
+    // segment's end.  One row tile is bound by memory: V is given back as early as can be.
+    auto step = [&](auto b_const, int t, uint32_t ph) -> bool {
+      constexpr int B = decltype(b_const)::value;
+      v_begin();
+      if (!wait(&bars->v_ok[B], ph)) return false;
+      if (NQ == 2) {
+        const bool more = t + 1 < tiles;
+        if (more && (!q_begin() || !wait(&bars->ring_full[2 * (1 - B)], B ? ph ^ 1 : ph))) return false;
+        if (!wait(&bars->p_full[0], B)) return false;
+        issue_o(0, 0, B);
+        if (v_left == 0) mma_commit_elect(&bars->o_done[0]);
+        if (more) {
+          issue_s(0, 0, 1 - B);
+          mma_commit_elect(&bars->s_full[0]);
+        }
+        if (!wait(&bars->p_full[1], B)) return false;
+        issue_o(1, 1, B);
+        if (v_left == 0) mma_commit_elect(&bars->o_done[1]);
+        if (more) {
+          issue_s(1, NQ - 1, 1 - B);
+          mma_commit_elect(&bars->s_full[1]);
+          mma_commit_elect(&bars->ring_empty[2 * (1 - B)]);
+          q_end();
+        }
+        mma_commit_elect(&bars->ring_empty[2 * B + 1]);
+      } else {
+        if (!wait(&bars->p_full[B], ph)) return false;
+        issue_o(B, v_seg & 1, B);
+        mma_commit_elect(&bars->o_done[B]);
+        mma_commit_elect(&bars->ring_empty[2 * B + 1]);
+        if (t + 2 < tiles) {   // K of tile t + 2 may still be on its way from memory
+          if (!q_begin() || !wait(&bars->ring_full[2 * B], ph ^ 1)) return false;
+          issue_s(B, 0, B);
+          mma_commit_elect(&bars->s_full[B]);
+          mma_commit_elect(&bars->ring_empty[2 * B]);
+          q_end();
         }
       }
       return true;
     };
-    if (qs.more()) ok = issue_s();
-    if (ok && qs.more()) ok = issue_s();
-    while (ok && vs.more()) {
-      const int w = NQ == 2 ? (int)(vn & 1) : 0;
-      ok = wait_warp(&bars->p_full[vn & 1], (vn >> 1) & 1, abort_flag);
-      if (ok && w == 0) {
-        ok = wait_warp(&bars->ring_full[vp.slot], vp.phase, abort_flag);
-        const Item& it = vs.it;
-        if (ok && !tile_full(a, it, it.tok0, it.ntok, it.tile(vs.off + vk))) {
-          ok = wait_warp(&bars->searched[edges & 3], (edges >> 2) & 1, abort_flag);
-          ++edges;
-        }
-      }
+    bool ok = true;
+    for (int t = 0; t < (NQ == 2 ? 1 : 2) && t < tiles && ok; ++t) {   // the first S products
+      ok = q_begin() && wait(&bars->ring_full[2 * t], 0);
       if (!ok) break;
-      tc_fence_after();
-      const uint32_t o = tmem + kColO + (NQ == 2 ? w : vseg & 1) * kD, p = tmem + (vn & 1) * kSlotTile;
-      const uint64_t v = v_desc + vp.slot * kTileDesc;
-      mma8_ts<id_o, false>(o, p, v, vk > 0);
-      mma_commit_elect(&bars->pv_done[vn & 1]);
-      ++vn;
-      if (w == NQ - 1) {
-        mma_commit_elect(&bars->ring_empty[vp.slot]);
-        vp.add(2);
-        if (++vk == vs.cnt) {
-          vk = 0;
-          ++vseg;
-          vs.next(a);
-        }
+      issue_s(t, 0, t);
+      mma_commit_elect(&bars->s_full[t]);
+      if (NQ == 2) {
+        issue_s(1, NQ - 1, t);
+        mma_commit_elect(&bars->s_full[1]);
       }
-      if (qs.more()) ok = issue_s();   // over the S buffer that the product above reads
+      mma_commit_elect(&bars->ring_empty[2 * t]);
+      q_end();
+    }
+    for (int t = 0; ok && t < tiles; t += 2) {
+      const uint32_t ph = (t >> 1) & 1;
+      ok = step(std::integral_constant<int, 0>{}, t, ph);
+      if (ok && t + 1 < tiles) ok = step(std::integral_constant<int, 1>{}, t + 1, ph);
     }
     // every MMA issued so far completes before TMEM is released
     mma_commit_elect(&bars->drain);
@@ -398,10 +462,10 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
   } else if (warp < 4) {
     // --------------------------------------------------- search of masked tiles' V
     fewer_regs<NQ>();
-    // Two warps, two rows a lane.  They pass every V tile in turn, masked or not, and a V slot is
-    // not filled again before they have: so a parity always means the use that they are at,
-    // and they are ahead of the softmax by at most the ring's two V tiles, which four marks
-    // and four segments' words cover.
+    // Two warps, two rows a lane.  They pass every V tile in turn, masked or not, and its product
+    // waits for them: so a parity always means the use that they are at, and they are ahead
+    // of the softmax by at most the ring's two V tiles, which four marks and four segments'
+    // words cover.
     uint32_t edges = 0;
     int seg = 0;
     Ring vp;
@@ -409,12 +473,13 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
     bool ok = true;
     for (Segments sg(a, run); ok && sg.more(); sg.next(a), ++seg) {
       const Item& it = sg.it;
+      const FullTiles full(a, it, it.tok0, it.ntok);
       int e = 0;
       for (int k = 0; ok && k < sg.cnt; ++k, vp.add(2)) {
         ok = wait_warp(&bars->ring_full[vp.slot], vp.phase, abort_flag);
         if (!ok) break;
-        if (tile_full(a, it, it.tok0, it.ntok, it.tile(sg.off + k))) {
-          if (lane == 0) mbar_arrive(&bars->ring_empty[vp.slot]);
+        if (full.has(it.tile(sg.off + k))) {
+          if (lane == 0) mbar_arrive(&bars->v_ok[vp.slot >> 1]);
           continue;
         }
         uint8_t* tile = sm + Lay::kOffRing + vp.slot * kTileBytes;
@@ -427,7 +492,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
           if (bits) fence_proxy_async_smem();
         }
         arrive_warp(&bars->searched[edges & 3], lane);
-        if (lane == 0) mbar_arrive(&bars->ring_empty[vp.slot]);
+        if (lane == 0) mbar_arrive(&bars->v_ok[vp.slot >> 1]);
         ++edges;
         ++e;
       }
@@ -448,69 +513,64 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
       const bool warp_live = __any_sync(0xffffffffu, live);
       const RowVis vis = row_vis(a, it, i, live, anc, &err);
       const int t0 = it.tok0 + w * a.T, nt = min(a.T, it.tok0 + it.ntok - t0);
+      const FullTiles all_full(a, it, it.tok0, it.ntok), full(a, it, t0, nt);
       uint4* bad = bad_all + (seg & 3) * kMaxEdges;
       float ref = -INFINITY, l = 0.f;
       int e = 0;
       bool any_bad = false;
       const uint32_t ocol = kColO + (NQ == 2 ? w : seg & 1) * kD;
-      // the job before this one of the same output, for which its product is waited for
-      auto done = [&](uint32_t job) {
-        return wait_warp(&bars->pv_done[job & 1], (job >> 1) & 1, abort_flag);
+      // The products of all tiles up to job `job` are in the output.  Two row tiles: S of job n has
+      // been signalled after them, so only a segment's end has to wait, for its own signal.
+      auto done = [&](uint32_t job, bool end) {
+        if (NQ == 1) return wait_warp(&bars->o_done[job & 1], (job >> 1) & 1, abort_flag);
+        return !end || wait_warp(&bars->o_done[w], seg & 1, abort_flag);
       };
       for (int k = 0; k < sg.cnt; ++k, n += NQ) {
         const int tile = it.tile(sg.off + k);
-        const bool edge = !tile_full(a, it, it.tok0, it.ntok, tile);
+        const bool edge = !all_full.has(tile);
         const uint32_t scol = (n & 1) * kSlotTile;
         ok = wait_warp(&bars->s_full[n & 1], (n >> 1) & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
         if (warp_live) {
-          float v[128];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32f(lane_addr + scol + 32 * c, v + 32 * c);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_wait32(v + 32 * c);
-          if (!tile_full(a, it, t0, nt, tile)) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const uint32_t m = vis.word(tile * kSlotTile + 32 * c);
-              if (__all_sync(0xffffffffu, m == 0xffffffffu)) continue;
-#pragma unroll
-              for (int x = 0; x < 32; ++x)
-                if (!((m >> x) & 1)) v[32 * c + x] = -INFINITY;
-            }
-          }
-          const float top = max128(v) * a.sl2;
-          if (k == 0) ref = top;
-          const bool move = live && top > ref + kSlack;
-          if (__any_sync(0xffffffffu, move)) {
-            ok = done(n - NQ);
-            if (!ok) break;
-            tc_fence_after();
-            const float f = move ? fast_exp2(ref - top) : 1.f;
-            l *= f;
-            if (move) ref = top;
+          const bool masked = !full.has(tile);
+          uint32_t pk[64];
+          float sum = 0.f, f = 1.f;
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-              float o[32];
-              tmem_ld32f(lane_addr + ocol + 32 * c, o);
-              tmem_wait32(o);
+          for (bool again = false;; again = true) {
+            float v[128];
 #pragma unroll
-              for (int x = 0; x < 32; ++x) o[x] *= f;
-              tmem_st16(lane_addr + ocol + 32 * c, (uint32_t*)o);
-              tmem_st16(lane_addr + ocol + 32 * c + 16, (uint32_t*)o + 16);
+            for (int c = 0; c < 4; ++c) tmem_ld32f(lane_addr + scol + 32 * c, v + 32 * c);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_wait32(v + 32 * c);
+            if (masked) {
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                const uint32_t m = vis.word(tile * kSlotTile + 32 * c);
+                if (__all_sync(0xffffffffu, m == 0xffffffffu)) continue;
+#pragma unroll
+                for (int x = 0; x < 32; ++x)
+                  if (!((m >> x) & 1)) v[32 * c + x] = -INFINITY;
+              }
             }
+            // rows without a reference, or whose sum left its range, take the maximum
+            const bool need = live && (ref == -INFINITY || !(sum < kMaxSum));
+            if (__any_sync(0xffffffffu, need)) {
+              const float to = fmaxf(ref, max128(v) * a.sl2);
+              if (need && ref != -INFINITY) f = fast_exp2(ref - to);
+              if (need) ref = to;
+            }
+            sum = exp128(v, a.sl2, ref == -INFINITY ? 0.f : ref, pk);
+            if (again || !__any_sync(0xffffffffu, live && !(sum < kMaxSum))) break;
           }
-          uint32_t pk[2][16];
-          uint64_t sum = half_exp(v, a.sl2, ref, pk);
-          tmem_st16(lane_addr + scol, pk[0]);
-          tmem_st16(lane_addr + scol + 32, pk[1]);
-          sum = add2(sum, half_exp(v + 64, a.sl2, ref, pk));
-          tmem_st16(lane_addr + scol + 64, pk[0]);
-          tmem_st16(lane_addr + scol + 96, pk[1]);
-          float l0, l1;
-          unpack2(sum, l0, l1);
-          l += l0 + l1;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_st16(lane_addr + scol + 32 * c, pk + 16 * c);
+          if (k > 0 && __any_sync(0xffffffffu, f != 1.f)) {
+            ok = done(n - NQ, false);
+            if (!ok) break;
+            scale_row(lane_addr + ocol, f);
+          }
+          l = l * f + sum;
           tmem_st_wait();
         }
         tc_fence_before();
@@ -526,7 +586,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
       }
       if (!ok) break;
       // ------------------------------------------------------------ the rows' results
-      ok = done(n - NQ);
+      ok = done(n - NQ, true);
       if (!ok) break;
       tc_fence_after();
       if (!warp_live) continue;
