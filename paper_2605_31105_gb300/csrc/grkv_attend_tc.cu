@@ -123,12 +123,11 @@ __device__ __forceinline__ float max128(const float* v) {
   return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
 
-// exp2(v sl2 - r) of 128 logits as bf16 pairs; returns the sum of the values before rounding.
-__device__ __forceinline__ float exp128(const float* v, float sl2, float r, uint32_t* pk) {
+// exp2(v sl2 - r) of 32 logits as bf16 pairs; the sums are of the values before rounding.
+__device__ __forceinline__ void exp32(const float* v, float sl2, float r, uint32_t* pk, uint64_t* acc) {
   const uint64_t s2 = pack2(sl2, sl2), m2 = pack2(-r, -r);
-  uint64_t acc[4] = {0, 0, 0, 0};
 #pragma unroll
-  for (int x = 0; x < 64; ++x) {
+  for (int x = 0; x < 16; ++x) {
     float p0, p1;
     unpack2(fma2(pack2(v[2 * x], v[2 * x + 1]), s2, m2), p0, p1);
     p0 = fast_exp2(p0);
@@ -136,9 +135,6 @@ __device__ __forceinline__ float exp128(const float* v, float sl2, float r, uint
     acc[x & 3] = add2(acc[x & 3], pack2(p0, p1));
     pk[x] = pack_bf16(p0, p1);
   }
-  float s0, s1;
-  unpack2(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), s0, s1);
-  return s0 + s1;
 }
 
 // Multiplies a row's output by f (all lanes of the warp; rare, so not in line).
@@ -517,7 +513,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
       uint4* bad = bad_all + (seg & 3) * kMaxEdges;
       float ref = -INFINITY, l = 0.f;
       int e = 0;
-      bool any_bad = false;
+      bool any_bad = false, no_ref = warp_live;   // some row has no reference yet
       const uint32_t ocol = kColO + (NQ == 2 ? w : seg & 1) * kD;
       // The products of all tiles up to job `job` are in the output.  Two row tiles: S of job n has
       // been signalled after them, so only a segment's end has to wait, for its own signal.
@@ -536,32 +532,48 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
           const bool masked = !full.has(tile);
           uint32_t pk[64];
           float sum = 0.f, f = 1.f;
+          bool look = no_ref;   // rows without a reference, or whose sum left its range
 #pragma unroll 1
           for (bool again = false;; again = true) {
+            // the first chunk's exponentials run while the others are on their way
             float v[128];
+            tmem_ld32f(lane_addr + scol, v);
+            tmem_wait32(v);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32f(lane_addr + scol + 32 * c, v + 32 * c);
+            for (int c = 1; c < 4; ++c) tmem_ld32f(lane_addr + scol + 32 * c, v + 32 * c);
+            if (masked || look) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_wait32(v + 32 * c);
-            if (masked) {
+              for (int c = 1; c < 4; ++c) tmem_wait32(v + 32 * c);
+              if (masked) {
 #pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                const uint32_t m = vis.word(tile * kSlotTile + 32 * c);
-                if (__all_sync(0xffffffffu, m == 0xffffffffu)) continue;
+                for (int c = 0; c < 4; ++c) {
+                  const uint32_t m = vis.word(tile * kSlotTile + 32 * c);
+                  if (__all_sync(0xffffffffu, m == 0xffffffffu)) continue;
 #pragma unroll
-                for (int x = 0; x < 32; ++x)
-                  if (!((m >> x) & 1)) v[32 * c + x] = -INFINITY;
+                  for (int x = 0; x < 32; ++x)
+                    if (!((m >> x) & 1)) v[32 * c + x] = -INFINITY;
+                }
+              }
+              if (look) {   // take the maximum
+                const bool need = live && (ref == -INFINITY || !(sum < kMaxSum));
+                const float to = fmaxf(ref, max128(v) * a.sl2);
+                if (need && ref != -INFINITY) f = fast_exp2(ref - to);
+                if (need) ref = to;
+                no_ref = __any_sync(0xffffffffu, live && ref == -INFINITY);
               }
             }
-            // rows without a reference, or whose sum left its range, take the maximum
-            const bool need = live && (ref == -INFINITY || !(sum < kMaxSum));
-            if (__any_sync(0xffffffffu, need)) {
-              const float to = fmaxf(ref, max128(v) * a.sl2);
-              if (need && ref != -INFINITY) f = fast_exp2(ref - to);
-              if (need) ref = to;
-            }
-            sum = exp128(v, a.sl2, ref == -INFINITY ? 0.f : ref, pk);
-            if (again || !__any_sync(0xffffffffu, live && !(sum < kMaxSum))) break;
+            const float r = ref == -INFINITY ? 0.f : ref;
+            uint64_t acc[4] = {0, 0, 0, 0};
+            exp32(v, a.sl2, r, pk, acc);
+#pragma unroll
+            for (int c = 1; c < 4; ++c) tmem_wait32(v + 32 * c);
+#pragma unroll
+            for (int c = 1; c < 4; ++c) exp32(v + 32 * c, a.sl2, r, pk + 16 * c, acc);
+            float s0, s1;
+            unpack2(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), s0, s1);
+            sum = s0 + s1;
+            look = __any_sync(0xffffffffu, live && !(sum < kMaxSum));
+            if (again || !look) break;
           }
 #pragma unroll
           for (int c = 0; c < 4; ++c) tmem_st16(lane_addr + scol + 32 * c, pk + 16 * c);
