@@ -276,10 +276,10 @@ def _fault(name, t, dtype, dev, need):
     return f"{name} holds {t.numel()} elements, the call takes {need}"
 
 
-def _addresses(p, ws, ws_bytes, stream, rows, words, lse=None):
+def _addresses(p, ws, ws_bytes, stream, rows, words, lse=(), first_row=()):
     """The addresses of a cache call's tensors, the workspace's address and bytes, and the
-    stream.  Tensors are checked: row data of the call's type, 32-bit integer arrays (64 bits for
-    first_row), contiguous, on the current device like the workspace, as large as the call reads
+    stream.  Tensors are checked: row data of the call's type, 32-bit integer arrays (fp32 for lse,
+    64 bits for first_row), contiguous, on the current device like the workspace, as large as the call reads
     or writes.  Addresses given as ints pass as they are, None where the call allows it."""
     import torch
     if isinstance(ws, int):
@@ -290,34 +290,33 @@ def _addresses(p, ws, ws_bytes, stream, rows, words, lse=None):
             raise ValueError("the workspace is not on the current CUDA device")
         if not ws.is_contiguous():
             raise ValueError("the workspace is not contiguous")
+        if ws_bytes is None:
+            ws_bytes = ws.numel() * ws.element_size()
+        ws = ws.data_ptr()
     row = torch.bfloat16 if p.dtype == GRKV_BF16 else torch.float32
     out = []
-    for dtype, group in ((row, rows), (torch.int32, words)):
+    for want, group in ((row, rows), (torch.int32, words), (torch.float32, lse),
+                        (torch.int64, first_row)):
         for name, t, need in group:
             if t is not None and not isinstance(t, int):
-                want = torch.int64 if name == "first_row" else dtype
-                at = t.get_device() if dev is None else dev
-                if (t.dtype != want or t.get_device() != at or not t.is_contiguous()
-                        or t.numel() < need):
-                    raise ValueError(_fault(name, t, want, at, need))
+                at = t.get_device()
+                if (t.dtype is not want or (dev is not None and at != dev) or t.numel() < need
+                        or not t.is_contiguous()):
+                    raise ValueError(_fault(name, t, want, at if dev is None else dev, need))
                 t = t.data_ptr()
             out.append(t)
-    if lse is not None:
-        t, need = lse
-        if t is not None and not isinstance(t, int):
-            at = t.get_device() if dev is None else dev
-            if (t.dtype != torch.float32 or t.get_device() != at or not t.is_contiguous()
-                    or t.numel() < need):
-                raise ValueError(_fault("lse", t, torch.float32, at, need))
-            t = t.data_ptr()
-        out.append(t)
     if stream is None:
-        stream = torch.cuda.current_stream().cuda_stream
+        stream = _raw_stream(torch.cuda.current_device() if dev is None else dev)
     elif not isinstance(stream, int):
         stream = stream.cuda_stream
-    if ws_bytes is None:
-        ws_bytes = ws.numel() * ws.element_size()
-    return out, (ws if dev is None else ws.data_ptr()), ws_bytes, stream
+    return out, ws, ws_bytes, stream
+
+
+def _raw_stream(dev):
+    """The current stream of a device, without the Stream object (3 us a call)."""
+    import torch
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(dev) if get else torch.cuda.current_stream(dev).cuda_stream
 
 
 def grkv_cache_workspace_size(p: grkv_cache_params) -> int:
@@ -370,8 +369,8 @@ def grkv_cache_append(p, k_new, v_new, k_pages, v_pages, table, lens, ws, count=
     (kn, vn, k, v, t, le, c, f), w, nb, st = _addresses(
         p, ws, ws_bytes, stream, (("k_new", k_new, need), ("v_new", v_new, need),
                                   ("k_pages", k_pages, n), ("v_pages", v_pages, n)),
-        (("table", table, u * p.max_pages), ("lens", lens, u), ("count", count, u),
-         ("first_row", first_row, u)))
+        (("table", table, u * p.max_pages), ("lens", lens, u), ("count", count, u)),
+        first_row=(("first_row", first_row, u),))
     rc = load().grkv_cache_append(ctypes.byref(p), kn, vn, f, c, t, le, k, v, w, nb, st)
     return _check(rc, "grkv_cache_append", check)
 
@@ -398,7 +397,7 @@ def _attend(fn, p, q, k_pages, v_pages, table, lens, q_lens, parent, out, lse, w
     (q, k, v, o, *rest, ls), w, nb, st = _addresses(
         p, ws, ws_bytes, stream,
         (("q", q, rows * p.d), ("k_pages", k_pages, n), ("v_pages", v_pages, n),
-         ("out", out, rows * p.d)), words, (lse, rows))
+         ("out", out, rows * p.d)), words, (("lse", lse, rows),))
     return fn(ctypes.byref(p), q, k, v, *rest, o, ls, w, nb, st)
 
 

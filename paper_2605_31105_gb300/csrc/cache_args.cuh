@@ -7,7 +7,7 @@ namespace grkv {
 
 constexpr int kMaxCacheGroup = 64;   // query heads per KV head of the attention
 constexpr int kMaxTree = 256;        // drafted nodes per unit
-constexpr int kMaxAttendCtas = 160;  // attention CTAs that the workspace holds partials for
+constexpr int kMaxAttendSms = 160;   // SMs whose CTAs' partial results the workspace holds
 
 struct CacheShape {
   int U, g, t;
@@ -27,15 +27,15 @@ struct AttendIo {
 // Workspace regions of the cache calls (byte offsets, 256-byte aligned).
 struct CacheWs {
   size_t status;
-  size_t rec;    // AttendRec [kMaxAttendCtas]
-  size_t pml;    // float2 [2 kMaxAttendCtas][rows] reference and sum of a partial row
-  size_t po;     // float  [2 kMaxAttendCtas][rows][d] its unnormalised output
+  size_t rec;    // AttendRec [CTAs]
+  size_t pml;    // float2 [2 CTAs][rows] reference and sum of a partial row
+  size_t po;     // float  [2 CTAs][rows][d] its unnormalised output
   size_t list;   // int    [P] free pages found by a reserve
   size_t jobs;   // int4   [U] its copies: old page, new page, slots
   size_t total;
 };
 
-int attend_rows(const CacheShape& s);   // rows of a work item
+int attend_rows(const CacheShape& s, int* ctas);   // rows of a work item; the most CTAs   // rows of a work item
 cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, const CacheWs& L,
                           cudaStream_t st);
 

@@ -1,6 +1,8 @@
-// Attention over the paged cache on CUDA cores, for fp32 and (GRKV_FORCE_SIMT) bf16.
+// Attention over the paged cache on CUDA cores, for fp32 and (GRKV_FORCE_SIMT) bf16: one kernel
+// for items of up to 16 rows (decoding), one for row tiles of up to 64, and the join of
+// partial results for all kernels.
 //
-// A row tile is up to 64 rows (T tokens x g query heads).  Its keys come in
+// A row tile of k_attend_simt is up to 64 rows (T tokens x g query heads).  Its keys come in
 // sub-tiles of 64 slots, two buffers deep, copied page by page to shared memory.  A thread
 // of 256 holds 4 rows x 4 slots of the logits and then 4 rows x 8 columns of the
 // output; the softmax is online: reference (running maximum, log2 units) and sum per row,
@@ -222,6 +224,171 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_simt(AttendArgs a) {
   }
 }
 
+// Items of up to R rows, R = 4, 8 or 16: bound by the read of the cache, which goes straight to
+// registers.  Each of 8 warps takes 16 slots of a slot tile, 32 / R at a time, a lane
+// four dimensions of all of them: R x 32 / R = 32 logits, whose sums over the lanes a
+// transpose-reduction of 31 shuffles leaves one to a lane, so that a step has one
+// exponential a lane.  The warps' references, sums and outputs are joined at a segment's end.
+// Up to 8 rows fit two CTAs on an SM, which keep 16 warps x 8 KB (fp32) in flight.  (64-row tiles, of which one query
+// of 4 heads fills a sixteenth: 32 units of up to 12005 slots, window 4096, 134 us.)
+constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
+
+template <int R>
+struct FewSmem {
+  PlanSmem plan;
+  uint32_t anc[kFewWarps][R][kMaxTree / 32];
+  float ml[kFewWarps][R][2];
+  float4 o[kFewWarps][R][32];
+};
+static_assert(sizeof(FewSmem<8>) <= 113 * 1024, "two CTAs per SM");
+
+template <typename T, int R>
+__global__ void __launch_bounds__(kFewThreads, R <= 8 ? 2 : 1) k_attend_few(AttendArgs a) {
+  constexpr int S = 32 / R;   // slots of a step
+  extern __shared__ __align__(16) uint8_t sm_few[];
+  FewSmem<R>& sm = *(FewSmem<R>*)sm_few;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int my_row = lane / S, my_slot = lane % S;   // of the logit that this lane ends with
+  plan_run(a, &sm.plan, kFewThreads);
+  const Run run = sm.plan.run;
+  int err = 0;
+
+  for (Segments sg(a, run); sg.more(); sg.next(a)) {
+    const Item& it = sg.it;
+    const FullTiles full(a, it, it.tok0, it.ntok);
+    float4 q[R], o[R];
+    int h, i;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      o[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+      q[r] = o[r];
+      if (row_of(a, it, 0, r, &h, &i))
+        q[r] = ld4((const T*)a.q + (((size_t)it.u * a.g + h) * a.t + i) * kD + lane * 4);
+    }
+    const bool live = row_of(a, it, 0, my_row, &h, &i);
+    // one lane of a row works out what the row sees, in the warp's own words
+    uint32_t* anc = sm.anc[warp][my_row];
+    RowVis vis{0, 0, 0, it.base, nullptr};
+    if (my_slot == 0) vis = row_vis(a, it, i, live, anc, &err);
+    __syncwarp();
+    vis.end_s = __shfl_sync(0xffffffffu, vis.end_s, my_row * S);
+    vis.lo = __shfl_sync(0xffffffffu, vis.lo, my_row * S);
+    vis.hi = __shfl_sync(0xffffffffu, vis.hi, my_row * S);
+    vis.anc = a.parent ? anc : nullptr;
+    float m = -INFINITY, l = 0.f;   // of row my_row: the same in its S lanes
+    const size_t row_off = lane * 4;
+    for (int k = 0; k < sg.cnt; ++k) {
+      const int tile = it.tile(sg.off + k), x0 = tile * kSlotTile + warp * 16;
+      const bool whole = full.has(tile);
+      const int c = x0 >> a.shift;
+      if (!it.wanted(x0, x0 + 16)) continue;
+      const size_t base = (((size_t)page_of(a, it.u, c, &err) << a.shift) + (x0 & ((1 << a.shift) - 1))) * kD;
+      const uint32_t seen = whole ? 0xffffffffu : vis.word(x0 & ~31) >> (x0 & 31);
+#pragma unroll 1
+      for (int s0 = 0; s0 < 16; s0 += S) {
+        const bool see = (seen >> (s0 + my_slot)) & 1;
+        if (!__any_sync(0xffffffffu, see)) continue;
+        float4 kk[S], vv[S];
+#pragma unroll
+        for (int s = 0; s < S; ++s) kk[s] = ld4((const T*)a.k + base + (size_t)(s0 + s) * kD + row_off);
+#pragma unroll
+        for (int s = 0; s < S; ++s) vv[s] = ld4((const T*)a.v + base + (size_t)(s0 + s) * kD + row_off);
+        float x[32];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int s = 0; s < S; ++s)
+            x[r * S + s] = fmaf(q[r].x, kk[s].x, fmaf(q[r].y, kk[s].y, fmaf(q[r].z, kk[s].z, q[r].w * kk[s].w)));
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) {   // lane e ends with the sum of x[e]
+          const bool up = (lane & d) != 0;
+#pragma unroll
+          for (int e = 0; e < d; ++e) {
+            const float send = up ? x[e] : x[e + d];
+            x[e] = (up ? x[e + d] : x[e]) + __shfl_xor_sync(0xffffffffu, send, d);
+          }
+        }
+        const float logit = see ? x[0] * a.sl2 : -INFINITY;
+        float top = logit;
+#pragma unroll
+        for (int d = S / 2; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const float M = fmaxf(m, top), ref = M == -INFINITY ? 0.f : M;
+        const float keep = fast_exp2(m - ref), p = see ? fast_exp2(logit - ref) : 0.f;
+        m = M;
+        l = l * keep + p;
+        const bool scale = __any_sync(0xffffffffu, keep != 1.f);
+        const uint32_t skip = whole ? 0u : __ballot_sync(0xffffffffu, !see);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (scale) {
+            const float f = __shfl_sync(0xffffffffu, keep, r * S);
+            o[r].x *= f;
+            o[r].y *= f;
+            o[r].z *= f;
+            o[r].w *= f;
+          }
+#pragma unroll
+          for (int s = 0; s < S; ++s) {
+            const float w = __shfl_sync(0xffffffffu, p, r * S + s);
+            if ((skip >> (r * S + s)) & 1) continue;   // whatever lies there stays out
+            o[r].x = fmaf(w, vv[s].x, o[r].x);
+            o[r].y = fmaf(w, vv[s].y, o[r].y);
+            o[r].z = fmaf(w, vv[s].z, o[r].z);
+            o[r].w = fmaf(w, vv[s].w, o[r].w);
+          }
+        }
+      }
+    }
+    // a row's sum is spread over its S lanes
+#pragma unroll
+    for (int d = S / 2; d >= 1; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+    if (my_slot == 0) {
+      sm.ml[warp][my_row][0] = m;
+      sm.ml[warp][my_row][1] = l;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) sm.o[warp][r][lane] = o[r];
+    __syncthreads();
+    const bool all = sg.whole();
+    for (int r = warp; r < R; r += kFewWarps) {
+      if (!row_of(a, it, 0, r, &h, &i)) continue;
+      float M = -INFINITY, L = 0.f;
+#pragma unroll
+      for (int w = 0; w < kFewWarps; ++w) M = fmaxf(M, sm.ml[w][r][0]);
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kFewWarps; ++w) {
+        const float f = weight_of(sm.ml[w][r][0], M);
+        const float4 y = sm.o[w][r][lane];
+        L += f * sm.ml[w][r][1];
+        sum.x = fmaf(f, y.x, sum.x);
+        sum.y = fmaf(f, y.y, sum.y);
+        sum.z = fmaf(f, y.z, sum.z);
+        sum.w = fmaf(f, y.w, sum.w);
+      }
+      if (all) {
+        const size_t dst = ((size_t)it.u * a.g + h) * a.t + i;
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        store_row4((T*)a.out + dst * kD + lane * 4,
+                   make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+        if (a.lse && lane == 0) a.lse[dst] = row_lse(M, L);
+      } else {
+        const size_t part = (size_t)sg.slot(blockIdx.x) * a.rows + r;
+        store_row4(a.po + part * kD + lane * 4, sum);
+        if (lane == 0) a.pml[part] = make_float2(M, L);
+      }
+    }
+    __syncthreads();   // the next segment writes the same shared memory
+  }
+  if (err) sm.plan.err = err;
+  __syncthreads();
+  if (tid == 0) {
+    AttendRec rec = sm.plan.rec;
+    rec.err = sm.plan.err;
+    a.rec[blockIdx.x] = rec;
+  }
+}
+
 // Adds up the partial results of the split items, and writes the call's status.  Block
 // (c, y) takes rows of the item that starts in CTA c: a warp each, or, where items have few
 // rows and so may have many parts, one row whose parts go round the eight warps.
@@ -293,14 +460,21 @@ cudaError_t launch_join(const AttendArgs& a, int G, cudaStream_t st) {
   return launch_kernel(true, 1, k_attend_join<T, false>, dim3(G, (a.rows + 7) / 8), 256, 0, st, a, G);
 }
 
-template <typename T>
-cudaError_t launch_simt(const AttendArgs& a, int G, cudaStream_t st) {
-  auto kern = k_attend_simt<T>;
-  const uint32_t smem = SimtLayout<T>::kBytes;
+template <typename... Args>
+cudaError_t launch_main(void (*kern)(Args...), int G, int threads, uint32_t smem, cudaStream_t st,
+                        const Args&... args) {
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   count_launches(1);
-  return launch_kernel(false, 1, kern, dim3(G), kThreads, smem, st, a);
+  return launch_kernel(false, 1, kern, dim3(G), threads, smem, st, args...);
+}
+
+template <typename T>
+cudaError_t launch_simt(const AttendArgs& a, int G, cudaStream_t st) {
+  if (a.rows <= 4) return launch_main(k_attend_few<T, 4>, G, kFewThreads, sizeof(FewSmem<4>), st, a);
+  if (a.rows <= 8) return launch_main(k_attend_few<T, 8>, G, kFewThreads, sizeof(FewSmem<8>), st, a);
+  if (a.rows <= 16) return launch_main(k_attend_few<T, 16>, G, kFewThreads, sizeof(FewSmem<16>), st, a);
+  return launch_main(k_attend_simt<T>, G, kThreads, SimtLayout<T>::kBytes, st, a);
 }
 
 }  // namespace
@@ -314,9 +488,15 @@ static void plan_rows(const CacheShape& s, int* T, int* nq) {
   *nq = tc && s.t > most ? 2 : 1;
 }
 
-int attend_rows(const CacheShape& s) {
+// k_attend_few with up to 8 rows: two CTAs per SM.
+static int ctas_per_sm(const CacheShape& s, int rows) {
+  return (s.dtype == GRKV_F32 || s.simt) && rows <= 8 ? 2 : 1;
+}
+
+int attend_rows(const CacheShape& s, int* ctas) {
   int T, nq;
   plan_rows(s, &T, &nq);
+  *ctas = kMaxAttendSms * ctas_per_sm(s, T * nq * s.g);
   return T * nq * s.g;
 }
 
@@ -348,8 +528,9 @@ cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, con
   plan_rows(s, &a.T, &a.nq);
   a.QB = (s.t + a.nq * a.T - 1) / (a.nq * a.T);
   a.rows = a.nq * a.T * s.g;
-  const int G = sm_count();
-  if (G <= 0 || G > kMaxAttendCtas) return cudaErrorInvalidDevice;
+  const int sms = sm_count();
+  if (sms <= 0 || sms > kMaxAttendSms) return cudaErrorInvalidDevice;
+  const int G = sms * ctas_per_sm(s, a.rows);
   const bool f32 = s.dtype == GRKV_F32;
   cudaError_t e = f32      ? launch_simt<float>(a, G, st)
                   : s.simt ? launch_simt<__nv_bfloat16>(a, G, st)

@@ -76,11 +76,12 @@ CacheWs plan_cache_ws(const CacheShape& s) {
     off = align256(off + bytes);
     return at;
   };
-  const size_t rows = (size_t)attend_rows(s);
+  int ctas;
+  const size_t rows = (size_t)attend_rows(s, &ctas);
   L.status = take(256);
-  L.rec = take((size_t)kMaxAttendCtas * 16);
-  L.pml = take(2 * (size_t)kMaxAttendCtas * rows * sizeof(float2));
-  L.po = take(2 * (size_t)kMaxAttendCtas * rows * kD * sizeof(float));
+  L.rec = take((size_t)ctas * 16);
+  L.pml = take(2 * (size_t)ctas * rows * sizeof(float2));
+  L.po = take(2 * (size_t)ctas * rows * kD * sizeof(float));
   // a reserve and an attention call do not need their parts at the same time
   const size_t attend = off;
   off = L.rec;
