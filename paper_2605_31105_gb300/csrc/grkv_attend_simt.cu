@@ -3,9 +3,11 @@
 // partial results for all kernels.
 //
 // A row tile of k_attend_simt is up to 64 rows (T tokens x g query heads).  Its keys come in
-// sub-tiles of 64 slots, two buffers deep, copied page by page to shared memory.  A thread
-// of 256 holds 4 rows x 4 slots of the logits and then 4 rows x 8 columns of the
-// output; the softmax is online: reference (running maximum, log2 units) and sum per row,
+// sub-tiles of 64 slots, copied page by page to shared memory: K while the last sub-tile's
+// values are multiplied, V while the logits are, so that one buffer each does and two CTAs
+// fit an SM (one CTA with two buffers each kept the FMA pipe 48% busy with two warps a
+// scheduler: 6 units of 1203 slots, 301 queries of 7 heads, 228 us against 217).  A thread of 256 holds 4 rows x 4 slots of the logits and then 4 rows x 8
+// columns of the output; the softmax is online: reference (running maximum, log2 units) and sum per row,
 // the output rescaled when the reference grows.  Slots that a row does not see carry p = -1
 // and are left out of its sums by comparison, so whatever lies there (a NaN, an infinity)
 // does not reach the row.
@@ -22,21 +24,21 @@ constexpr int kRowTile = 64;   // rows of a tile
 constexpr int kSub = 64;       // slots of a sub-tile
 constexpr int kThreads = 256;
 constexpr int kQStride = kD + 4;        // floats
-constexpr int kPStride = kSub + 4;
+constexpr int kPStride = kSub / 2 + 4;   // P goes to shared memory in two halves
 
 template <typename T>
 struct SimtLayout {
   static constexpr int kStride = kD + 16 / (int)sizeof(T);      // elements of a K or V row
   static constexpr uint32_t kSubBytes = kSub * kStride * sizeof(T);
   static constexpr uint32_t kOffQ = 0;
-  static constexpr uint32_t kOffKv = kOffQ + kRowTile * kQStride * 4;   // [2][K, V]
-  static constexpr uint32_t kOffP = kOffKv + 4 * kSubBytes;
+  static constexpr uint32_t kOffKv = kOffQ + kRowTile * kQStride * 4;   // K, V
+  static constexpr uint32_t kOffP = kOffKv + 2 * kSubBytes;
   static constexpr uint32_t kOffAnc = kOffP + kRowTile * kPStride * 4;
   static constexpr uint32_t kOffMask = kOffAnc + kRowTile * (kMaxTree / 8);
-  static constexpr uint32_t kOffPlan = kOffMask + 2 * kRowTile * 8;
+  static constexpr uint32_t kOffPlan = kOffMask + kRowTile * 8;
   static constexpr uint32_t kBytes = kOffPlan + ((sizeof(PlanSmem) + 15) & ~15);
 };
-static_assert(SimtLayout<float>::kBytes <= 227 * 1024, "smem");
+static_assert(SimtLayout<float>::kBytes <= 113 * 1024, "two CTAs per SM");
 
 __device__ __forceinline__ float4 ld4(const float* p) { return *(const float4*)p; }
 __device__ __forceinline__ float4 ld4(const __nv_bfloat16* p) {
@@ -46,13 +48,13 @@ __device__ __forceinline__ float4 ld4(const __nv_bfloat16* p) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 1) k_attend_simt(AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) k_attend_simt(AttendArgs a) {
   using Lay = SimtLayout<T>;
   extern __shared__ __align__(16) uint8_t sm[];
   float* qs = (float*)(sm + Lay::kOffQ);
   float* ps = (float*)(sm + Lay::kOffP);
   uint32_t(*anc)[kMaxTree / 32] = (uint32_t(*)[kMaxTree / 32])(sm + Lay::kOffAnc);
-  uint32_t(*masks)[2] = (uint32_t(*)[2])(sm + Lay::kOffMask);   // [2][rows]
+  uint32_t(*mask)[2] = (uint32_t(*)[2])(sm + Lay::kOffMask);
   PlanSmem* plan = (PlanSmem*)(sm + Lay::kOffPlan);
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   plan_run(a, plan, kThreads);
@@ -62,11 +64,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_simt(AttendArgs a) {
   for (Segments sg(a, run); sg.more(); sg.next(a)) {
     const Item& it = sg.it;
     const FullTiles full_tiles(a, it, it.tok0, it.ntok);
-    auto kv = [&](int buf, int which) {
-      return (T*)(sm + Lay::kOffKv + (2 * buf + which) * Lay::kSubBytes);
-    };
-    // sub-tiles of the segment: two per slot tile
-    auto load = [&](int n) {
+    T* const kv[2] = {(T*)(sm + Lay::kOffKv), (T*)(sm + Lay::kOffKv + Lay::kSubBytes)};
+    // K (0) or V (1) of a sub-tile of the segment: two per slot tile
+    auto load = [&](int n, int which) {
       const int x = it.tile(sg.off + (n >> 1)) * kSlotTile + (n & 1) * kSub;
       constexpr int kChunks = kD * (int)sizeof(T) / 16;
       for (int e = tid; e < kSub * kChunks; e += kThreads) {
@@ -75,12 +75,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_simt(AttendArgs a) {
         const size_t at =
             (((size_t)page_of(a, it.u, c, &err) << a.shift) + (slot & ((1 << a.shift) - 1))) * kD;
         const int off = ch * (16 / (int)sizeof(T));
-        cp_async16(smem_u32(kv(n & 1, 0) + row * Lay::kStride + off), (const T*)a.k + at + off);
-        cp_async16(smem_u32(kv(n & 1, 1) + row * Lay::kStride + off), (const T*)a.v + at + off);
+        cp_async16(smem_u32(kv[which] + row * Lay::kStride + off),
+                   (const T*)(which ? a.v : a.k) + at + off);
       }
     };
     const int subs = 2 * sg.cnt;
-    load(0);
+    load(0, 0);
     // the item's queries; rows that do not exist are zero
     for (int e = tid; e < kRowTile * (kD / 4); e += kThreads) {
       const int r = e / (kD / 4), d = e % (kD / 4) * 4;
@@ -104,18 +104,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_simt(AttendArgs a) {
 #pragma unroll
       for (int c = 0; c < 8; ++c) acc[r][c] = 0.f;
     }
-    for (int n = 0; n < subs; ++n) {
+    auto ready = [&](int n) {   // before the barrier in front of sub-tile n's logits
       cp_async_wait_all();
-      const int tile = it.tile(sg.off + (n >> 1)), x = tile * kSlotTile + (n & 1) * kSub;
-      const bool full = full_tiles.has(tile);
-      uint32_t(*mask)[2] = masks + (n & 1) * kRowTile;
       if (tid < kRowTile) {
+        const int x = it.tile(sg.off + (n >> 1)) * kSlotTile + (n & 1) * kSub;
         mask[tid][0] = vis.word(x);
         mask[tid][1] = vis.word(x + 32);
       }
-      __syncthreads();   // the sub-tile and the masks are there; the last one has been read
-      if (n + 1 < subs) load(n + 1);
-      const T *ks = kv(n & 1, 0), *vs = kv(n & 1, 1);
+    };
+    ready(0);
+    for (int n = 0; n < subs; ++n) {
+      __syncthreads();   // K and the masks are there; the last V has been read
+      load(n, 1);
+      const bool full = full_tiles.has(it.tile(sg.off + (n >> 1)));
+      const T *ks = kv[0], *vs = kv[1];
       float sc[4][4] = {};
       for (int d = 0; d < kD; d += 4) {
         float4 q4[4], k4[4];
@@ -159,34 +161,49 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_simt(AttendArgs a) {
           const bool see = (w >> ((tx + 16 * j) & 31)) & 1;
           const float p = fast_exp2(sc[r][j] - ref);
           if (see) l[r] += p;
-          ps[row * kPStride + tx + 16 * j] = see ? p : -1.f;
+          sc[r][j] = see ? p : -1.f;
         }
       }
-      __syncwarp();   // a warp writes and reads its own 8 rows
-      for (int j = 0; j < kSub; j += 4) {
-        float4 p4[4];
+      cp_async_wait_all();
+      __syncthreads();   // V is there, K has been read
+      if (n + 1 < subs) load(n + 1, 0);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) p4[r] = ld4(ps + (ty * 4 + r) * kPStride + j);
+      for (int half = 0; half < 2; ++half) {
+        __syncwarp();   // a warp writes and reads its own 8 rows
 #pragma unroll
-        for (int jj = 0; jj < 4; ++jj) {
-          const float4 va = ld4(vs + (j + jj) * Lay::kStride + tx * 4);
-          const float4 vb = ld4(vs + (j + jj) * Lay::kStride + 64 + tx * 4);
+        for (int r = 0; r < 4; ++r) {
+          ps[(ty * 4 + r) * kPStride + tx] = sc[r][2 * half];
+          ps[(ty * 4 + r) * kPStride + tx + 16] = sc[r][2 * half + 1];
+        }
+        __syncwarp();
+        const T* vh = vs + half * (kSub / 2) * Lay::kStride;
+#pragma unroll 2
+        for (int j = 0; j < kSub / 2; j += 4) {
+          float4 p4[4];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float p = jj == 0 ? p4[r].x : jj == 1 ? p4[r].y : jj == 2 ? p4[r].z : p4[r].w;
-            if (full || !(p < 0.f)) {
-              acc[r][0] = fmaf(p, va.x, acc[r][0]);
-              acc[r][1] = fmaf(p, va.y, acc[r][1]);
-              acc[r][2] = fmaf(p, va.z, acc[r][2]);
-              acc[r][3] = fmaf(p, va.w, acc[r][3]);
-              acc[r][4] = fmaf(p, vb.x, acc[r][4]);
-              acc[r][5] = fmaf(p, vb.y, acc[r][5]);
-              acc[r][6] = fmaf(p, vb.z, acc[r][6]);
-              acc[r][7] = fmaf(p, vb.w, acc[r][7]);
+          for (int r = 0; r < 4; ++r) p4[r] = ld4(ps + (ty * 4 + r) * kPStride + j);
+#pragma unroll
+          for (int jj = 0; jj < 4; ++jj) {
+            const float4 va = ld4(vh + (j + jj) * Lay::kStride + tx * 4);
+            const float4 vb = ld4(vh + (j + jj) * Lay::kStride + 64 + tx * 4);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float p = jj == 0 ? p4[r].x : jj == 1 ? p4[r].y : jj == 2 ? p4[r].z : p4[r].w;
+              if (full || !(p < 0.f)) {
+                acc[r][0] = fmaf(p, va.x, acc[r][0]);
+                acc[r][1] = fmaf(p, va.y, acc[r][1]);
+                acc[r][2] = fmaf(p, va.z, acc[r][2]);
+                acc[r][3] = fmaf(p, va.w, acc[r][3]);
+                acc[r][4] = fmaf(p, vb.x, acc[r][4]);
+                acc[r][5] = fmaf(p, vb.y, acc[r][5]);
+                acc[r][6] = fmaf(p, vb.z, acc[r][6]);
+                acc[r][7] = fmaf(p, vb.w, acc[r][7]);
+              }
             }
           }
         }
       }
+      if (n + 1 < subs) ready(n + 1);
     }
     const bool whole = sg.whole();
     const size_t part = (size_t)sg.slot(blockIdx.x) * a.rows;
@@ -488,9 +505,9 @@ static void plan_rows(const CacheShape& s, int* T, int* nq) {
   *nq = tc && s.t > most ? 2 : 1;
 }
 
-// k_attend_few with up to 8 rows: two CTAs per SM.
+// The CUDA-core kernels fit an SM twice, but for k_attend_few with 16 rows.
 static int ctas_per_sm(const CacheShape& s, int rows) {
-  return (s.dtype == GRKV_F32 || s.simt) && rows <= 8 ? 2 : 1;
+  return (s.dtype == GRKV_F32 || s.simt) && (rows <= 8 || rows > 16) ? 2 : 1;
 }
 
 int attend_rows(const CacheShape& s, int* ctas) {
