@@ -32,6 +32,8 @@ struct AttendArgs {
   int nq;      // row tiles of an item
   int QB;      // items of a unit
   int rows;    // rows of an item, nq * T * g
+  int extra;   // tiles' worth of work of an item besides its tiles
+  int wide;    // there may be 2^30 of them or more
   float sl2;   // scale * log2(e)
   AttendRec* rec;
   float2* pml;
@@ -120,13 +122,15 @@ struct RowVis {
   }
 };
 
-// The slots that token i of the item's unit sees (live: the row exists).  In a tree the row's
-// ancestor bits go to anc, 8 words that only this thread writes; a bad parent sets
-// *err and counts as none.
+// The slots that token i of the item's unit sees (live: the row exists), for a segment whose
+// slots end before `end`.  In a tree the row's ancestor bits go to anc, 8 words that only
+// this thread writes; a bad parent sets *err and counts as none.  The walk up the tree, a
+// chain of dependent loads, is made only where a drafted slot or a window needs it.
 __device__ __forceinline__ RowVis row_vis(const AttendArgs& a, const Item& it, int i, bool live,
-                                          uint32_t* anc, int* err) {
+                                          int end, uint32_t* anc, int* err) {
   RowVis r{0, 0, 0, it.base, nullptr};
-  if (a.parent) {
+  const bool walk = a.parent && (a.W || end > it.base);
+  if (walk) {
 #pragma unroll
     for (int w = 0; w < kMaxTree / 32; ++w) anc[w] = 0;
     r.anc = anc;
@@ -134,117 +138,152 @@ __device__ __forceinline__ RowVis row_vis(const AttendArgs& a, const Item& it, i
   if (!live) return r;
   int p = it.base + i;
   r.hi = p + 1;
-  if (a.parent) {
+  if (walk) {
     const int32_t* par = a.parent + (size_t)it.u * a.t;
-    int depth = 0;
+    int depth = 0, w = i >> 5;
+    uint32_t bits = 1u << (i & 31);
     for (int x = i;;) {
-      const int y = par[x];
+      const int y = __ldg(par + x);
       if (y < -1 || y >= x) *err = GRKV_ERR_INVALID_ARG;
       if (y < 0 || y >= x) break;
       x = y;
       ++depth;
+      if (x >> 5 != w) {   // words are left downwards
+        anc[w] = bits;
+        w = x >> 5;
+        bits = 0;
+      }
+      bits |= 1u << (x & 31);
     }
+    anc[w] = bits;
     p = it.base + depth;
-    for (int x = i, k = 0; k <= depth; ++k) {   // the ancestor k steps up is at position p - k
-      if (!a.W || k < a.W || p - k < a.s) anc[x >> 5] |= 1u << (x & 31);
-      x = par[x];
-    }
-    r.hi = it.base;
+    if (a.W && depth >= a.W)   // the ancestor k steps up, at position p - k, may be out of the window
+      for (int x = i, k = 0; k <= depth; ++k) {
+        if (k >= a.W && p - k >= a.s) anc[x >> 5] &= ~(1u << (x & 31));
+        x = __ldg(par + x);
+      }
   }
+  if (a.parent) r.hi = it.base;
   r.hi = max(r.hi, 0);
   r.lo = a.W ? min(max(0, p - a.W + 1), r.hi) : 0;
   r.end_s = min(a.s, r.lo);
   return r;
 }
 
-// The CTA's run of tiles.
-struct Run {
-  long long total;   // tiles of all items
-  int G;             // CTAs that have any
-  int u, qb, off;    // first item and its first tile here
-  int left;          // tiles of the run
-  __device__ long long start(int c) const { return total * c / G; }
-  __device__ int owner(long long t) const { return (int)(((t + 1) * G + total - 1) / total) - 1; }
+// Where the CTAs' runs start.  Positions count an item's tiles and, in front of them, a.extra for
+// the work that it brings by itself (its queries, its results); CTA c starts at
+// q c + r c / G, with total = q G + r.
+template <typename I>   // of positions: 32 bits where they all fit
+struct Split {
+  I total, q;
+  int r, G;
+  __device__ Split(I all, int ctas) : total(all), G(ctas) {
+    q = all / ctas;
+    r = (int)(all - q * ctas);
+  }
+  __device__ I start(int c) const { return q * c + (uint32_t)(r * c) / (uint32_t)G; }
+  __device__ int owner(I t) const {
+    int c = min(G - 1, (int)((float)t * ((float)G / (float)total)));
+    while (c > 0 && start(c) > t) --c;
+    while (c + 1 < G && start(c + 1) <= t) ++c;
+    return c;
+  }
 };
 
-// The fewest tiles worth a CTA of their own: a tile takes about 1 us and joining a
-// partial result about as long.
-constexpr int kMinRun = 1;
+// A CTA's run: `left` tiles from tile `off` of item (u, qb) on.
+struct Run {
+  int u, qb, off, left;
+};
 
 struct PlanSmem {
   Run run;
   AttendRec rec;
-  long long warp_sum[32];
+  long long warp_sum[32], first, last;   // tiles in front of the run, and up to its end
+  int warp_items[32];
   int err;
 };
 
-// Every thread of the block takes part (n threads, a multiple of 32).  Afterwards ps->run
-// holds the CTA's run (left == 0: none), ps->rec the split item that starts in it, and
-// ps->err any fault of the lengths.
-__device__ __forceinline__ void plan_run(const AttendArgs& a, PlanSmem* ps, int n) {
+template <typename I>
+__device__ __forceinline__ Run plan_run_of(const AttendArgs& a, PlanSmem* ps, int n) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int items = a.U * a.QB;
   const int per = (items + n - 1) / n, i0 = min(items, tid * per), i1 = min(items, i0 + per);
   if (tid == 0) {
     ps->err = 0;
-    ps->run = Run{0, 1, 0, 0, 0, 0};
+    ps->run = Run{0, 0, 0, 0};
     ps->rec = AttendRec{-1, 0, 0, 0};
+    ps->first = ps->last = 0;
   }
   __syncthreads();
   const int first_u = i0 / a.QB, first_qb = i0 - first_u * a.QB;
-  long long mine = 0;
+  I mine = 0;
+  int live = 0;   // items with rows
   for (int i = i0, u = first_u, qb = first_qb, L = 0, T = 0; i < i1; ++i) {
     if (i == i0 || qb == 0) {
       L = unit_len(a, u);
       T = unit_tokens(a, u);
       if (L != __ldg(a.len + u) || (a.qlen && T != __ldg(a.qlen + u))) ps->err = GRKV_ERR_INVALID_ARG;
     }
-    mine += make_item(a, u, qb, L, T).nt;
+    const int nt = make_item(a, u, qb, L, T).nt;
+    mine += nt;
+    live += nt > 0;
     if (++qb == a.QB) {
       qb = 0;
       ++u;
     }
   }
-  long long scan = mine;
+  I scan = mine;
+  int scan_live = live;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const long long x = __shfl_up_sync(0xffffffffu, scan, d);
-    if (lane >= d) scan += x;
+    const I x = __shfl_up_sync(0xffffffffu, scan, d);
+    const int y = __shfl_up_sync(0xffffffffu, scan_live, d);
+    if (lane >= d) {
+      scan += x;
+      scan_live += y;
+    }
   }
-  if (lane == 31) ps->warp_sum[warp] = scan;
+  if (lane == 31) {
+    ps->warp_sum[warp] = scan;
+    ps->warp_items[warp] = scan_live;
+  }
   __syncthreads();
-  long long before = 0, total = 0;
+  I tiles = 0, all = 0;   // tiles in front of this thread's items, and of all
+  int front = 0, all_live = 0;
   for (int w = 0; w < n / 32; ++w) {
-    const long long x = ps->warp_sum[w];
-    if (w < warp) before += x;
-    total += x;
+    if (w < warp) {
+      tiles += (I)ps->warp_sum[w];
+      front += ps->warp_items[w];
+    }
+    all += (I)ps->warp_sum[w];
+    all_live += ps->warp_items[w];
   }
-  before += scan - mine;
-  if (total > 0) {
-    Run r;
-    r.total = total;
-    r.G = (int)min((long long)gridDim.x, max(1ll, total / kMinRun));
+  tiles += scan - mine;
+  front += scan_live - live;
+  if (all > 0) {
+    const Split<I> sp(all + (I)a.extra * all_live, (int)min((I)gridDim.x, all));
     const int c = blockIdx.x;
-    const long long t0 = r.start(c);
-    const long long t1 = r.start(c + 1);
-    // the first and the last tile are each in the items of one thread
-    const bool first = before <= t0 && t0 < before + mine;
-    const bool last = before < t1 && t1 <= before + mine;
-    if (c < r.G && (first || last)) {
-      long long at = before;
+    I at = tiles + (I)a.extra * front;
+    const I end = at + mine + (I)a.extra * live;
+    const I t0 = sp.start(c), t1 = sp.start(c + 1);
+    // each end of the run is in the items of one thread
+    const bool first = at <= t0 && t0 < end, last = at < t1 && t1 <= end;
+    if (c < sp.G && (first || last)) {
       for (int i = i0, u = first_u, qb = first_qb; i < i1; ++i) {
         const int nt = make_item(a, u, qb).nt;
-        if (at <= t0 && t0 < at + nt) {
-          r.u = u;
-          r.qb = qb;
-          r.off = (int)(t0 - at);
-          r.left = (int)(t1 - t0);
-          ps->run = r;
+        if (nt > 0) {
+          const I from = at + a.extra, to = from + nt;   // its tiles
+          if (at <= t0 && t0 < to) {
+            const int off = (int)max((I)0, t0 - from);
+            ps->run = Run{u, qb, off, 0};
+            ps->first = tiles + off;
+          }
+          if (at < t1 && t1 <= to) ps->last = tiles + max((I)0, t1 - from);
+          if (t0 <= from && from < t1 && t1 < to) ps->rec = AttendRec{u, qb, sp.owner(to - 1), 0};
+          at = to;
+          tiles += nt;
+          if (at >= t1) break;
         }
-        if (t0 <= at && at < t1 && t1 < at + nt)
-          ps->rec = AttendRec{u, qb, r.owner(at + nt - 1), 0};
-        at += nt;
-        if (at >= t1) break;
         if (++qb == a.QB) {
           qb = 0;
           ++u;
@@ -253,6 +292,16 @@ __device__ __forceinline__ void plan_run(const AttendArgs& a, PlanSmem* ps, int 
     }
   }
   __syncthreads();
+  Run run = ps->run;
+  run.left = (int)(ps->last - ps->first);
+  return run;
+}
+
+// Every thread of the block takes part (n threads, a multiple of 32).  Returns the CTA's run
+// (left == 0: none); ps->rec holds the split item that starts in it, ps->err any fault of
+// the lengths.
+__device__ __forceinline__ Run plan_run(const AttendArgs& a, PlanSmem* ps, int n) {
+  return a.wide ? plan_run_of<long long>(a, ps, n) : plan_run_of<int>(a, ps, n);
 }
 
 // A CTA's segments in order: each is a run of tiles of one item.
@@ -276,6 +325,7 @@ struct Segments {
   }
   __device__ bool more() const { return left > 0; }
   __device__ bool whole() const { return off == 0 && cnt == it.nt; }
+  __device__ int end() const { return (it.tile(off + cnt - 1) + 1) * kSlotTile; }
   __device__ int slot(int cta) const { return off == 0 ? 2 * cta + 1 : 2 * cta; }
   __device__ void next(const AttendArgs& a) {
     left -= cnt;

@@ -57,8 +57,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_simt(AttendArgs a) {
   uint32_t(*mask)[2] = (uint32_t(*)[2])(sm + Lay::kOffMask);
   PlanSmem* plan = (PlanSmem*)(sm + Lay::kOffPlan);
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  plan_run(a, plan, kThreads);
-  const Run run = plan->run;
+  const Run run = plan_run(a, plan, kThreads);
   int err = 0;
 
   for (Segments sg(a, run); sg.more(); sg.next(a)) {
@@ -94,7 +93,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_simt(AttendArgs a) {
     if (tid < kRowTile) {
       int h, i;
       const bool live = row_of(a, it, 0, tid, &h, &i);
-      vis = row_vis(a, it, i, live, anc[tid], &err);
+      vis = row_vis(a, it, i, live, sg.end(), anc[tid], &err);
     }
     float m[4], l[4], acc[4][8];
 #pragma unroll
@@ -266,8 +265,7 @@ __global__ void __launch_bounds__(kFewThreads, R <= 8 ? 2 : 1) k_attend_few(Atte
   FewSmem<R>& sm = *(FewSmem<R>*)sm_few;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int my_row = lane / S, my_slot = lane % S;   // of the logit that this lane ends with
-  plan_run(a, &sm.plan, kFewThreads);
-  const Run run = sm.plan.run;
+  const Run run = plan_run(a, &sm.plan, kFewThreads);
   int err = 0;
 
   for (Segments sg(a, run); sg.more(); sg.next(a)) {
@@ -286,12 +284,12 @@ __global__ void __launch_bounds__(kFewThreads, R <= 8 ? 2 : 1) k_attend_few(Atte
     // one lane of a row works out what the row sees, in the warp's own words
     uint32_t* anc = sm.anc[warp][my_row];
     RowVis vis{0, 0, 0, it.base, nullptr};
-    if (my_slot == 0) vis = row_vis(a, it, i, live, anc, &err);
+    if (my_slot == 0) vis = row_vis(a, it, i, live, sg.end(), anc, &err);
     __syncwarp();
     vis.end_s = __shfl_sync(0xffffffffu, vis.end_s, my_row * S);
     vis.lo = __shfl_sync(0xffffffffu, vis.lo, my_row * S);
     vis.hi = __shfl_sync(0xffffffffu, vis.hi, my_row * S);
-    vis.anc = a.parent ? anc : nullptr;
+    vis.anc = __shfl_sync(0xffffffffu, vis.anc != nullptr, my_row * S) ? anc : nullptr;
     float m = -INFINITY, l = 0.f;   // of row my_row: the same in its S lanes
     const size_t row_off = lane * 4;
     for (int k = 0; k < sg.cnt; ++k) {
@@ -406,9 +404,10 @@ __global__ void __launch_bounds__(kFewThreads, R <= 8 ? 2 : 1) k_attend_few(Atte
   }
 }
 
-// Adds up the partial results of the split items, and writes the call's status.  Block
-// (c, y) takes rows of the item that starts in CTA c: a warp each, or, where items have few
-// rows and so may have many parts, one row whose parts go round the eight warps.
+// Adds up the partial results of the split items, and writes the call's status.  Blocks
+// (c, y) take the rows of the item that starts in CTA c.  Few rows (kFewRows) may have many
+// parts: a block takes one row, whose parts go round the eight warps.  Else a warp takes
+// one row, or four where there are only two parts: eight loads of outputs are in flight.
 template <typename T, bool kFewRows>
 __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int G) {
   chain_wait();
@@ -422,30 +421,72 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int G) {
     if (lane == 0) *a.status = err;
   }
   const AttendRec rec = a.rec[c];
-  const int row = kFewRows ? blockIdx.y : blockIdx.y * 8 + warp;
-  if (rec.u < 0 || row >= a.rows) return;
+  const bool four = !kFewRows && rec.last == c + 1;
+  const int row0 = kFewRows ? blockIdx.y : four ? blockIdx.y * 32 + warp * 4 : blockIdx.y * 8 + warp;
+  if (rec.u < 0 || row0 >= a.rows) return;
   const Item it = make_item(a, rec.u, rec.qb);
-  const int per = a.T * a.g, w = row / per;
-  int h, i;
-  if (!row_of(a, it, w, row - w * per, &h, &i)) return;
-  float M = -INFINITY;
+  const int per = a.T * a.g;
   // part 0 is in the CTA's second slot, the others in the first of the CTAs after it
-  auto at = [&](int x) { return (size_t)(x == c ? 2 * c + 1 : 2 * x) * a.rows + row; };
-  for (int x = c + lane; x <= rec.last; x += 32) M = fmaxf(M, a.pml[at(x)].x);
+  auto at = [&](int x, int row) { return (size_t)(x == c ? 2 * c + 1 : 2 * x) * a.rows + row; };
+  auto store = [&](int row, float M, float l, float4 o) {
+    const int w = row / per;
+    int h, i;
+    if (!row_of(a, it, w, row - w * per, &h, &i)) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const size_t dst = ((size_t)it.u * a.g + h) * a.t + i;
+    store_row4((T*)a.out + dst * kD + lane * 4,
+               make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (a.lse && lane == 0) a.lse[dst] = row_lse(M, l);
+  };
+  if (four) {
+    float2 ml[4][2];
+    float4 p[4][2];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const size_t x = at(c + y, min(row0 + r, a.rows - 1));
+        ml[r][y] = a.pml[x];
+        p[r][y] = ((const float4*)(a.po + x * kD))[lane];
+      }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float M = fmaxf(ml[r][0].x, ml[r][1].x);
+      const float f = weight_of(ml[r][0].x, M), g = weight_of(ml[r][1].x, M);
+      if (row0 + r < a.rows)
+        store(row0 + r, M, f * ml[r][0].y + g * ml[r][1].y,
+              make_float4(fmaf(f, p[r][0].x, g * p[r][1].x), fmaf(f, p[r][0].y, g * p[r][1].y),
+                          fmaf(f, p[r][0].z, g * p[r][1].z), fmaf(f, p[r][0].w, g * p[r][1].w)));
+    }
+    return;
+  }
+  const int x0 = c + (kFewRows ? warp : 0);
+  constexpr int kStep = kFewRows ? 8 : 1, kUnroll = kFewRows ? 4 : 8;
+  float M = -INFINITY;
+  for (int x = c + lane; x <= rec.last; x += 32) M = fmaxf(M, a.pml[at(x, row0)].x);
 #pragma unroll
   for (int d = 16; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
   float l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int x = c + (kFewRows ? warp : 0); x <= rec.last; x += kFewRows ? 8 : 1) {
-    const float2 ml = a.pml[at(x)];
-    const float f = weight_of(ml.x, M);
-    const float4 p = ((const float4*)(a.po + at(x) * kD))[lane];
-    l += f * ml.y;
-    o.x = fmaf(f, p.x, o.x);
-    o.y = fmaf(f, p.y, o.y);
-    o.z = fmaf(f, p.z, o.z);
-    o.w = fmaf(f, p.w, o.w);
+  for (int x = x0; x <= rec.last; x += kStep * kUnroll) {   // kUnroll parts to a round trip
+    float2 ml[kUnroll];
+    float4 p[kUnroll];
+#pragma unroll
+    for (int y = 0; y < kUnroll; ++y) {
+      const bool has = x + y * kStep <= rec.last;
+      const size_t z = at(has ? x + y * kStep : c, row0);
+      ml[y] = has ? a.pml[z] : make_float2(-INFINITY, 0.f);
+      p[y] = has ? ((const float4*)(a.po + z * kD))[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int y = 0; y < kUnroll; ++y) {
+      const float f = weight_of(ml[y].x, M);
+      l += f * ml[y].y;
+      o.x = fmaf(f, p[y].x, o.x);
+      o.y = fmaf(f, p[y].y, o.y);
+      o.z = fmaf(f, p[y].z, o.z);
+      o.w = fmaf(f, p[y].w, o.w);
+    }
   }
   if (kFewRows) {
     sum_o[warp][lane] = o;
@@ -462,11 +503,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int G) {
       o.w += p.w;
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const size_t dst = ((size_t)it.u * a.g + h) * a.t + i;
-  store_row4((T*)a.out + dst * kD + lane * 4,
-             make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-  if (a.lse && lane == 0) a.lse[dst] = row_lse(M, l);
+  store(row0, M, l, o);
 }
 
 template <typename T>
@@ -545,6 +582,9 @@ cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, con
   plan_rows(s, &a.T, &a.nq);
   a.QB = (s.t + a.nq * a.T - 1) / (a.nq * a.T);
   a.rows = a.nq * a.T * s.g;
+  // two row tiles: an item's start and end take about three tiles' time, 8 K cycles
+  a.extra = a.nq == 2 ? 3 : 0;
+  a.wide = (int64_t)s.U * a.QB * (((int64_t)s.cols << s.shift) / kSlotTile + 3 + a.extra) >= 1 << 30;
   const int sms = sm_count();
   if (sms <= 0 || sms > kMaxAttendSms) return cudaErrorInvalidDevice;
   const int G = sms * ctas_per_sm(s, a.rows);

@@ -27,6 +27,8 @@
 // four words, and V is searched for non-finite elements first: they are set to zero
 // in shared memory (0 x NaN would reach rows that do not see the slot; what was
 // never loaded is there too) and added again, at the end, to the rows that do see them.
+#include <stddef.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -62,17 +64,17 @@ struct TcLayout {
 };
 static_assert(TcLayout<2>::kBytes <= 227 * 1024 && sizeof(PlanSmem) <= 1024, "smem");
 
+// Arrivals that complete a phase: 4 softmax warps, 2 searchers, else one.
 struct TcBars {
-  uint64_t ring_full[kRing], ring_empty[kRing];
-  uint64_t q_full[2], q_empty[2];
-  uint64_t s_full[2], p_full[2], o_done[2];
-  uint64_t v_ok[2];       // V of the slot has been passed by both searchers
-  uint64_t searched[4];   // V of a masked tile has been searched (uses in turn)
-  uint64_t drain;
+  uint64_t p_full[2];     // 4: P written
+  uint64_t v_ok[2];       // 2: V of the slot has been passed by both searchers
+  uint64_t searched[4];   // 2: V of a masked tile has been searched (uses in turn)
+  uint64_t ring_full[kRing], ring_empty[kRing], q_full[2], q_empty[2], s_full[2], o_done[2], drain;
   uint32_t tmem;
   int abort;
 };
-static_assert(sizeof(TcBars) <= 512, "barrier block");
+constexpr int kBars = 8 + 2 * kRing + 9;
+static_assert(sizeof(TcBars) <= 512 && kBars <= 32 && offsetof(TcBars, tmem) == 8 * kBars, "barriers");
 
 struct Ring {
   uint32_t slot = 0, phase = 0;
@@ -247,31 +249,22 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // warp-uniform for the compiler
 
-  if (tid == 0) {
-    for (int i = 0; i < kRing; ++i) {
-      mbar_init(&bars->ring_full[i], 1);
-      mbar_init(&bars->ring_empty[i], 1);
+  if (warp == 0) {   // a barrier a lane: the instructions of a start are fetched one by one
+    if (lane < kBars) mbar_init((uint64_t*)bars + lane, lane < 2 ? 4 : lane < 8 ? 2 : 1);
+    if (lane == 0) {
+      bars->abort = 0;
+      prefetch_tensormap(&tmQ);
+      prefetch_tensormap(&tmK);
+      prefetch_tensormap(&tmV);
     }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&bars->q_full[i], 1);
-      mbar_init(&bars->q_empty[i], 1);
-      mbar_init(&bars->s_full[i], 1);
-      mbar_init(&bars->p_full[i], 4);
-      mbar_init(&bars->o_done[i], 1);
-      mbar_init(&bars->v_ok[i], 2);
-    }
-    for (int i = 0; i < 4; ++i) mbar_init(&bars->searched[i], 2);
-    mbar_init(&bars->drain, 1);
-    bars->abort = 0;
     fence_mbar_init();
   }
   if (warp == 1) {
     tmem_alloc(&bars->tmem, 512);
     tmem_relinquish();
   }
-  plan_run(a, plan, Lay::kThreads);   // ends with a barrier
+  const Run run = plan_run(a, plan, Lay::kThreads);   // ends with a barrier
   tc_fence_after();
-  const Run run = plan->run;
   const uint32_t tmem = bars->tmem;
   volatile int* abort_flag = &bars->abort;
   int err = 0;
@@ -279,11 +272,6 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
   if (warp == 0) {
     // -------------------------------------------------------------- producer
     fewer_regs<NQ>();
-    if (lane == 0) {
-      prefetch_tensormap(&tmQ);
-      prefetch_tensormap(&tmK);
-      prefetch_tensormap(&tmV);
-    }
     const uint64_t keep = l2_evict_normal();
     const int per_tile = kSlotTile >> a.shift;
     const uint32_t page_bytes = 128u << a.shift;   // of one half
@@ -483,9 +471,12 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
 #pragma unroll 1
         for (int r = 0; r < 2; ++r) {
           const int q = (warp - 2) * 2 + r;
-          const uint32_t bits = __ballot_sync(0xffffffffu, clean_row(tile, q * 32 + lane));
+          // (what lies in slots that were not loaded may look like anything; no row sees it)
+          const int slot = it.tile(sg.off + k) * kSlotTile + q * 32 + lane;
+          const bool found = clean_row(tile, q * 32 + lane);
+          const uint32_t bits = __ballot_sync(0xffffffffu, found && it.wanted(slot, slot + 1));
           if (lane == 0 && e < kMaxEdges) words[q] = bits;
-          if (bits) fence_proxy_async_smem();
+          fence_proxy_async_smem();
         }
         arrive_warp(&bars->searched[edges & 3], lane);
         if (lane == 0) mbar_arrive(&bars->v_ok[vp.slot >> 1]);
@@ -507,7 +498,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
       int h, i;
       const bool live = row_of(a, it, w, row, &h, &i);
       const bool warp_live = __any_sync(0xffffffffu, live);
-      const RowVis vis = row_vis(a, it, i, live, anc, &err);
+      const RowVis vis = row_vis(a, it, i, live, sg.end(), anc, &err);
       const int t0 = it.tok0 + w * a.T, nt = min(a.T, it.tok0 + it.ntok - t0);
       const FullTiles all_full(a, it, it.tok0, it.ntok), full(a, it, t0, nt);
       uint4* bad = bad_all + (seg & 3) * kMaxEdges;
