@@ -177,11 +177,14 @@ template <typename I>   // of positions: 32 bits where they all fit
 struct Split {
   I total, q;
   int r, G;
-  __device__ Split(I all, int ctas) : total(all), G(ctas) {
+  float inv;
+  __device__ Split(I all, int ctas) : total(all), G(ctas), inv(1.f / (float)ctas) {
     q = all / ctas;
     r = (int)(all - q * ctas);
   }
-  __device__ I start(int c) const { return q * c + (uint32_t)(r * c) / (uint32_t)G; }
+  // r c / G through fp32: r c + 1/2 over G is at least 1 / (2 G) > 2^-10 from a whole number, and
+  // below 2^9, so that an error of a few 2^-23 of it does not reach one
+  __device__ I start(int c) const { return q * c + (int)(((float)(r * c) + 0.5f) * inv); }
   __device__ int owner(I t) const {
     int c = min(G - 1, (int)((float)t * ((float)G / (float)total)));
     while (c > 0 && start(c) > t) --c;
@@ -202,6 +205,13 @@ struct PlanSmem {
   int warp_items[32];
   int err;
 };
+
+__device__ __forceinline__ int warp_total(int x) { return __reduce_add_sync(0xffffffffu, x); }
+__device__ __forceinline__ long long warp_total(long long x) {
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+  return x;
+}
 
 template <typename I>
 __device__ __forceinline__ Run plan_run_of(const AttendArgs& a, PlanSmem* ps, int n) {
@@ -248,18 +258,12 @@ __device__ __forceinline__ Run plan_run_of(const AttendArgs& a, PlanSmem* ps, in
     ps->warp_items[warp] = scan_live;
   }
   __syncthreads();
-  I tiles = 0, all = 0;   // tiles in front of this thread's items, and of all
-  int front = 0, all_live = 0;
-  for (int w = 0; w < n / 32; ++w) {
-    if (w < warp) {
-      tiles += (I)ps->warp_sum[w];
-      front += ps->warp_items[w];
-    }
-    all += (I)ps->warp_sum[w];
-    all_live += ps->warp_items[w];
-  }
-  tiles += scan - mine;
-  front += scan_live - live;
+  // tiles and items in front of this thread's items, and of all
+  const I sum = lane < n / 32 ? (I)ps->warp_sum[lane] : 0;
+  const int cnt = lane < n / 32 ? ps->warp_items[lane] : 0;
+  const I all = warp_total(sum), tiles_before = warp_total(lane < warp ? sum : (I)0);
+  const int all_live = warp_total(cnt), front = warp_total(lane < warp ? cnt : 0) + scan_live - live;
+  I tiles = tiles_before + scan - mine;
   if (all > 0) {
     const Split<I> sp(all + (I)a.extra * all_live, (int)min((I)gridDim.x, all));
     const int c = blockIdx.x;

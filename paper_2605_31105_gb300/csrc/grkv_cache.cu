@@ -114,52 +114,77 @@ struct Table {
   }
 };
 
+// The status of a call whose only block writes it whole (solo), which saves the call a memset,
+// or of one whose blocks add their faults to a cleared word.
+struct Status {
+  int* word;
+  int* at;   // where faults go
+  bool solo;
+  __device__ Status(int* word_, int* shared, bool solo_) : word(word_), at(solo_ ? shared : word_), solo(solo_) {
+    if (!solo) return;
+    if (threadIdx.x == 0) *at = 0;
+    __syncthreads();
+  }
+  __device__ void end() const {   // all threads of the block
+    if (!solo) return;
+    __syncthreads();
+    if (threadIdx.x == 0) *word = *at;
+  }
+};
+
 // ------------------------------------------------------------------- fork, trim
-__global__ void k_cache_fork(Table tb, int units_in, const int32_t* __restrict__ src,
-                             const int32_t* __restrict__ table_in,
-                             const int32_t* __restrict__ len_in, int32_t* table_out,
-                             int32_t* len_out, int32_t* refs, int* status) {
-  for (int u = blockIdx.x; u < tb.U; u += gridDim.x) {
+// A thread per table entry.
+__global__ void __launch_bounds__(1024)
+    k_cache_fork(Table tb, int units_in, const int32_t* __restrict__ src,
+                 const int32_t* __restrict__ table_in, const int32_t* __restrict__ len_in,
+                 int32_t* table_out, int32_t* len_out, int32_t* refs, int* word, bool solo) {
+  __shared__ int shared;
+  const Status st(word, &shared, solo);
+  const int all = tb.U * tb.cols;
+  for (int x = blockIdx.x * blockDim.x + threadIdx.x; x < all; x += gridDim.x * blockDim.x) {
+    const int u = x / tb.cols, c = x - u * tb.cols;
     int s = src[u];
     if (s < -1 || s >= units_in) {
-      if (threadIdx.x == 0) set_status(status, GRKV_ERR_INVALID_ARG);
+      set_status(st.at, GRKV_ERR_INVALID_ARG);
       s = -1;
     }
-    const int len = s >= 0 ? tb.clamped(len_in[s], status) : 0;
-    const int need = (len + tb.page() - 1) >> tb.shift;
-    for (int c = threadIdx.x; c < tb.cols; c += blockDim.x) {
-      int e = -1;
-      if (c < need) {
-        e = table_in[(size_t)s * tb.cols + c];
-        if ((unsigned)e < (unsigned)tb.P) {
-          atomicAdd(refs + e, 1);
-        } else {
-          set_status(status, GRKV_ERR_INVALID_ARG);
-          e = -1;
-        }
+    const int len = s >= 0 ? tb.clamped(len_in[s], st.at) : 0;
+    int e = -1;
+    if (c << tb.shift < len) {
+      e = table_in[(size_t)s * tb.cols + c];
+      if ((unsigned)e < (unsigned)tb.P) {
+        atomicAdd(refs + e, 1);
+      } else {
+        set_status(st.at, GRKV_ERR_INVALID_ARG);
+        e = -1;
       }
-      table_out[(size_t)u * tb.cols + c] = e;
     }
-    if (threadIdx.x == 0) len_out[u] = len;
+    table_out[x] = e;
+    if (c == 0) len_out[u] = len;
   }
+  st.end();
 }
 
-__global__ void k_cache_trim(Table tb, int32_t* table, const int32_t* __restrict__ len,
-                             int32_t* refs, int* status) {
-  for (int u = blockIdx.x; u < tb.U; u += gridDim.x) {
-    const int need = (tb.clamped(len[u], status) + tb.page() - 1) >> tb.shift;
-    for (int c = need + threadIdx.x; c < tb.cols; c += blockDim.x) {
-      const int e = table[(size_t)u * tb.cols + c];
-      if (e < 0) continue;
-      if (e >= tb.P) {
-        set_status(status, GRKV_ERR_INVALID_ARG);
-      } else if (atomicSub(refs + e, 1) <= 0) {   // nobody held it: the count stays
-        atomicAdd(refs + e, 1);
-        set_status(status, GRKV_ERR_INVALID_ARG);
-      }
-      table[(size_t)u * tb.cols + c] = -1;
+__global__ void __launch_bounds__(1024)
+    k_cache_trim(Table tb, int32_t* table, const int32_t* __restrict__ len, int32_t* refs, int* word,
+                 bool solo) {
+  __shared__ int shared;
+  const Status st(word, &shared, solo);
+  const int all = tb.U * tb.cols;
+  for (int x = blockIdx.x * blockDim.x + threadIdx.x; x < all; x += gridDim.x * blockDim.x) {
+    const int u = x / tb.cols, c = x - u * tb.cols, n = tb.clamped(len[u], st.at);
+    if (c << tb.shift < n) continue;
+    const int e = table[x];
+    if (e < 0) continue;
+    if (e >= tb.P) {
+      set_status(st.at, GRKV_ERR_INVALID_ARG);
+    } else if (atomicSub(refs + e, 1) <= 0) {   // nobody held it: the count stays
+      atomicAdd(refs + e, 1);
+      set_status(st.at, GRKV_ERR_INVALID_ARG);
     }
+    table[x] = -1;
   }
+  st.end();
 }
 
 // ---------------------------------------------------------------------- reserve
@@ -189,48 +214,78 @@ __device__ __forceinline__ int block_scan(int x, int* total, int* warp_sum) {
 
 // One block.  The columns that unit u is to write are [len / page, ceil(want / page)); one
 // needs a new page if it has none or one that others hold too.  The decisions are all made
-// on the counts as the call found them, before any of them changes.
+// on the counts as the call found them, before any of them changes: where every unit has a
+// thread of its own and at most 32 such columns (a few tokens of every unit of a batch) they
+// stay in that thread's registers, else they are marked in the table, -2 - page.
+constexpr int kListShared = 4096;   // free pages that fit the block's own list
 __global__ void __launch_bounds__(kReserveThreads)
     k_cache_reserve(Table tb, int32_t* table, const int32_t* __restrict__ len,
-                    const int32_t* __restrict__ want, int32_t* refs, int32_t* list, int4* jobs,
-                    int* status) {
-  __shared__ int warp_sum[32];
+                    const int32_t* __restrict__ want, int32_t* refs, int32_t* list_ws, int4* jobs,
+                    int* word) {
+  __shared__ int warp_sum[32], shared, list_sm[kListShared];
+  __shared__ uint32_t free_words[kReserveThreads / 2];   // a bit a page, 16 a thread
   const int tid = threadIdx.x, n = blockDim.x;
+  // Marks which of the 16 K pages from p0 on nobody holds (read after a barrier).
+  auto look = [&](int p0) {
+    const int lane = tid & 31, a = p0 + (tid >> 5) * 512 + lane;
+    int held[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) held[k] = a + k * 32 < tb.P ? refs[a + k * 32] : 1;
+    uint32_t mine = 0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const uint32_t w = __ballot_sync(0xffffffffu, held[k] <= 0);
+      if (lane == k) mine = w;
+    }
+    if (lane < 16) free_words[(tid >> 5) * 16 + lane] = mine;
+  };
+  look(0);
+  const Status st(word, &shared, true);
   const int per = (tb.U + n - 1) / n, u0 = min(tb.U, tid * per), u1 = min(tb.U, u0 + per);
   auto columns = [&](int u, int* c0, int* c1) {
-    const int a = tb.clamped(len[u], status), b = tb.clamped(want[u], status);
+    const int a = tb.clamped(len[u], st.at), b = tb.clamped(want[u], st.at);
     *c0 = a >> tb.shift;
     *c1 = b > a ? (b + tb.page() - 1) >> tb.shift : *c0;
     return a;
   };
   int mine = 0;
+  uint32_t bits = 0;   // of the thread's only unit: columns from c0 on that need a page
+  bool wide = per > 1;
   for (int u = u0; u < u1; ++u) {
     int c0, c1;
     columns(u, &c0, &c1);
+    wide |= c1 - c0 > 32;
     for (int c = c0; c < c1; ++c) {
       const int e = table[(size_t)u * tb.cols + c];
-      if (e >= tb.P) set_status(status, GRKV_ERR_INVALID_ARG);
-      mine += e < 0 || e >= tb.P || refs[e] > 1;
+      if (e >= tb.P) set_status(st.at, GRKV_ERR_INVALID_ARG);
+      if (e < 0 || e >= tb.P || refs[e] > 1) {
+        ++mine;
+        bits |= 1u << ((c - c0) & 31);
+      }
     }
   }
+  const bool marks = __syncthreads_or(wide);
   int need;
   int at = block_scan(mine, &need, warp_sum);
+  int32_t* list = need <= kListShared ? list_sm : list_ws;
   // the lowest free pages
   int found = 0;
   for (int p0 = 0; p0 < tb.P && found < need; p0 += n * 16) {
-    int free_bits = 0;
     const int a = p0 + tid * 16;
-#pragma unroll
-    for (int k = 0; k < 16; ++k)
-      if (a + k < tb.P && refs[a + k] <= 0) free_bits |= 1 << k;
+    if (p0 > 0) {
+      __syncthreads();
+      look(p0);
+      __syncthreads();
+    }
+    uint32_t free_bits = (free_words[tid >> 1] >> (16 * (tid & 1))) & 0xffffu;
     int all, r = found + block_scan(__popc(free_bits), &all, warp_sum);
     for (; free_bits && r < need; free_bits &= free_bits - 1) list[r++] = a + __ffs(free_bits) - 1;
     found += all;
   }
   const bool enough = found >= need;
-  if (!enough && tid == 0) set_status(status, GRKV_ERR_NO_PAGES);
+  if (!enough && tid == 0) set_status(st.at, GRKV_ERR_NO_PAGES);
   __syncthreads();
-  if (enough) {   // a page that is to be replaced is marked -2 - page
+  if (enough && marks) {
     for (int u = u0; u < u1; ++u) {
       int c0, c1;
       columns(u, &c0, &c1);
@@ -243,18 +298,25 @@ __global__ void __launch_bounds__(kReserveThreads)
       }
     }
   }
-  __syncthreads();
+  if (marks) __syncthreads();
   for (int u = u0; u < u1; ++u) {
     int4 job = make_int4(-1, -1, 0, 0);
     int c0, c1;
     const int a = columns(u, &c0, &c1);
     for (int c = c0; enough && c < c1; ++c) {
       int32_t* e = table + (size_t)u * tb.cols + c;
-      if (*e >= 0) continue;
+      int old = *e;   // the page to replace, or negative
+      if (marks) {
+        if (old >= 0) continue;
+        old = old <= -2 ? -2 - old : -1;
+      } else {
+        if (!((bits >> (c - c0)) & 1)) continue;
+        if (old >= tb.P) old = -1;
+      }
       const int page = list[at++];
       refs[page] = 1;
-      if (*e <= -2) {
-        const int old = -2 - *e, part = a - (c << tb.shift);
+      if (old >= 0) {
+        const int part = a - (c << tb.shift);
         atomicSub(refs + old, 1);
         if (part > 0) job = make_int4(old, page, part, 0);
       }
@@ -262,6 +324,7 @@ __global__ void __launch_bounds__(kReserveThreads)
     }
     jobs[u] = job;
   }
+  st.end();
 }
 
 // Copies the filled slots of the shared pages that a reserve replaced.
@@ -282,8 +345,9 @@ __global__ void k_cache_copy(int U, int row16, int page, const int4* __restrict_
 // --------------------------------------------------------------- append, compact
 struct RowMove {
   Table tb;
-  int t, row16;              // rows per unit, 16-byte chunks of a row
+  int t;                     // rows per unit
   const int32_t* count;      // rows of a unit, or null: t
+  const int32_t* len;        // slots of a unit
   int* status;
 };
 
@@ -304,39 +368,69 @@ __device__ __forceinline__ int rows_of(const RowMove& m, int u) {
   return min(max(n, 0), m.t);
 }
 
-// A thread per 16-byte chunk of a new row.
-__global__ void k_cache_append(RowMove m, const uint4* __restrict__ k_new,
-                               const uint4* __restrict__ v_new, const int64_t* __restrict__ first,
-                               const int32_t* __restrict__ table, const int32_t* __restrict__ len,
-                               uint4* k, uint4* v) {
-  const size_t all = (size_t)m.tb.U * m.t * m.row16;
-  for (size_t x = (size_t)blockIdx.x * blockDim.x + threadIdx.x; x < all;
-       x += (size_t)gridDim.x * blockDim.x) {
-    const size_t row = x / m.row16;
-    const int ch = (int)(x - row * m.row16), u = (int)(row / m.t), i = (int)(row - (size_t)u * m.t);
-    const int n = rows_of(m, u), slot = m.tb.clamped(len[u], m.status) - n + i;
-    if (i >= n) continue;
+// Copies of rows: a block takes 4 x 256 / kRow16 rows of one unit (grid (blocks of rows, units)),
+// kRow16 lanes a row of kRow16 16-byte chunks, four rows of K and V in flight to a thread.
+constexpr int kMoveThreads = 256, kMoveUnroll = 4;
+constexpr int move_rows(int row16) { return kMoveUnroll * kMoveThreads / row16; }
+
+// where(u, i, n, len, &from, &to): source and destination row of row i of unit u's n; false: none
+template <int kRow16, typename Where>
+__device__ __forceinline__ void move_block(const RowMove& m, const uint4* k_in, const uint4* v_in,
+                                           uint4* k, uint4* v, Where where) {
+  const int ch = threadIdx.x % kRow16, r = threadIdx.x / kRow16;
+  for (int u = blockIdx.y; u < m.tb.U; u += gridDim.y) {
+    const int len = m.tb.clamped(m.len[u], m.status);
+    const int n = rows_of(m, u), i0 = blockIdx.x * move_rows(kRow16) + r;
+    long long to[kMoveUnroll];
+    uint4 x[kMoveUnroll], y[kMoveUnroll];
+#pragma unroll
+    for (int j = 0; j < kMoveUnroll; ++j) {
+      const int i = i0 + j * (kMoveThreads / kRow16);
+      long long from = 0;
+      to[j] = -1;
+      if (i >= n || !where(u, i, n, len, &from, &to[j])) {
+        to[j] = -1;
+        continue;
+      }
+      x[j] = k_in[from * kRow16 + ch];
+      y[j] = v_in[from * kRow16 + ch];
+    }
+#pragma unroll
+    for (int j = 0; j < kMoveUnroll; ++j) {
+      if (to[j] < 0) continue;
+      k[to[j] * kRow16 + ch] = x[j];
+      v[to[j] * kRow16 + ch] = y[j];
+    }
+  }
+}
+
+template <int kRow16>
+__global__ void __launch_bounds__(kMoveThreads)
+    k_cache_append(RowMove m, const uint4* __restrict__ k_new, const uint4* __restrict__ v_new,
+                   const int64_t* __restrict__ first, const int32_t* __restrict__ table, uint4* k,
+                   uint4* v) {
+  move_block<kRow16>(m, k_new, v_new, k, v, [&](int u, int i, int n, int len, long long* from,
+                                                long long* to) {
+    const int slot = len - n + i;
     if (slot < 0) {
       set_status(m.status, GRKV_ERR_INVALID_ARG);
-      continue;
+      return false;
     }
-    const long long to = pool_row(m.tb, table, u, slot, m.status);
-    if (to < 0) continue;
-    const size_t from = first ? (size_t)first[u] + i : row;
-    k[to * m.row16 + ch] = __ldg(k_new + from * m.row16 + ch);
-    v[to * m.row16 + ch] = __ldg(v_new + from * m.row16 + ch);
-  }
+    *from = first ? first[u] + i : (long long)u * m.t + i;
+    *to = pool_row(m.tb, table, u, slot, m.status);
+    return *to >= 0;
+  });
 }
 
 // Where row i of unit u's kept rows comes from and goes to; false (and the status) if the
 // call's contract is broken there.
 __device__ __forceinline__ bool kept_row(const RowMove& m, const int32_t* idx,
-                                         const int32_t* table_in, const int32_t* len_in,
-                                         const int32_t* table_out, const int32_t* first, bool in_place,
-                                         int u, int i, long long* from, long long* to) {
+                                         const int32_t* table_in, int len, const int32_t* table_out,
+                                         const int32_t* first, bool in_place, int u, int i,
+                                         long long* from, long long* to) {
   const int cap = m.tb.cols << m.tb.shift, f = first ? first[u] : 0, src = idx[(size_t)u * m.t + i];
   const int dst = min(max(f, 0), cap) + i;
-  if (src < 0 || src >= m.tb.clamped(len_in[u], m.status) || f < 0 || dst >= cap ||
+  if (src < 0 || src >= len || f < 0 || dst >= cap ||
       (in_place && src < dst)) {
     set_status(m.status, GRKV_ERR_INVALID_ARG);
     return false;
@@ -347,36 +441,27 @@ __device__ __forceinline__ bool kept_row(const RowMove& m, const int32_t* idx,
 }
 
 // To other pages: every row by itself.
-__global__ void k_cache_gather(RowMove m, const int32_t* __restrict__ idx,
-                               const int32_t* __restrict__ table_in,
-                               const int32_t* __restrict__ len_in,
-                               const int32_t* __restrict__ table_out,
-                               const int32_t* __restrict__ first, uint4* k, uint4* v) {
-  const size_t all = (size_t)m.tb.U * m.t * m.row16;
-  for (size_t x = (size_t)blockIdx.x * blockDim.x + threadIdx.x; x < all;
-       x += (size_t)gridDim.x * blockDim.x) {
-    const size_t row = x / m.row16;
-    const int ch = (int)(x - row * m.row16), u = (int)(row / m.t), i = (int)(row - (size_t)u * m.t);
-    long long from, to;
-    if (i >= rows_of(m, u) ||
-        !kept_row(m, idx, table_in, len_in, table_out, first, false, u, i, &from, &to))
-      continue;
-    k[to * m.row16 + ch] = k[from * m.row16 + ch];
-    v[to * m.row16 + ch] = v[from * m.row16 + ch];
-  }
+template <int kRow16>
+__global__ void __launch_bounds__(kMoveThreads)
+    k_cache_gather(RowMove m, const int32_t* __restrict__ idx, const int32_t* __restrict__ table_in,
+                   const int32_t* __restrict__ table_out, const int32_t* __restrict__ first, uint4* k,
+                   uint4* v) {
+  move_block<kRow16>(m, k, v, k, v, [&](int u, int i, int, int len, long long* from, long long* to) {
+    return kept_row(m, idx, table_in, len, table_out, first, false, u, i, from, to);
+  });
 }
 
 // In place: a row only moves down, so chunks of rows in ascending order, each read as a whole
 // before it is written, never overwrite a row that is still to be read.  A block owns 64
 // bytes of every row of one unit's keys or values (grid (U, 2, row bytes / 64)).
 constexpr int kShiftThreads = 256, kShiftUnroll = 4;
+template <int kRow16>
 __global__ void __launch_bounds__(kShiftThreads)
     k_cache_shift(RowMove m, const int32_t* __restrict__ idx, const int32_t* __restrict__ table,
-                  const int32_t* __restrict__ len_in, const int32_t* __restrict__ first, uint4* k,
-                  uint4* v) {
+                  const int32_t* __restrict__ first, uint4* k, uint4* v) {
   const int u = blockIdx.x, ch = blockIdx.z * 4 + (threadIdx.x & 3), r0 = threadIdx.x >> 2;
   uint4* pool = blockIdx.y ? v : k;
-  const int n = rows_of(m, u);
+  const int n = rows_of(m, u), len = m.tb.clamped(m.len[u], m.status);
   constexpr int kRows = kShiftThreads / 4;
   for (int base = 0; base < n; base += kRows * kShiftUnroll) {
     uint4 x[kShiftUnroll];
@@ -386,22 +471,47 @@ __global__ void __launch_bounds__(kShiftThreads)
       const int i = base + j * kRows + r0;
       long long from;
       to[j] = -1;
-      if (i < n && kept_row(m, idx, table, len_in, table, first, true, u, i, &from, &to[j]) &&
+      if (i < n && kept_row(m, idx, table, len, table, first, true, u, i, &from, &to[j]) &&
           from != to[j])
-        x[j] = pool[from * m.row16 + ch];
+        x[j] = pool[from * kRow16 + ch];
       else
         to[j] = -1;
     }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kShiftUnroll; ++j)
-      if (to[j] >= 0) pool[to[j] * m.row16 + ch] = x[j];
+      if (to[j] >= 0) pool[to[j] * kRow16 + ch] = x[j];
     __syncthreads();
   }
 }
 
 Table table_of(const CacheShape& s) { return Table{s.U, s.cols, s.P, s.shift}; }
 int row16_of(const CacheShape& s) { return kD * (s.dtype == GRKV_F32 ? 4 : 2) / 16; }
+
+// A launch of k_cache_fork or k_cache_trim, 1024 entries a block.  Up to 2 K entries go to one
+// block, which also writes the status: its second round costs what a memset does (1.2 us).
+template <typename... Params, typename... Args>
+int table_call(const CacheShape& s, const CacheWs& L, char* ws, cudaStream_t st,
+               void (*kern)(Params...), Args&&... args) {
+  const int entries = s.U * s.cols;
+  const bool solo = entries <= 1 << 11;
+  if (!solo) GRKV_TRY(clear_status(ws, L, st));
+  count_launches(1);
+  return cuda_rc(launch_kernel(false, 1, kern, dim3(solo ? 1u : (unsigned)((entries + 1023) / 1024)), 1024,
+                               0, st, table_of(s), std::forward<Args>(args)..., (int*)(ws + L.status),
+                               solo));
+}
+
+// A launch of k_cache_append or k_cache_gather: rows of 16 (bf16) or 32 (fp32) chunks.
+template <typename... Params, typename... Args>
+cudaError_t launch_rows(const CacheShape& s, void (*k16)(Params...), void (*k32)(Params...),
+                        cudaStream_t st, Args&&... args) {
+  const int row16 = row16_of(s), rows = move_rows(row16);
+  count_launches(1);
+  return launch_kernel(false, 1, row16 == 16 ? k16 : k32,
+                       dim3((unsigned)((s.t + rows - 1) / rows), (unsigned)std::min(s.U, 65535)),
+                       kMoveThreads, 0, st, std::forward<Args>(args)...);
+}
 
 int attend(const grkv_cache_params* p, const AttendIo& io, bool tree, void* ws, size_t ws_bytes,
            void* stream) {
@@ -476,12 +586,9 @@ int grkv_cache_fork(const grkv_cache_params* p, int32_t units_in, const int32_t*
     if (units_in > 0) GRKV_TRY(check_ptrs({table_in, len_in}, 4));
     if (table_in == table_out || len_in == len_out) return GRKV_ERR_INVALID_ARG;
   }
-  GRKV_TRY(clear_status((char*)ws, L, st));
-  if (s.U == 0) return GRKV_OK;
-  count_launches(1);
-  return cuda_rc(launch_kernel(false, 1, k_cache_fork, dim3(std::min(s.U, 65535)), 128, 0, st,
-                               table_of(s), units_in, src, table_in, len_in, table_out, len_out,
-                               refs, (int*)((char*)ws + L.status)));
+  if (s.U == 0) return clear_status((char*)ws, L, st);
+  return table_call(s, L, (char*)ws, st, k_cache_fork, units_in, src, table_in, len_in, table_out,
+                    len_out, refs);
 }
 
 int grkv_cache_trim(const grkv_cache_params* p, int32_t* table, const int32_t* len, int32_t* refs,
@@ -491,11 +598,8 @@ int grkv_cache_trim(const grkv_cache_params* p, int32_t* table, const int32_t* l
   GRKV_TRY(begin(p, ws, ws_bytes, &s, &L));
   if (s.U > 0) GRKV_TRY(check_ptrs({table, len, refs}, 4));
   cudaStream_t st = (cudaStream_t)stream;
-  GRKV_TRY(clear_status((char*)ws, L, st));
-  if (s.U == 0) return GRKV_OK;
-  count_launches(1);
-  return cuda_rc(launch_kernel(false, 1, k_cache_trim, dim3(std::min(s.U, 65535)), 128, 0, st,
-                               table_of(s), table, len, refs, (int*)((char*)ws + L.status)));
+  if (s.U == 0) return clear_status((char*)ws, L, st);
+  return table_call(s, L, (char*)ws, st, k_cache_trim, table, len, refs);
 }
 
 int grkv_cache_reserve(const grkv_cache_params* p, int32_t* table, const int32_t* len,
@@ -510,8 +614,7 @@ int grkv_cache_reserve(const grkv_cache_params* p, int32_t* table, const int32_t
   }
   cudaStream_t st = (cudaStream_t)stream;
   char* w = (char*)ws;
-  GRKV_TRY(clear_status(w, L, st));
-  if (s.U == 0) return GRKV_OK;
+  if (s.U == 0) return clear_status(w, L, st);
   count_launches(2);
   GRKV_TRY(cuda_rc(launch_kernel(false, 1, k_cache_reserve, dim3(1), kReserveThreads, 0, st,
                                  table_of(s), table, len, want, refs, (int32_t*)(w + L.list),
@@ -537,12 +640,10 @@ int grkv_cache_append(const grkv_cache_params* p, const void* k_new, const void*
   cudaStream_t st = (cudaStream_t)stream;
   GRKV_TRY(clear_status((char*)ws, L, st));
   if (s.U == 0) return GRKV_OK;
-  const RowMove m{table_of(s), s.t, row16_of(s), count, (int*)((char*)ws + L.status)};
-  const size_t blocks = ((size_t)s.U * s.t * m.row16 + 255) / 256;
-  count_launches(1);
-  return cuda_rc(launch_kernel(false, 1, k_cache_append, dim3((unsigned)std::min<size_t>(blocks, 1 << 20)),
-                               256, 0, st, m, (const uint4*)k_new, (const uint4*)v_new, first_row,
-                               table, len, (uint4*)k_pages, (uint4*)v_pages));
+  const RowMove m{table_of(s), s.t, count, len, (int*)((char*)ws + L.status)};
+  return cuda_rc(launch_rows(s, k_cache_append<16>, k_cache_append<32>, st, m, (const uint4*)k_new,
+                             (const uint4*)v_new, first_row, table, (uint4*)k_pages,
+                             (uint4*)v_pages));
 }
 
 int grkv_cache_compact(const grkv_cache_params* p, const int32_t* idx, const int32_t* keep,
@@ -561,16 +662,15 @@ int grkv_cache_compact(const grkv_cache_params* p, const int32_t* idx, const int
   cudaStream_t st = (cudaStream_t)stream;
   GRKV_TRY(clear_status((char*)ws, L, st));
   if (s.U == 0) return GRKV_OK;
-  const RowMove m{table_of(s), s.t, row16_of(s), keep, (int*)((char*)ws + L.status)};
+  const RowMove m{table_of(s), s.t, keep, len_in, (int*)((char*)ws + L.status)};
+  uint4 *k = (uint4*)k_pages, *v = (uint4*)v_pages;
+  if (table_in != table_out)
+    return cuda_rc(launch_rows(s, k_cache_gather<16>, k_cache_gather<32>, st, m, idx, table_in,
+                               table_out, first, k, v));
   count_launches(1);
-  if (table_in == table_out)
-    return cuda_rc(launch_kernel(false, 1, k_cache_shift, dim3(s.U, 2, m.row16 / 4), kShiftThreads,
-                                 0, st, m, idx, table_in, len_in, first, (uint4*)k_pages,
-                                 (uint4*)v_pages));
-  const size_t blocks = ((size_t)s.U * s.t * m.row16 + 255) / 256;
-  return cuda_rc(launch_kernel(false, 1, k_cache_gather, dim3((unsigned)std::min<size_t>(blocks, 1 << 20)),
-                               256, 0, st, m, idx, table_in, len_in, table_out, first,
-                               (uint4*)k_pages, (uint4*)v_pages));
+  const int row16 = row16_of(s);
+  return cuda_rc(launch_kernel(false, 1, row16 == 16 ? k_cache_shift<16> : k_cache_shift<32>,
+                               dim3(s.U, 2, row16 / 4), kShiftThreads, 0, st, m, idx, table_in, first, k, v));
 }
 
 }  // extern "C"
