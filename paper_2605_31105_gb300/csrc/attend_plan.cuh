@@ -227,7 +227,7 @@ __device__ __forceinline__ Run plan_run_of(const AttendArgs& a, PlanSmem* ps, in
   __syncthreads();
   const int first_u = i0 / a.QB, first_qb = i0 - first_u * a.QB;
   I mine = 0;
-  int live = 0;   // items with rows
+  int live = 0, nt0 = 0;   // items with rows; the first one's tiles
   for (int i = i0, u = first_u, qb = first_qb, L = 0, T = 0; i < i1; ++i) {
     if (i == i0 || qb == 0) {
       L = unit_len(a, u);
@@ -235,6 +235,7 @@ __device__ __forceinline__ Run plan_run_of(const AttendArgs& a, PlanSmem* ps, in
       if (L != __ldg(a.len + u) || (a.qlen && T != __ldg(a.qlen + u))) ps->err = GRKV_ERR_INVALID_ARG;
     }
     const int nt = make_item(a, u, qb, L, T).nt;
+    if (i == i0) nt0 = nt;
     mine += nt;
     live += nt > 0;
     if (++qb == a.QB) {
@@ -274,7 +275,7 @@ __device__ __forceinline__ Run plan_run_of(const AttendArgs& a, PlanSmem* ps, in
     const bool first = at <= t0 && t0 < end, last = at < t1 && t1 <= end;
     if (c < sp.G && (first || last)) {
       for (int i = i0, u = first_u, qb = first_qb; i < i1; ++i) {
-        const int nt = make_item(a, u, qb).nt;
+        const int nt = i == i0 ? nt0 : make_item(a, u, qb).nt;
         if (nt > 0) {
           const I from = at + a.extra, to = from + nt;   // its tiles
           if (at <= t0 && t0 < to) {
@@ -362,6 +363,13 @@ __device__ __forceinline__ bool row_of(const AttendArgs& a, const Item& it, int 
   const int x = w * a.T + r - *h * a.T;
   *i = it.tok0 + x;
   return *h < a.g && x < it.ntok;
+}
+
+// Four columns (from 4 c4) of row r of a CTA's part.  Parts are stored a column group after the
+// other, rows inside, so that the tensor-core kernel's threads, a row each, write (and
+// k_attend_join's read) 16 bytes next to each other.
+__device__ __forceinline__ float4* part4(const AttendArgs& a, int slot, int c4, int r) {
+  return (float4*)a.po + ((size_t)slot * (kD / 4) + c4) * a.rows + r;
 }
 
 // What a partial result with reference m weighs against reference M.

@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_simt(AttendArgs a) {
       if (n + 1 < subs) ready(n + 1);
     }
     const bool whole = sg.whole();
-    const size_t part = (size_t)sg.slot(blockIdx.x) * a.rows;
+    const int slot = sg.slot(blockIdx.x);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int row = ty * 4 + r;
@@ -224,9 +224,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_simt(AttendArgs a) {
         store_row4((T*)a.out + o * kD + 64 + tx * 4, x1);
         if (a.lse && tx == 0) a.lse[o] = row_lse(m[r], l[r]);
       } else {
-        store_row4(a.po + (part + row) * kD + tx * 4, x0);
-        store_row4(a.po + (part + row) * kD + 64 + tx * 4, x1);
-        if (tx == 0) a.pml[part + row] = make_float2(m[r], l[r]);
+        *part4(a, slot, tx, row) = x0;
+        *part4(a, slot, 16 + tx, row) = x1;
+        if (tx == 0) a.pml[(size_t)slot * a.rows + row] = make_float2(m[r], l[r]);
       }
     }
     __syncthreads();   // the next segment overwrites the queries and both buffers
@@ -388,9 +388,9 @@ __global__ void __launch_bounds__(kFewThreads, R <= 8 ? 2 : 1) k_attend_few(Atte
                    make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
         if (a.lse && lane == 0) a.lse[dst] = row_lse(M, L);
       } else {
-        const size_t part = (size_t)sg.slot(blockIdx.x) * a.rows + r;
-        store_row4(a.po + part * kD + lane * 4, sum);
-        if (lane == 0) a.pml[part] = make_float2(M, L);
+        const int slot = sg.slot(blockIdx.x);
+        *part4(a, slot, lane, r) = sum;
+        if (lane == 0) a.pml[(size_t)slot * a.rows + r] = make_float2(M, L);
       }
     }
     __syncthreads();   // the next segment writes the same shared memory
@@ -405,113 +405,125 @@ __global__ void __launch_bounds__(kFewThreads, R <= 8 ? 2 : 1) k_attend_few(Atte
 }
 
 // Adds up the partial results of the split items, and writes the call's status.  Blocks
-// (c, y) take the rows of the item that starts in CTA c.  Few rows (kFewRows) may have many
-// parts: a block takes one row, whose parts go round the eight warps.  Else a warp takes
-// one row, or four where there are only two parts: eight loads of outputs are in flight.
+// (c, y) take the item that starts in CTA c, a thread four columns of a row (an element).  Items
+// of up to 16 rows may have many parts: the one block's threads go over them in groups of
+// one thread per element.  Else a thread has one element, or four where there are only two
+// parts: eight loads of outputs are in flight.
+constexpr int kJoinFewRows = 16;
 template <typename T, bool kFewRows>
-__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int G) {
+__global__ void __launch_bounds__(kFewRows ? 1024 : 256) k_attend_join(AttendArgs a, int G) {
   chain_wait();
-  __shared__ float4 sum_o[8][32];
-  __shared__ float sum_l[8];
-  const int c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (c == 0 && blockIdx.y == 0 && warp == 0) {
+  const int c = blockIdx.x, tid = threadIdx.x;
+  if (c == 0 && blockIdx.y == 0 && tid < 32) {
     int err = 0;
-    for (int x = lane; x < G; x += 32) err = min(err, a.rec[x].err);
+    for (int x = tid; x < G; x += 32) err = min(err, a.rec[x].err);
     err = __reduce_min_sync(0xffffffffu, err);
-    if (lane == 0) *a.status = err;
+    if (tid == 0) *a.status = err;
   }
   const AttendRec rec = a.rec[c];
-  const bool four = !kFewRows && rec.last == c + 1;
-  const int row0 = kFewRows ? blockIdx.y : four ? blockIdx.y * 32 + warp * 4 : blockIdx.y * 8 + warp;
-  if (rec.u < 0 || row0 >= a.rows) return;
+  if (rec.u < 0) return;
+  const int elems = a.rows * (kD / 4), parts = rec.last - c + 1;
   const Item it = make_item(a, rec.u, rec.qb);
-  const int per = a.T * a.g;
   // part 0 is in the CTA's second slot, the others in the first of the CTAs after it
-  auto at = [&](int x, int row) { return (size_t)(x == c ? 2 * c + 1 : 2 * x) * a.rows + row; };
-  auto store = [&](int row, float M, float l, float4 o) {
-    const int w = row / per;
+  auto slot = [&](int x) { return x == 0 ? 2 * c + 1 : 2 * (c + x); };
+  auto store = [&](int row, int c4, float M, float l, float4 o) {
+    const int per = a.T * a.g, w = row / per;
     int h, i;
     if (!row_of(a, it, w, row - w * per, &h, &i)) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const size_t dst = ((size_t)it.u * a.g + h) * a.t + i;
-    store_row4((T*)a.out + dst * kD + lane * 4,
-               make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-    if (a.lse && lane == 0) a.lse[dst] = row_lse(M, l);
+    store_row4((T*)a.out + dst * kD + c4 * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (a.lse && c4 == 0) a.lse[dst] = row_lse(M, l);
   };
-  if (four) {
+  auto add = [&](float f, float2 ml, float4 p, float* l, float4* o) {
+    *l += f * ml.y;
+    o->x = fmaf(f, p.x, o->x);
+    o->y = fmaf(f, p.y, o->y);
+    o->z = fmaf(f, p.z, o->z);
+    o->w = fmaf(f, p.w, o->w);
+  };
+  if (!kFewRows && parts == 2) {
     float2 ml[4][2];
     float4 p[4][2];
+    const int e0 = blockIdx.y * 1024 + tid;
+    if (blockIdx.y * 1024 >= elems) return;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        const size_t x = at(c + y, min(row0 + r, a.rows - 1));
-        ml[r][y] = a.pml[x];
-        p[r][y] = ((const float4*)(a.po + x * kD))[lane];
+        const int e = min(e0 + 256 * k, elems - 1), c4 = e / a.rows, row = e - c4 * a.rows;
+        ml[k][y] = a.pml[(size_t)slot(y) * a.rows + row];
+        p[k][y] = *part4(a, slot(y), c4, row);
       }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const float M = fmaxf(ml[r][0].x, ml[r][1].x);
-      const float f = weight_of(ml[r][0].x, M), g = weight_of(ml[r][1].x, M);
-      if (row0 + r < a.rows)
-        store(row0 + r, M, f * ml[r][0].y + g * ml[r][1].y,
-              make_float4(fmaf(f, p[r][0].x, g * p[r][1].x), fmaf(f, p[r][0].y, g * p[r][1].y),
-                          fmaf(f, p[r][0].z, g * p[r][1].z), fmaf(f, p[r][0].w, g * p[r][1].w)));
+    for (int k = 0; k < 4; ++k) {
+      const int e = e0 + 256 * k, c4 = e / a.rows;
+      const float M = fmaxf(ml[k][0].x, ml[k][1].x);
+      float l = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) add(weight_of(ml[k][y].x, M), ml[k][y], p[k][y], &l, &o);
+      if (e < elems) store(e - c4 * a.rows, c4, M, l, o);
     }
     return;
   }
-  const int x0 = c + (kFewRows ? warp : 0);
-  constexpr int kStep = kFewRows ? 8 : 1, kUnroll = kFewRows ? 4 : 8;
-  float M = -INFINITY;
-  for (int x = c + lane; x <= rec.last; x += 32) M = fmaxf(M, a.pml[at(x, row0)].x);
-#pragma unroll
-  for (int d = 16; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-  float l = 0.f;
+  const int groups = kFewRows ? 1024 / elems : 1;
+  const int e = kFewRows ? tid % elems : blockIdx.y * 256 + tid, grp = kFewRows ? tid / elems : 0;
+  if (!kFewRows && e >= elems) return;
+  const int c4 = e / a.rows, row = e - c4 * a.rows;
+  constexpr int kUnroll = 8;
+  float M = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int x = x0; x <= rec.last; x += kStep * kUnroll) {   // kUnroll parts to a round trip
+  for (int x = grp; grp < groups && x < parts; x += groups * kUnroll) {   // kUnroll parts to a trip
     float2 ml[kUnroll];
     float4 p[kUnroll];
 #pragma unroll
     for (int y = 0; y < kUnroll; ++y) {
-      const bool has = x + y * kStep <= rec.last;
-      const size_t z = at(has ? x + y * kStep : c, row0);
-      ml[y] = has ? a.pml[z] : make_float2(-INFINITY, 0.f);
-      p[y] = has ? ((const float4*)(a.po + z * kD))[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+      const int z = x + y * groups;
+      ml[y] = make_float2(-INFINITY, 0.f);
+      p[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (z >= parts) continue;
+      ml[y] = a.pml[(size_t)slot(z) * a.rows + row];
+      p[y] = *part4(a, slot(z), c4, row);
     }
+    float top = M;
 #pragma unroll
-    for (int y = 0; y < kUnroll; ++y) {
-      const float f = weight_of(ml[y].x, M);
-      l += f * ml[y].y;
-      o.x = fmaf(f, p[y].x, o.x);
-      o.y = fmaf(f, p[y].y, o.y);
-      o.z = fmaf(f, p[y].z, o.z);
-      o.w = fmaf(f, p[y].w, o.w);
-    }
+    for (int y = 0; y < kUnroll; ++y) top = fmaxf(top, ml[y].x);
+    const float keep = weight_of(M, top);
+    M = top;
+    l *= keep;
+    o = make_float4(o.x * keep, o.y * keep, o.z * keep, o.w * keep);
+#pragma unroll
+    for (int y = 0; y < kUnroll; ++y) add(weight_of(ml[y].x, M), ml[y], p[y], &l, &o);
   }
   if (kFewRows) {
-    sum_o[warp][lane] = o;
-    if (lane == 0) sum_l[warp] = l;
-    __syncthreads();   // the block has one row: all of its warps are here
-    if (warp > 0) return;
-#pragma unroll
-    for (int x = 1; x < 8; ++x) {
-      const float4 p = sum_o[x][lane];
-      l += sum_l[x];
-      o.x += p.x;
-      o.y += p.y;
-      o.z += p.z;
-      o.w += p.w;
+    __shared__ float4 sum_o[1024];
+    __shared__ float2 sum_ml[1024];
+    sum_o[tid] = o;
+    sum_ml[tid] = make_float2(M, l);
+    __syncthreads();
+    if (grp > 0) return;
+    float top = M;
+    for (int x = 1; x < groups; ++x) top = fmaxf(top, sum_ml[x * elems + e].x);
+    const float keep = weight_of(M, top);
+    M = top;
+    l *= keep;
+    o = make_float4(o.x * keep, o.y * keep, o.z * keep, o.w * keep);
+    for (int x = 1; x < groups; ++x) {
+      const float2 ml = sum_ml[x * elems + e];
+      add(weight_of(ml.x, M), ml, sum_o[x * elems + e], &l, &o);
     }
   }
-  store(row0, M, l, o);
+  store(row, c4, M, l, o);
 }
 
 template <typename T>
 cudaError_t launch_join(const AttendArgs& a, int G, cudaStream_t st) {
   count_launches(1);
-  if (a.rows <= 16)
-    return launch_kernel(true, 1, k_attend_join<T, true>, dim3(G, a.rows), 256, 0, st, a, G);
-  return launch_kernel(true, 1, k_attend_join<T, false>, dim3(G, (a.rows + 7) / 8), 256, 0, st, a, G);
+  if (a.rows <= kJoinFewRows)
+    return launch_kernel(true, 1, k_attend_join<T, true>, dim3(G), 1024, 0, st, a, G);
+  return launch_kernel(true, 1, k_attend_join<T, false>, dim3(G, (a.rows * (kD / 4) + 255) / 256), 256, 0,
+                       st, a, G);
 }
 
 template <typename... Args>

@@ -387,22 +387,35 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
       if (!wait(&bars->v_ok[B], ph)) return false;
       if (NQ == 2) {
         const bool more = t + 1 < tiles;
-        if (more && (!q_begin() || !wait(&bars->ring_full[2 * (1 - B)], B ? ph ^ 1 : ph))) return false;
-        if (!wait(&bars->p_full[0], B)) return false;
-        issue_o(0, 0, B);
-        if (v_left == 0) mma_commit_elect(&bars->o_done[0]);
-        if (more) {
-          issue_s(0, 0, 1 - B);
-          mma_commit_elect(&bars->s_full[0]);
-        }
-        if (!wait(&bars->p_full[1], B)) return false;
-        issue_o(1, 1, B);
-        if (v_left == 0) mma_commit_elect(&bars->o_done[1]);
-        if (more) {
-          issue_s(1, NQ - 1, 1 - B);
+        auto k_ready = [&]() { return wait(&bars->ring_full[2 * (1 - B)], B ? ph ^ 1 : ph); };
+        auto s_done = [&]() {
           mma_commit_elect(&bars->s_full[1]);
           mma_commit_elect(&bars->ring_empty[2 * (1 - B)]);
           q_end();
+        };
+        if (more && q_left > 0) {
+          if (!k_ready() || !wait(&bars->p_full[0], B)) return false;
+          issue_o(0, 0, B);
+          issue_s(0, 0, 1 - B);
+          mma_commit_elect(&bars->s_full[0]);
+          if (!wait(&bars->p_full[1], B)) return false;
+          issue_o(1, 1, B);
+          issue_s(1, NQ - 1, 1 - B);
+          s_done();
+        } else {   // the segment's last tile: its outputs do not wait for the next one's queries
+          if (!wait(&bars->p_full[0], B)) return false;
+          issue_o(0, 0, B);
+          mma_commit_elect(&bars->o_done[0]);
+          if (!wait(&bars->p_full[1], B)) return false;
+          issue_o(1, 1, B);
+          mma_commit_elect(&bars->o_done[1]);
+          if (more) {
+            if (!q_begin() || !k_ready()) return false;
+            issue_s(0, 0, 1 - B);
+            mma_commit_elect(&bars->s_full[0]);
+            issue_s(1, NQ - 1, 1 - B);
+            s_done();
+          }
         }
         mma_commit_elect(&bars->ring_empty[2 * B + 1]);
       } else {
@@ -595,23 +608,20 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
       if (!warp_live) continue;
       if (__any_sync(0xffffffffu, any_bad))
         add_bad(a, it, sg.off, sg.cnt, vis, bad, live, lane_addr + ocol);
-      const bool whole = sg.whole();
-      const float f = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
-      // rows of out and lse, or of the CTA's part; both counts fit 32 bits
-      const int dst = whole ? ((it.u * a.g + h) * a.t + i)
-                            : sg.slot(blockIdx.x) * a.rows + w * a.T * a.g + row;
-      int rows[4];
+      if (sg.whole()) {
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        const int dst = (it.u * a.g + h) * a.t + i;   // fits 32 bits
+        int rows[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        rows[j] = __shfl_sync(0xffffffffu, live ? dst : -1, 8 * j + (lane >> 2));
-      uint8_t* stage = sm + Lay::kOffStage + (warp - 4) * 2048;
+        for (int j = 0; j < 4; ++j)
+          rows[j] = __shfl_sync(0xffffffffu, live ? dst : -1, 8 * j + (lane >> 2));
+        uint8_t* stage = sm + Lay::kOffStage + (warp - 4) * 2048;
 #pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
-        float o[32];
-        tmem_ld32f(lane_addr + ocol + 32 * c, o);
-        tmem_wait32(o);
-        uint4 x[4];
-        if (whole) {
+        for (int c = 0; c < 4; ++c) {
+          float o[32];
+          tmem_ld32f(lane_addr + ocol + 32 * c, o);
+          tmem_wait32(o);
+          uint4 x[4];
 #pragma unroll
           for (int y = 0; y < 4; ++y)
             x[y] = make_uint4(pack_bf16(o[8 * y] * f, o[8 * y + 1] * f),
@@ -619,21 +629,22 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
                               pack_bf16(o[8 * y + 4] * f, o[8 * y + 5] * f),
                               pack_bf16(o[8 * y + 6] * f, o[8 * y + 7] * f));
           store_rows(stage, lane, x, rows, (uint8_t*)a.out + 64 * c, kD * 2);
-        } else {
-#pragma unroll
-          for (int hh = 0; hh < 2; ++hh) {
-#pragma unroll
-            for (int y = 0; y < 4; ++y)
-              x[y] = *(const uint4*)(o + 16 * hh + 4 * y);
-            store_rows(stage, lane, x, rows, (uint8_t*)a.po + 128 * c + 64 * hh, kD * 4);
-          }
         }
-      }
-      if (live) {
-        if (!whole)
-          a.pml[dst] = make_float2(ref, l);
-        else if (a.lse)
-          a.lse[dst] = row_lse(ref, l);
+        if (live && a.lse) a.lse[dst] = row_lse(ref, l);
+      } else {
+        const int slot = sg.slot(blockIdx.x), r = w * a.T * a.g + row;
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          float o[32];
+          tmem_ld32f(lane_addr + ocol + 32 * c, o);
+          tmem_wait32(o);
+          float4* p = part4(a, slot, 8 * c, r);
+#pragma unroll
+          for (int y = 0; y < 8; ++y)
+            if (live) p[(size_t)y * a.rows] = make_float4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
+          __syncwarp();   // the next TMEM load is the whole warp's
+        }
+        if (live) a.pml[(size_t)slot * a.rows + r] = make_float2(ref, l);
       }
       tc_fence_before();
     }
