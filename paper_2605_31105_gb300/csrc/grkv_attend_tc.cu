@@ -294,11 +294,23 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
           tma_load_3d(dst + kTileBytes / 2, &tmQ, &bars->q_full[qb], 64, i, it.u * a.g, keep);
         }
       }
-      for (int k = 0; ok && k < sg.cnt; ++k) {
+      // the page of this lane in tile k of the segment, or -1; the next tile's is asked for before
+      // this one's slots are waited for
+      auto look_up = [&](int k, bool* has) {
         const int c = it.tile(sg.off + k) * per_tile + lane;
-        const bool mine =
-            lane < per_tile && c < a.cols && it.wanted(c << a.shift, (c + 1) << a.shift);
-        const int page = mine ? page_of(a, it.u, c, &err) : 0;
+        *has = lane < per_tile && c < a.cols && it.wanted(c << a.shift, (c + 1) << a.shift);
+        return *has ? __ldg(a.table + (size_t)it.u * a.cols + c) : 0;
+      };
+      bool has, mine;
+      int entry = look_up(0, &has);
+      for (int k = 0; ok && k < sg.cnt; ++k) {
+        mine = has;
+        int page = entry;
+        if (k + 1 < sg.cnt) entry = look_up(k + 1, &has);
+        if (mine && (unsigned)page >= (unsigned)a.P) {   // an entry outside the pool: page 0
+          err = GRKV_ERR_INVALID_ARG;
+          page = 0;
+        }
         const uint32_t n = __popc(__ballot_sync(0xffffffffu, mine));
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
