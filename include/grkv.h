@@ -294,7 +294,7 @@ typedef struct {
   int32_t units;      /* U >= 0                                                       */
   int32_t group;      /* g: query heads per KV head, 1..64                            */
   int32_t d;          /* head dimension; 128 only                                     */
-  int32_t pages;      /* P >= 1: pages of the pool                                    */
+  int32_t pages;      /* P: pages of the pool, 1..2^30                                */
   int32_t page;       /* slots per page: 16, 32, 64 or 128                            */
   int32_t max_pages;  /* columns of a table row; max_pages page <= 2^28               */
   int32_t tokens;     /* t >= 1: rows per unit of q, new rows or idx (1); U g t <= 2^28 */
@@ -335,12 +335,12 @@ int grkv_cache_trim(const grkv_cache_params* p, int32_t* table, const int32_t* l
 
 /* Writes new rows to the last count[u] (NULL: t) of the len[u] slots of every unit: len is
  * the length with the new rows.  Row i of unit u is row u t + i of k_new, v_new
- * [U][t][d], or, with first_row, row first_row[u] + i (the packed outputs of
- * grkv_compress_ragged). */
+ * [U][t][d], or, with first_row, row first_row[u] + i of k_new, v_new [new_rows][d] (the
+ * packed outputs of grkv_compress_ragged); new_rows is not read without first_row. */
 int grkv_cache_append(const grkv_cache_params* p, const void* k_new, const void* v_new,
-                      const int64_t* first_row, const int32_t* count, const int32_t* table,
-                      const int32_t* len, void* k_pages, void* v_pages, void* ws, size_t ws_bytes,
-                      void* stream);
+                      const int64_t* first_row, int64_t new_rows, const int32_t* count,
+                      const int32_t* table, const int32_t* len, void* k_pages, void* v_pages,
+                      void* ws, size_t ws_bytes, void* stream);
 
 /* Moves kept rows together: slot first[u] + i (first NULL: 0) of table_out takes slot
  * idx[u][i] of table_in, i < keep[u] (NULL: t); idx [U][t], slots below len_in[u].

@@ -117,7 +117,8 @@ def load():
     lib.grkv_cache_params_init.restype = None
     lib.grkv_cache_workspace_size.argtypes = [_cp, ctypes.POINTER(_sz)]
     for name, lead in (("grkv_cache_reserve", [_vp] * 6), ("grkv_cache_trim", [_vp] * 3),
-                       ("grkv_cache_fork", [_i] + [_vp] * 6), ("grkv_cache_append", [_vp] * 8),
+                       ("grkv_cache_fork", [_i] + [_vp] * 6),
+                       ("grkv_cache_append", [_vp] * 3 + [ctypes.c_int64] + [_vp] * 5),
                        ("grkv_cache_compact", [_vp] * 8), ("grkv_attend", [_vp] * 8),
                        ("grkv_attend_tree", [_vp] * 9)):
         getattr(lib, name).argtypes = [_cp, *lead, _vp, _sz, _vp]
@@ -269,11 +270,11 @@ def cache_params(units, group, pages, page, max_pages, **kw) -> grkv_cache_param
 def _fault(name, t, dtype, dev, need):
     if t.dtype != dtype:
         return f"{name} is {t.dtype}, the call takes {dtype}"
-    if t.get_device() != dev:
-        return f"{name} is on {t.device}, the workspace on device {dev}"
     if not t.is_contiguous():
         return f"{name} is not contiguous"
-    return f"{name} holds {t.numel()} elements, the call takes {need}"
+    if t.numel() < need:
+        return f"{name} holds {t.numel()} elements, the call takes {need}"
+    return f"{name} is on {t.device}, the workspace on device {dev}"
 
 
 def _addresses(p, ws, ws_bytes, stream, rows, words, lse=(), first_row=()):
@@ -300,9 +301,9 @@ def _addresses(p, ws, ws_bytes, stream, rows, words, lse=(), first_row=()):
         for name, t, need in group:
             if t is not None and not isinstance(t, int):
                 at = t.get_device()
-                if (t.dtype is not want or (dev is not None and at != dev) or t.numel() < need
-                        or not t.is_contiguous()):
-                    raise ValueError(_fault(name, t, want, at if dev is None else dev, need))
+                if (t.dtype is not want or at < 0 or (dev is not None and at != dev)
+                        or t.numel() < need or not t.is_contiguous()):
+                    raise ValueError(_fault(name, t, want, dev, need))
                 t = t.data_ptr()
             out.append(t)
     if stream is None:
@@ -363,15 +364,20 @@ def grkv_cache_trim(p, table, lens, refs, ws, ws_bytes=None, stream=None, check=
 
 def grkv_cache_append(p, k_new, v_new, k_pages, v_pages, table, lens, ws, count=None,
                       first_row=None, ws_bytes=None, stream=None, check=True):
-    """New rows to the last `count` of the `lens` slots of every unit."""
+    """New rows to the last `count` of the `lens` slots of every unit.  With first_row the rows
+    are packed: unit u's start at row first_row[u] of k_new and v_new."""
     u, n = p.units, p.pages * p.page * p.d
-    need = 0 if first_row is not None else u * p.tokens * p.d
+    need, new_rows = u * p.tokens * p.d, 0
+    if first_row is not None:   # rows of both arrays that the packed form may name
+        new_rows = u * p.tokens if isinstance(k_new, int) else min(
+            k_new.numel(), v_new.numel()) // p.d
+        need = new_rows * p.d
     (kn, vn, k, v, t, le, c, f), w, nb, st = _addresses(
         p, ws, ws_bytes, stream, (("k_new", k_new, need), ("v_new", v_new, need),
                                   ("k_pages", k_pages, n), ("v_pages", v_pages, n)),
         (("table", table, u * p.max_pages), ("lens", lens, u), ("count", count, u)),
         first_row=(("first_row", first_row, u),))
-    rc = load().grkv_cache_append(ctypes.byref(p), kn, vn, f, c, t, le, k, v, w, nb, st)
+    rc = load().grkv_cache_append(ctypes.byref(p), kn, vn, f, new_rows, c, t, le, k, v, w, nb, st)
     return _check(rc, "grkv_cache_append", check)
 
 

@@ -48,7 +48,8 @@ int make_cache_shape(const grkv_cache_params* p, CacheShape* s) {
   if (p->d != kD || p->group > kMaxCacheGroup) return GRKV_ERR_UNSUPPORTED;
   if (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128)
     return GRKV_ERR_UNSUPPORTED;
-  // slots of a unit, entries of a table and rows of a call stay within 32-bit integers
+  // pages, slots of a unit, entries of a table and rows of a call stay within 32-bit integers
+  if (p->pages > 1 << 30) return GRKV_ERR_UNSUPPORTED;
   if ((int64_t)p->max_pages * p->page > (int64_t)1 << 28) return GRKV_ERR_UNSUPPORTED;
   if (p->tokens > 1 << 28 || (int64_t)p->units * p->max_pages > (int64_t)1 << 30 ||
       (int64_t)p->units * p->group * p->tokens > (int64_t)1 << 28)
@@ -407,16 +408,17 @@ __device__ __forceinline__ void move_block(const RowMove& m, const uint4* k_in, 
 template <int kRow16>
 __global__ void __launch_bounds__(kMoveThreads)
     k_cache_append(RowMove m, const uint4* __restrict__ k_new, const uint4* __restrict__ v_new,
-                   const int64_t* __restrict__ first, const int32_t* __restrict__ table, uint4* k,
-                   uint4* v) {
+                   const int64_t* __restrict__ first, long long new_rows,
+                   const int32_t* __restrict__ table, uint4* k, uint4* v) {
   move_block<kRow16>(m, k_new, v_new, k, v, [&](int u, int i, int n, int len, long long* from,
                                                 long long* to) {
     const int slot = len - n + i;
-    if (slot < 0) {
+    const long long f = first ? first[u] : (long long)u * m.t;
+    if (slot < 0 || f < 0 || f > new_rows - 1 - i) {
       set_status(m.status, GRKV_ERR_INVALID_ARG);
       return false;
     }
-    *from = first ? first[u] + i : (long long)u * m.t + i;
+    *from = f + i;
     *to = pool_row(m.tb, table, u, slot, m.status);
     return *to >= 0;
   });
@@ -625,9 +627,9 @@ int grkv_cache_reserve(const grkv_cache_params* p, int32_t* table, const int32_t
 }
 
 int grkv_cache_append(const grkv_cache_params* p, const void* k_new, const void* v_new,
-                      const int64_t* first_row, const int32_t* count, const int32_t* table,
-                      const int32_t* len, void* k_pages, void* v_pages, void* ws, size_t ws_bytes,
-                      void* stream) {
+                      const int64_t* first_row, int64_t new_rows, const int32_t* count,
+                      const int32_t* table, const int32_t* len, void* k_pages, void* v_pages,
+                      void* ws, size_t ws_bytes, void* stream) {
   CacheShape s;
   CacheWs L;
   GRKV_TRY(begin(p, ws, ws_bytes, &s, &L));
@@ -636,13 +638,15 @@ int grkv_cache_append(const grkv_cache_params* p, const void* k_new, const void*
     GRKV_TRY(check_ptrs({table, len}, 4));
   }
   GRKV_TRY(check_optional(first_row, 8));
+  if (first_row && new_rows < 0) return GRKV_ERR_INVALID_ARG;
   GRKV_TRY(check_optional(count, 4));
   cudaStream_t st = (cudaStream_t)stream;
   GRKV_TRY(clear_status((char*)ws, L, st));
   if (s.U == 0) return GRKV_OK;
   const RowMove m{table_of(s), s.t, count, len, (int*)((char*)ws + L.status)};
   return cuda_rc(launch_rows(s, k_cache_append<16>, k_cache_append<32>, st, m, (const uint4*)k_new,
-                             (const uint4*)v_new, first_row, table, (uint4*)k_pages,
+                             (const uint4*)v_new, first_row,
+                             first_row ? (long long)new_rows : (long long)s.U * s.t, table, (uint4*)k_pages,
                              (uint4*)v_pages));
 }
 

@@ -25,7 +25,7 @@ def test_defaults(lib):  # noqa: F811
     (dict(n_sink=-1), -1), (dict(scale=-1.0), -1), (dict(scale=float("inf")), -1),
     (dict(scale=float("nan")), -1), (dict(dtype=5), -1), (dict(flags=b.GRKV_DETERMINISTIC), -1),
     (dict(d=64), -2), (dict(group=65), -2), (dict(page=48), -2), (dict(page=256), -2),
-    (dict(max_pages=1 << 27), -2), (dict(tokens=(1 << 28) + 1), -2),
+    (dict(max_pages=1 << 27), -2), (dict(pages=(1 << 30) + 1), -2), (dict(tokens=(1 << 28) + 1), -2),
     (dict(units=1 << 20, tokens=1 << 10), -2), (dict(units=1 << 26, max_pages=17), -2)])
 def test_parameters(lib, kw, code):  # noqa: F811
     p = params()
@@ -97,11 +97,15 @@ def test_tensors_are_checked_by_the_binding(lib):  # noqa: F811
         with pytest.raises(ValueError, match=word):
             b.grkv_attend(p, *a, FAKE, **{**kw, **k})
 
-    refused("q is torch.float32", q.float(), pool, pool, table, lens, out)
-    refused("lens is torch.int64", q, pool, pool, table, lens.long(), out)
-    refused("k_pages is not contiguous", q, pool.transpose(0, 1), pool, table, lens, out)
-    refused("v_pages holds", q, pool, pool[:99], table, lens, out)
-    refused("table holds", q, pool, pool, table[:7], lens, out)
-    refused("lse is torch.bfloat16", q, pool, pool, table, lens, out, lse=out)
+    f = FAKE                       # the tensors that are not looked at
+    refused("q is torch.float32", q.float(), f, f, f, f, f)
+    refused("lens is torch.int64", f, f, f, f, lens.long(), f)
+    refused("k_pages is not contiguous", f, pool.transpose(0, 1), f, f, f, f)
+    refused("v_pages holds", f, f, pool[:99], f, f, f)
+    refused("table holds", f, f, f, table[:7], f, f)
+    refused("lse is torch.bfloat16", f, f, f, f, f, f, lse=out)
+    refused("q is on cpu", q, f, f, f, f, f)
+    assert b.load().grkv_cache_append(p, FAKE, FAKE, FAKE, -1, None, FAKE, FAKE, FAKE, FAKE, FAKE,
+                                      kw["ws_bytes"], None) == b.GRKV_ERR_INVALID_ARG
     with pytest.raises(ValueError, match="not on the current CUDA device"):
         b.grkv_attend(p, q, pool, pool, table, lens, out, torch.zeros(kw["ws_bytes"], dtype=torch.uint8))

@@ -248,6 +248,17 @@ def test_faults_are_reported_and_nothing_else_moves(grkv_lib):
                             count=R.int_dev(count))
         d.ok(inv)
         d.same()
+    # append of packed rows that are not there
+    for first in (-1, 3, 2 ** 62, -2 ** 63):
+        d = new()
+        b.grkv_cache_append(d.p, rows, rows, d.k, d.v, d.table, d.lens, d.ws,
+                            count=R.int_dev([2, 0]),
+                            first_row=torch.tensor([first, 0], dtype=torch.int64, device="cuda"))
+        d.ok(inv)
+        if first == 3:                          # the first of two rows is the last there is
+            at = R.at(d.c.table, 0, 38, page)
+            d.c.k[at] = d.c.v[at] = 1
+        d.same()
     # compact: sources out of range, or before their place
     for idx, first in (([[40, 0]], 0), ([[-1, 0]], 0), ([[4, 5]], 30), ([[5, 6]], -1),
                        ([[5, 6]], big)):
@@ -373,3 +384,89 @@ def test_compressed_caches_are_decoded_with_drafts(grkv_lib):
     attend(3)
     held = (table >= 0).sum().item()
     assert refs.sum().item() == held == sum(R.pages_of(int(x), page) for x in lens.tolist())
+
+
+def test_no_units(grkv_lib):
+    p = b.cache_params(0, 1, 8, 16, 4)
+    ws = torch.full((b.grkv_cache_workspace_size(p),), 0xFF, dtype=torch.uint8, device="cuda")
+    e = torch.empty(0, dtype=torch.int32, device="cuda")
+    rows = torch.empty(0, dtype=torch.bfloat16, device="cuda")
+    pool = torch.zeros(8, 16, D, dtype=torch.bfloat16, device="cuda")
+    refs = torch.zeros(8, dtype=torch.int32, device="cuda")
+    for call in (lambda: b.grkv_cache_trim(p, e, e, refs, ws),
+                 lambda: b.grkv_cache_reserve(p, e, e, e, refs, pool, pool, ws),
+                 lambda: b.grkv_cache_append(p, rows, rows, pool, pool, e, e, ws),
+                 lambda: b.grkv_cache_compact(p, e, pool, pool, e, e, e, ws),
+                 lambda: b.grkv_cache_fork(p, e, e, e, torch.empty_like(e), torch.empty_like(e),
+                                           refs, ws)):
+        ws[:4] = 0xFF
+        call()
+        assert b.grkv_status(ws) == b.GRKV_OK
+
+
+@pytest.mark.parametrize("units,cols", [(7, 5), (300, 40)])
+def test_fork_and_trim_of_small_and_large_tables(grkv_lib, units, cols):
+    """One block that writes the status itself, and many that add to a cleared word."""
+    rng = np.random.default_rng(units)
+    page = 16
+    c = R.Cache([int(x) for x in rng.integers(0, (cols - 1) * page, units)], page, "bf16", 3)
+    c.table = np.concatenate([c.table, np.full((units, cols - c.cols), -1, np.int32)], 1)
+    c.cols = cols
+    d = Dev(c)
+    src = [int(x) for x in rng.integers(-1, units, units)]
+    t2, l2 = R.fork(src, c.table, c.lens, c.refs, cols, page)
+    table, lens = torch.full_like(d.table, 5), torch.full_like(d.lens, 5)
+    b.grkv_cache_fork(d.p, R.int_dev(src), d.table, d.lens, table, lens, d.refs, d.ws)
+    d.ok()
+    assert np.array_equal(table.cpu().numpy(), t2) and np.array_equal(lens.cpu().numpy(), l2)
+    d.same()
+    half = [int(x) // 2 for x in l2]
+    b.grkv_cache_trim(d.p, table, R.int_dev(half), d.refs, d.ws)
+    d.ok()
+    R.trim(t2, half, c.refs, page)
+    assert np.array_equal(table.cpu().numpy(), t2)
+    d.same()
+    bad = R.int_dev([units] + src[1:])
+    table.fill_(-1)
+    b.grkv_cache_fork(d.p, bad, d.table, d.lens, table, lens, d.refs, d.ws)
+    d.ok(b.GRKV_ERR_INVALID_ARG)
+    b.grkv_cache_trim(d.p, table, torch.zeros_like(lens), d.refs, d.ws)
+    d.ok()
+
+
+def test_pools_beyond_32_bit_offsets(grkv_lib):
+    """Pages whose elements lie past 2^31: every call that reads or writes them."""
+    pages, page, n, t = 140000, 128, 300, 3         # 2.3e9 elements a pool
+    pool = [torch.empty(pages, page, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    far = [139999, 7, 139000, 138000]
+    table = R.int_dev([far])
+    lens, refs = R.int_dev([n]), torch.ones(pages, dtype=torch.int32, device="cuda")
+    p = b.cache_params(1, 2, pages, page, 4, tokens=n)
+    ws = torch.empty(b.grkv_cache_workspace_size(p), dtype=torch.uint8, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=gen).bfloat16()
+    kn, vn = rnd(1, n, D), rnd(1, n, D)
+    b.grkv_cache_append(p, kn, vn, *pool, table, lens, ws)
+    assert b.grkv_status(ws) == b.GRKV_OK
+    got = torch.cat([pool[0][x] for x in far[:3]])[:n]
+    assert torch.equal(got, kn[0])
+    for flags in (0, b.GRKV_FORCE_SIMT):
+        pq = b.cache_params(1, 2, pages, page, 4, tokens=t, flags=flags)
+        q, out = rnd(1, 2, t, D), rnd(1, 2, t, D)
+        b.grkv_attend(pq, q, *pool, table, lens, out, ws)
+        assert b.grkv_status(ws) == b.GRKV_OK
+        o, _, mass, err = R.attend_unit(q[0].double().cpu().numpy(), kn[0].double().cpu().numpy(),
+                                        vn[0].double().cpu().numpy(), t, 0, 4)
+        tol = (2 * err + 2.0 ** -13 + 2.0 ** -8)[..., None] * mass + 2.0 ** -8 * np.abs(o)
+        assert (np.abs(out[0].double().cpu().numpy() - o) <= tol).all()
+    pc = b.cache_params(1, 2, pages, page, 4, tokens=2)
+    b.grkv_cache_compact(pc, R.int_dev([[5, 299]]), *pool, table, lens, table, ws,
+                         first=R.int_dev([2]))
+    assert b.grkv_status(ws) == b.GRKV_OK
+    assert torch.equal(pool[1][far[0], 2:4], vn[0, [5, 299]])
+    refs[:139998] = 2                               # two free pages, at the end
+    refs[139998:] = 0
+    b.grkv_cache_reserve(pc, table, R.int_dev([130]), R.int_dev([140]), refs, *pool, ws)
+    assert b.grkv_status(ws) == b.GRKV_OK
+    assert table[0, 1].item() == 139998
+    assert torch.equal(pool[0][139998, :2], kn[0, 128:130])
