@@ -267,9 +267,33 @@ def cache_params(units, group, pages, page, max_pages, **kw) -> grkv_cache_param
     return p
 
 
-def _fault(name, t, dtype, dev, need):
-    if t.dtype != dtype:
-        return f"{name} is {t.dtype}, the call takes {dtype}"
+# The tensors of the calls, in the order of _addresses' arguments, each with its kind: r for row
+# data of the call's type, i for 32-bit integers, l for 64-bit ones, f for fp32.
+_CALLS = {
+    "attend": "q:r k_pages:r v_pages:r out:r table:i lens:i q_lens:i lse:f",
+    "attend_tree": "q:r k_pages:r v_pages:r out:r table:i lens:i q_lens:i parent:i lse:f",
+    "reserve": "k_pages:r v_pages:r table:i lens:i want:i refs:i",
+    "fork": "src:i table_in:i lens_in:i table_out:i lens_out:i refs:i",
+    "trim": "table:i lens:i refs:i",
+    "append": "k_new:r v_new:r k_pages:r v_pages:r table:i lens:i count:i first_row:l",
+    "compact": "k_pages:r v_pages:r idx:i table_in:i lens_in:i table_out:i keep:i first:i",
+}
+_dtypes = {}   # (call, p.dtype) -> the tensors' types
+
+
+def _types_of(call, dtype):
+    import torch
+    kinds = {"r": torch.bfloat16 if dtype == GRKV_BF16 else torch.float32, "i": torch.int32,
+             "l": torch.int64, "f": torch.float32}
+    types = tuple(kinds[x.split(":")[1]] for x in _CALLS[call].split())
+    _dtypes[call, dtype] = types
+    return types
+
+
+def _fault(call, at, t, want, dev, need):
+    name = _CALLS[call].split()[at].split(":")[0]
+    if t.dtype != want:
+        return f"{name} is {t.dtype}, the call takes {want}"
     if not t.is_contiguous():
         return f"{name} is not contiguous"
     if t.numel() < need:
@@ -277,13 +301,13 @@ def _fault(name, t, dtype, dev, need):
     return f"{name} is on {t.device}, the workspace on device {dev}"
 
 
-def _addresses(p, ws, ws_bytes, stream, rows, words, lse=(), first_row=()):
+def _addresses(call, p, ws, ws_bytes, stream, tensors, needs):
     """The addresses of a cache call's tensors, the workspace's address and bytes, and the
-    stream.  Tensors are checked: row data of the call's type, 32-bit integer arrays (fp32 for lse,
-    64 bits for first_row), contiguous, on the current device like the workspace, as large as the call reads
-    or writes.  Addresses given as ints pass as they are, None where the call allows it."""
+    stream.  Tensors are checked: types, contiguous, on the current device like the workspace, as
+    large as the call reads or writes.  Addresses given as ints pass as they are, None where the
+    call allows it.  (A call's checks are most of its time on the host: 4 us for 8 tensors.)"""
     import torch
-    if isinstance(ws, int):
+    if type(ws) is int:
         dev = None
     else:
         dev = ws.get_device()
@@ -294,21 +318,20 @@ def _addresses(p, ws, ws_bytes, stream, rows, words, lse=(), first_row=()):
         if ws_bytes is None:
             ws_bytes = ws.numel() * ws.element_size()
         ws = ws.data_ptr()
-    row = torch.bfloat16 if p.dtype == GRKV_BF16 else torch.float32
+    dtype = p.dtype
+    types = _dtypes.get((call, dtype)) or _types_of(call, dtype)
     out = []
-    for want, group in ((row, rows), (torch.int32, words), (torch.float32, lse),
-                        (torch.int64, first_row)):
-        for name, t, need in group:
-            if t is not None and not isinstance(t, int):
-                at = t.get_device()
-                if (t.dtype is not want or at < 0 or (dev is not None and at != dev)
-                        or t.numel() < need or not t.is_contiguous()):
-                    raise ValueError(_fault(name, t, want, dev, need))
-                t = t.data_ptr()
-            out.append(t)
+    for t, want, need in zip(tensors, types, needs):
+        if t is not None and type(t) is not int:
+            at = t.get_device()
+            if (t.dtype is not want or at < 0 or (at != dev and dev is not None)
+                    or t.numel() < need or not t.is_contiguous()):
+                raise ValueError(_fault(call, len(out), t, want, dev, need))
+            t = t.data_ptr()
+        out.append(t)
     if stream is None:
         stream = _raw_stream(torch.cuda.current_device() if dev is None else dev)
-    elif not isinstance(stream, int):
+    elif type(stream) is not int:
         stream = stream.cuda_stream
     return out, ws, ws_bytes, stream
 
@@ -330,12 +353,12 @@ def grkv_cache_workspace_size(p: grkv_cache_params) -> int:
 def grkv_cache_reserve(p, table, lens, want, refs, k_pages, v_pages, ws, ws_bytes=None,
                        stream=None, check=True):
     """Own pages for slots [lens, want) of every unit."""
-    u, n = p.units, p.pages * p.page * p.d
+    u, pages = p.units, p.pages
+    n = pages * p.page * p.d
     (k, v, t, le, wa, r), w, nb, st = _addresses(
-        p, ws, ws_bytes, stream, (("k_pages", k_pages, n), ("v_pages", v_pages, n)),
-        (("table", table, u * p.max_pages), ("lens", lens, u), ("want", want, u),
-         ("refs", refs, p.pages)))
-    rc = load().grkv_cache_reserve(ctypes.byref(p), t, le, wa, r, k, v, w, nb, st)
+        "reserve", p, ws, ws_bytes, stream, (k_pages, v_pages, table, lens, want, refs),
+        (n, n, u * p.max_pages, u, u, pages))
+    rc = load().grkv_cache_reserve(p, t, le, wa, r, k, v, w, nb, st)
     return _check(rc, "grkv_cache_reserve", check)
 
 
@@ -346,19 +369,18 @@ def grkv_cache_fork(p, src, table_in, lens_in, table_out, lens_out, refs, ws, un
         units_in = lens_in.numel()
     u, m = p.units, p.max_pages
     (s, ti, li, to, lo, r), w, nb, st = _addresses(
-        p, ws, ws_bytes, stream, (),
-        (("src", src, u), ("table_in", table_in, units_in * m), ("lens_in", lens_in, units_in),
-         ("table_out", table_out, u * m), ("lens_out", lens_out, u), ("refs", refs, p.pages)))
-    rc = load().grkv_cache_fork(ctypes.byref(p), units_in, s, ti, li, to, lo, r, w, nb, st)
+        "fork", p, ws, ws_bytes, stream, (src, table_in, lens_in, table_out, lens_out, refs),
+        (u, units_in * m, units_in, u * m, u, p.pages))
+    rc = load().grkv_cache_fork(p, units_in, s, ti, li, to, lo, r, w, nb, st)
     return _check(rc, "grkv_cache_fork", check)
 
 
 def grkv_cache_trim(p, table, lens, refs, ws, ws_bytes=None, stream=None, check=True):
     """Gives back the pages behind lens."""
-    (t, le, r), w, nb, st = _addresses(
-        p, ws, ws_bytes, stream, (),
-        (("table", table, p.units * p.max_pages), ("lens", lens, p.units), ("refs", refs, p.pages)))
-    rc = load().grkv_cache_trim(ctypes.byref(p), t, le, r, w, nb, st)
+    u = p.units
+    (t, le, r), w, nb, st = _addresses("trim", p, ws, ws_bytes, stream, (table, lens, refs),
+                                       (u * p.max_pages, u, p.pages))
+    rc = load().grkv_cache_trim(p, t, le, r, w, nb, st)
     return _check(rc, "grkv_cache_trim", check)
 
 
@@ -366,62 +388,55 @@ def grkv_cache_append(p, k_new, v_new, k_pages, v_pages, table, lens, ws, count=
                       first_row=None, ws_bytes=None, stream=None, check=True):
     """New rows to the last `count` of the `lens` slots of every unit.  With first_row the rows
     are packed: unit u's start at row first_row[u] of k_new and v_new."""
-    u, n = p.units, p.pages * p.page * p.d
-    need, new_rows = u * p.tokens * p.d, 0
+    u, d = p.units, p.d
+    n, need, new_rows = p.pages * p.page * d, u * p.tokens * d, 0
     if first_row is not None:   # rows of both arrays that the packed form may name
         new_rows = u * p.tokens if isinstance(k_new, int) else min(
-            k_new.numel(), v_new.numel()) // p.d
-        need = new_rows * p.d
+            k_new.numel(), v_new.numel()) // d
+        need = new_rows * d
     (kn, vn, k, v, t, le, c, f), w, nb, st = _addresses(
-        p, ws, ws_bytes, stream, (("k_new", k_new, need), ("v_new", v_new, need),
-                                  ("k_pages", k_pages, n), ("v_pages", v_pages, n)),
-        (("table", table, u * p.max_pages), ("lens", lens, u), ("count", count, u)),
-        first_row=(("first_row", first_row, u),))
-    rc = load().grkv_cache_append(ctypes.byref(p), kn, vn, f, new_rows, c, t, le, k, v, w, nb, st)
+        "append", p, ws, ws_bytes, stream,
+        (k_new, v_new, k_pages, v_pages, table, lens, count, first_row),
+        (need, need, n, n, u * p.max_pages, u, u, u))
+    rc = load().grkv_cache_append(p, kn, vn, f, new_rows, c, t, le, k, v, w, nb, st)
     return _check(rc, "grkv_cache_append", check)
 
 
 def grkv_cache_compact(p, idx, k_pages, v_pages, table_in, lens_in, table_out, ws, keep=None,
                        first=None, ws_bytes=None, stream=None, check=True):
     """Slot first + i of table_out takes slot idx[u][i] of table_in."""
-    u, n = p.units, p.pages * p.page * p.d
+    u = p.units
+    n, m = p.pages * p.page * p.d, u * p.max_pages
     (k, v, i, ti, li, to, ke, f), w, nb, st = _addresses(
-        p, ws, ws_bytes, stream, (("k_pages", k_pages, n), ("v_pages", v_pages, n)),
-        (("idx", idx, u * p.tokens), ("table_in", table_in, u * p.max_pages),
-         ("lens_in", lens_in, u), ("table_out", table_out, u * p.max_pages), ("keep", keep, u),
-         ("first", first, u)))
-    rc = load().grkv_cache_compact(ctypes.byref(p), i, ke, f, ti, li, to, k, v, w, nb, st)
+        "compact", p, ws, ws_bytes, stream,
+        (k_pages, v_pages, idx, table_in, lens_in, table_out, keep, first),
+        (n, n, u * p.tokens, m, u, m, u, u))
+    rc = load().grkv_cache_compact(p, i, ke, f, ti, li, to, k, v, w, nb, st)
     return _check(rc, "grkv_cache_compact", check)
-
-
-def _attend(fn, p, q, k_pages, v_pages, table, lens, q_lens, parent, out, lse, ws, ws_bytes, stream):
-    u, n = p.units, p.pages * p.page * p.d
-    rows = u * p.group * p.tokens
-    words = [("table", table, u * p.max_pages), ("lens", lens, u), ("q_lens", q_lens, u)]
-    if parent is not None:
-        words.append(("parent", parent, u * p.tokens))
-    (q, k, v, o, *rest, ls), w, nb, st = _addresses(
-        p, ws, ws_bytes, stream,
-        (("q", q, rows * p.d), ("k_pages", k_pages, n), ("v_pages", v_pages, n),
-         ("out", out, rows * p.d)), words, (("lse", lse, rows),))
-    return fn(ctypes.byref(p), q, k, v, *rest, o, ls, w, nb, st)
 
 
 def grkv_attend(p, q, k_pages, v_pages, table, lens, out, ws, q_lens=None, lse=None,
                 ws_bytes=None, stream=None, check=True):
     """Attention of the last q_lens slots of every unit over its pages."""
-    rc = _attend(load().grkv_attend, p, q, k_pages, v_pages, table, lens, q_lens, None, out, lse,
-                 ws, ws_bytes, stream)
+    u, d = p.units, p.d
+    n, rows = p.pages * p.page * d, u * p.group * p.tokens
+    (q, k, v, o, t, le, ql, ls), w, nb, st = _addresses(
+        "attend", p, ws, ws_bytes, stream, (q, k_pages, v_pages, out, table, lens, q_lens, lse),
+        (rows * d, n, n, rows * d, u * p.max_pages, u, u, rows))
+    rc = load().grkv_attend(p, q, k, v, t, le, ql, o, ls, w, nb, st)
     return _check(rc, "grkv_attend", check)
 
 
 def grkv_attend_tree(p, q, k_pages, v_pages, table, lens, parent, out, ws, q_lens=None, lse=None,
                      ws_bytes=None, stream=None, check=True):
     """grkv_attend for trees of drafted tokens: parent [U][t], -1 for roots."""
-    if parent is None:
-        parent = 0
-    rc = _attend(load().grkv_attend_tree, p, q, k_pages, v_pages, table, lens, q_lens, parent,
-                 out, lse, ws, ws_bytes, stream)
+    u, d, tokens = p.units, p.d, p.tokens
+    n, rows = p.pages * p.page * d, u * p.group * tokens
+    (q, k, v, o, t, le, ql, pa, ls), w, nb, st = _addresses(
+        "attend_tree", p, ws, ws_bytes, stream,
+        (q, k_pages, v_pages, out, table, lens, q_lens, parent, lse),
+        (rows * d, n, n, rows * d, u * p.max_pages, u, u, u * tokens, rows))
+    rc = load().grkv_attend_tree(p, q, k, v, t, le, ql, pa, o, ls, w, nb, st)
     return _check(rc, "grkv_attend_tree", check)
 
 
