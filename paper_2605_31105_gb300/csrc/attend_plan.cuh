@@ -178,9 +178,14 @@ struct Split {
   I total, q;
   int r, G;
   float inv;
-  __device__ Split(I all, int ctas) : total(all), G(ctas), inv(1.f / (float)ctas) {
-    q = all / ctas;
-    r = (int)(all - q * ctas);
+  // Few instructions rather than divisions: at a kernel's start each is fetched from afar.
+  __device__ Split(I all, int ctas) : total(all), G(ctas) {
+    asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"((float)ctas));
+    q = sizeof(I) == 8 ? all / ctas : (I)((float)all * inv);
+    I left = all - q * ctas;
+    for (; left < 0; left += ctas) --q;        // one step at most below 2^22 tiles, 257 at 2^30
+    for (; left >= ctas; left -= ctas) ++q;
+    r = (int)left;
   }
   // r c / G through fp32: r c + 1/2 over G is at least 1 / (2 G) > 2^-10 from a whole number, and
   // below 2^9, so that an error of a few 2^-23 of it does not reach one
