@@ -362,9 +362,10 @@ int grkv_cache_compact(const grkv_cache_params* p, const int32_t* idx, const int
  * or only logits of -inf) gives out = 0 and lse = -inf.  Rows from q_len[u] on are left as
  * they were.  Slots that a row does not see do not reach it, whatever they hold,
  * and a page without a slot that some row of its unit sees is not read: its entry may be negative.
- * t = 1 is decoding, larger t a chunk of prefill.  bf16 rounds the unnormalised
- * probabilities to bf16 for the product with V (fp32 sums); results do not change from
- * run to run. */
+ * t = 1 is decoding, larger t a chunk of prefill.  Sums are fp32; bf16 rounds the
+ * unnormalised probabilities to bf16 for the product with V.  Where a slot that a row sees
+ * holds NaN or infinity, that row's elements come out non-finite (an infinity may come out
+ * as NaN).  Results do not change from run to run. */
 int grkv_attend(const grkv_cache_params* p, const void* q, const void* k_pages, const void* v_pages,
                 const int32_t* table, const int32_t* len, const int32_t* q_len, void* out,
                 float* lse, void* ws, size_t ws_bytes, void* stream);

@@ -19,9 +19,16 @@
 // range.  The first tile's largest P is 1, so no sum underflows; and where a later tile's sum
 // exceeds 2^60 the row takes that tile's maximum, the tile is done again and the output
 // scaled in TMEM.  A running maximum costs 64 three-operand maxima per row and tile in front of
-// the exponentials (half their time), and now and then the output's rescaling.  P is rounded to bf16 for the product with V: a
-// relative 2^-8 a term, of the size of the output's own rounding; the sum of a row is taken
-// in fp32 before it.
+// the exponentials (half their time), and now and then the output's rescaling.
+//
+// P is rounded to bf16 for the product with V: a relative 2^-8 a term at most, of the size of
+// the output's own rounding.  The outputs of few rows may rest on few probabilities, whose
+// roundings do not average, and those are mostly in the tile that gave the reference (a
+// cache's sinks).  So items of up to 64 rows (every single token) take two products for the
+// first slot tile of a segment, with P's rounding and with what that left: one query over 64
+// units of up to 16384 slots takes 59 us against 57 (for every tile 65; 256 units of 32768:
+// 680 against 624).  Items of more rows round once: trees of 65 rows over 128 units take
+// 43.7 us against 45.5.  A row's sum is taken in fp32 before that.
 //
 // Slot tiles that every row sees whole take no masks.  In the others the masks of a row are
 // four words, and V is searched for non-finite elements first: they are set to zero
@@ -47,6 +54,7 @@ constexpr long long kWaitBudget = 1ll << 32;                  // cycles (~2 s)
 constexpr int kMaxEdges = 16;   // masked tiles of a segment: at most 4 at each end of the
                                 // window (256 tokens) and one at the sinks' end
 constexpr float kMaxSum = 0x1p60f;   // of a row's P over one tile
+constexpr int kFewRows = 64;   // up to which P keeps its low part in a segment's first tile
 constexpr uint32_t kColO = 256; // TMEM: two S buffers, then two outputs
 
 template <int NQ>
@@ -113,19 +121,21 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
-__device__ __forceinline__ float max128(const float* v) {
+__device__ __forceinline__ float max32(const float* v) {
   float m[4];
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
     m[c] = max3(v[c], v[4 + c], v[8 + c]);
-#pragma unroll
-    for (int x = 12; x < 124; x += 8) m[c] = max3(m[c], v[x + c], v[x + 4 + c]);
-    m[c] = fmaxf(m[c], v[124 + c]);
+    m[c] = max3(m[c], v[12 + c], v[16 + c]);
+    m[c] = max3(m[c], v[20 + c], v[24 + c]);
+    m[c] = fmaxf(m[c], v[28 + c]);
   }
   return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
 
-// exp2(v sl2 - r) of 32 logits as bf16 pairs; the sums are of the values before rounding.
+// exp2(v sl2 - r) of 32 logits as 16 bf16 pairs, and with kLow 16 more of what that rounding
+// leaves; the sums are of the values before rounding.
+template <bool kLow>
 __device__ __forceinline__ void exp32(const float* v, float sl2, float r, uint32_t* pk, uint64_t* acc) {
   const uint64_t s2 = pack2(sl2, sl2), m2 = pack2(-r, -r);
 #pragma unroll
@@ -136,6 +146,8 @@ __device__ __forceinline__ void exp32(const float* v, float sl2, float r, uint32
     p1 = fast_exp2(p1);
     acc[x & 3] = add2(acc[x & 3], pack2(p0, p1));
     pk[x] = pack_bf16(p0, p1);
+    if (kLow)
+      pk[16 + x] = pack_bf16(p0 - __uint_as_float(pk[x] << 16), p1 - __uint_as_float(pk[x] & 0xffff0000u));
   }
 }
 
@@ -268,6 +280,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
   const uint32_t tmem = bars->tmem;
   volatile int* abort_flag = &bars->abort;
   int err = 0;
+  const bool few = NQ == 1 && a.rows <= kFewRows;   // the first slot tile takes both parts of P
 
   if (warp == 0) {
     // -------------------------------------------------------------- producer
@@ -385,8 +398,10 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
     };
     auto issue_o = [&](int buf, int o, int slot) {
       tc_fence_after();
-      mma8_ts<id_o, false>(tmem + kColO + o * kD, tmem + buf * kSlotTile,
-                           v_desc + slot * 2 * kTileDesc, !v_first);
+      const uint32_t d = tmem + kColO + o * kD, p = tmem + buf * kSlotTile;
+      const uint64_t v = v_desc + slot * 2 * kTileDesc;
+      mma8_ts<id_o, false>(d, p, v, !v_first);
+      if (few && v_first) mma8_ts<id_o, false>(d, p + 16, v, true);   // what the rounding of P left
     };
     const int tiles = run.left;
     // Slot tile t, in slot B = t & 1; ph = (t >> 1) & 1.  With two row tiles everything but P is
@@ -546,53 +561,82 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
         tc_fence_after();
         if (warp_live) {
           const bool masked = !full.has(tile);
-          uint32_t pk[64];
           float sum = 0.f, f = 1.f;
           bool look = no_ref;   // rows without a reference, or whose sum left its range
-#pragma unroll 1
-          for (bool again = false;; again = true) {
-            // the first chunk's exponentials run while the others are on their way
-            float v[128];
-            tmem_ld32f(lane_addr + scol, v);
-            tmem_wait32(v);
+          auto mask32 = [&](int c, float* v) {   // -inf for the slots of chunk c that the row does not see
+            const uint32_t m = vis.word(tile * kSlotTile + 32 * c);
+            if (__all_sync(0xffffffffu, m == 0xffffffffu)) return;
 #pragma unroll
-            for (int c = 1; c < 4; ++c) tmem_ld32f(lane_addr + scol + 32 * c, v + 32 * c);
-            if (masked || look) {
-#pragma unroll
-              for (int c = 1; c < 4; ++c) tmem_wait32(v + 32 * c);
-              if (masked) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                  const uint32_t m = vis.word(tile * kSlotTile + 32 * c);
-                  if (__all_sync(0xffffffffu, m == 0xffffffffu)) continue;
-#pragma unroll
-                  for (int x = 0; x < 32; ++x)
-                    if (!((m >> x) & 1)) v[32 * c + x] = -INFINITY;
-                }
-              }
-              if (look) {   // take the maximum
-                const bool need = live && (ref == -INFINITY || !(sum < kMaxSum));
-                const float to = fmaxf(ref, max128(v) * a.sl2);
-                if (need && ref != -INFINITY) f = fast_exp2(ref - to);
-                if (need) ref = to;
-                no_ref = __any_sync(0xffffffffu, live && ref == -INFINITY);
-              }
-            }
-            const float r = ref == -INFINITY ? 0.f : ref;
-            uint64_t acc[4] = {0, 0, 0, 0};
-            exp32(v, a.sl2, r, pk, acc);
-#pragma unroll
-            for (int c = 1; c < 4; ++c) tmem_wait32(v + 32 * c);
-#pragma unroll
-            for (int c = 1; c < 4; ++c) exp32(v + 32 * c, a.sl2, r, pk + 16 * c, acc);
+            for (int x = 0; x < 32; ++x)
+              if (!((m >> x) & 1)) v[x] = -INFINITY;
+          };
+          auto new_ref = [&](float top) {   // such rows take the maximum
+            const bool need = live && (ref == -INFINITY || !(sum < kMaxSum));
+            const float to = fmaxf(ref, top * a.sl2);
+            if (need && ref != -INFINITY) f = fast_exp2(ref - to);
+            if (need) ref = to;
+            no_ref = __any_sync(0xffffffffu, live && ref == -INFINITY);
+          };
+          auto total = [&](const uint64_t* acc) {
             float s0, s1;
             unpack2(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), s0, s1);
-            sum = s0 + s1;
-            look = __any_sync(0xffffffffu, live && !(sum < kMaxSum));
-            if (again || !look) break;
-          }
+            return s0 + s1;
+          };
+          if (few && k == 0) {
+            // both parts of P; a chunk at a time, over the logits that it comes from
+            float top = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c) {   // the maximum first
+              float v[32];
+              tmem_ld32f(lane_addr + scol + 32 * (c & 3), v);
+              tmem_wait32(v);
+              if (masked) mask32(c & 3, v);
+              if (c < 4) {
+                top = fmaxf(top, max32(v));
+                if (c == 3) new_ref(top);
+                continue;
+              }
+              uint32_t pk[32];
+              uint64_t acc[4] = {0, 0, 0, 0};
+              exp32<true>(v, a.sl2, ref == -INFINITY ? 0.f : ref, pk, acc);
+              sum += total(acc);
+              tmem_st16(lane_addr + scol + 32 * (c & 3), pk);
+              tmem_st16(lane_addr + scol + 32 * (c & 3) + 16, pk + 16);
+            }
+          } else {
+            uint32_t pk[64];
+#pragma unroll 1
+            for (bool again = false;; again = true) {
+              // the first chunk's exponentials run while the others are on their way
+              float v[128];
+              tmem_ld32f(lane_addr + scol, v);
+              tmem_wait32(v);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_st16(lane_addr + scol + 32 * c, pk + 16 * c);
+              for (int c = 1; c < 4; ++c) tmem_ld32f(lane_addr + scol + 32 * c, v + 32 * c);
+              if (masked || look) {
+#pragma unroll
+                for (int c = 1; c < 4; ++c) tmem_wait32(v + 32 * c);
+                if (masked) {
+#pragma unroll
+                  for (int c = 0; c < 4; ++c) mask32(c, v + 32 * c);
+                }
+                if (look)
+                  new_ref(fmaxf(fmaxf(max32(v), max32(v + 32)), fmaxf(max32(v + 64), max32(v + 96))));
+              }
+              const float r = ref == -INFINITY ? 0.f : ref;
+              uint64_t acc[4] = {0, 0, 0, 0};
+              exp32<false>(v, a.sl2, r, pk, acc);
+#pragma unroll
+              for (int c = 1; c < 4; ++c) tmem_wait32(v + 32 * c);
+#pragma unroll
+              for (int c = 1; c < 4; ++c) exp32<false>(v + 32 * c, a.sl2, r, pk + 16 * c, acc);
+              sum = total(acc);
+              look = __any_sync(0xffffffffu, live && !(sum < kMaxSum));
+              if (again || !look) break;
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_st16(lane_addr + scol + 32 * c, pk + 16 * c);
+          }
           if (k > 0 && __any_sync(0xffffffffu, f != 1.f)) {
             ok = done(n - NQ, false);
             if (!ok) break;
