@@ -8,6 +8,7 @@ namespace grkv {
 constexpr int kMaxCacheGroup = 64;   // query heads per KV head of the attention
 constexpr int kMaxTree = 256;        // drafted nodes per unit
 constexpr int kMaxAttendSms = 160;   // SMs whose CTAs' partial results the workspace holds
+constexpr int64_t kMaxAttendTiles = (int64_t)1 << 36;   // of a call: a CTA counts its own in 32 bits
 
 struct CacheShape {
   int U, g, t;
@@ -35,7 +36,8 @@ struct CacheWs {
   size_t total;
 };
 
-int attend_rows(const CacheShape& s, int* ctas);   // rows of a work item; the most CTAs   // rows of a work item
+int attend_rows(const CacheShape& s, int* ctas);   // rows of a work item; the most CTAs
+int64_t attend_tiles(const CacheShape& s);         // key tiles of a call at most
 cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, const CacheWs& L,
                           cudaStream_t st);
 

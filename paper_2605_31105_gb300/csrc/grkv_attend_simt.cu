@@ -566,6 +566,16 @@ int attend_rows(const CacheShape& s, int* ctas) {
   return T * nq * s.g;
 }
 
+int64_t attend_tiles(const CacheShape& s) {
+  int T, nq;
+  plan_rows(s, &T, &nq);
+  const int item = nq * T;
+  const int64_t cap = (((int64_t)s.cols << s.shift) + kSlotTile - 1) / kSlotTile;
+  // with a window: its slots from the first to the last token (in a tree from the base on), the sinks
+  const int64_t seen = s.W ? ((int64_t)s.W + s.s + item + kMaxTree) / kSlotTile + 4 : cap;
+  return (int64_t)s.U * ((s.t + item - 1) / item) * std::max<int64_t>(1, std::min(cap, seen));
+}
+
 cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, const CacheWs& L,
                           cudaStream_t st) {
   AttendArgs a{};
@@ -596,7 +606,7 @@ cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, con
   a.rows = a.nq * a.T * s.g;
   // two row tiles: an item's start and end take about three tiles' time, 8 K cycles
   a.extra = a.nq == 2 ? 3 : 0;
-  a.wide = (int64_t)s.U * a.QB * (((int64_t)s.cols << s.shift) / kSlotTile + 3 + a.extra) >= 1 << 30;
+  a.wide = attend_tiles(s) + (int64_t)s.U * a.QB * a.extra >= 1 << 30;
   const int sms = sm_count();
   if (sms <= 0 || sms > kMaxAttendSms) return cudaErrorInvalidDevice;
   const int G = sms * ctas_per_sm(s, a.rows);

@@ -520,7 +520,7 @@ int attend(const grkv_cache_params* p, const AttendIo& io, bool tree, void* ws, 
   CacheShape s;
   CacheWs L;
   GRKV_TRY(begin(p, ws, ws_bytes, &s, &L));
-  if (tree && s.t > kMaxTree) return GRKV_ERR_UNSUPPORTED;
+  if ((tree && s.t > kMaxTree) || attend_tiles(s) > kMaxAttendTiles) return GRKV_ERR_UNSUPPORTED;
   cudaStream_t st = (cudaStream_t)stream;
   if (s.U == 0) return clear_status((char*)ws, L, st);
   GRKV_TRY(check_ptrs({io.q, io.k, io.v, io.out}, 16));

@@ -76,6 +76,9 @@ def test_fork_onto_itself_and_sizes(lib):  # noqa: F811
     q = params(tokens=257)
     assert b.grkv_attend_tree(q, *[FAKE] * 7, FAKE, ws_bytes=b.grkv_cache_workspace_size(q),
                               stream=0, check=False) == b.GRKV_ERR_UNSUPPORTED
+    q = b.cache_params(1, 1, 100, 128, 1 << 21, tokens=1 << 24)   # 2^16 items x 2^21 slot tiles
+    assert b.grkv_attend(q, *[FAKE] * 7, ws_bytes=b.grkv_cache_workspace_size(q), stream=0,
+                         check=False) == b.GRKV_ERR_UNSUPPORTED
     assert b.strerror(b.GRKV_ERR_NO_PAGES) == "too few free pages in the pool"
 
 

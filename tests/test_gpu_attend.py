@@ -248,7 +248,7 @@ def test_runs_are_equal_and_graphs_replay(grkv_lib, dtype, flags):
     o1, l1 = run(c, p, q)
     kd, vd = c.dev()
     dq, out = q.cuda(), torch.zeros(q.shape, dtype=q.dtype, device="cuda")
-    lse = torch.zeros(q.shape[:3], device="cuda")
+    lse = torch.zeros(q.shape[:3], dtype=torch.float32, device="cuda")
     table, lens = R.int_dev(c.table), R.int_dev(c.lens)
     ws = [workspace(p), workspace(p)]
     graphs = []
@@ -331,7 +331,7 @@ def test_long_chunks_agree_between_the_kernels(grkv_lib, units, g, t, n, window)
     page = 32
     cols = R.pages_of(n, page)
     gen = torch.Generator(device="cuda").manual_seed(n)
-    rnd = lambda *s: torch.randn(*s, device="cuda", generator=gen).bfloat16()
+    rnd = lambda *s: torch.randn(*s, dtype=torch.float32, device="cuda", generator=gen).bfloat16()
     k, v, q = rnd(units * cols, page, D), rnd(units * cols, page, D), rnd(units, g, t, D)
     table = torch.randperm(units * cols, device="cuda", generator=gen).int().view(units, cols)
     lens = torch.tensor([n - 7 * u for u in range(units)], dtype=torch.int32, device="cuda")
@@ -339,7 +339,7 @@ def test_long_chunks_agree_between_the_kernels(grkv_lib, units, g, t, n, window)
     for flags in (0, b.GRKV_FORCE_SIMT):
         p = b.cache_params(units, g, units * cols, page, cols, tokens=t, window=window, flags=flags)
         ws, out = workspace(p), torch.zeros_like(q)
-        lse = torch.zeros(units, g, t, device="cuda")
+        lse = torch.zeros(units, g, t, dtype=torch.float32, device="cuda")
         for _ in range(2):
             b.grkv_attend(p, q, k, v, table, lens, out, ws, lse=lse)
             assert b.grkv_status(ws) == b.GRKV_OK
@@ -351,6 +351,26 @@ def test_long_chunks_agree_between_the_kernels(grkv_lib, units, g, t, n, window)
     assert ((o1 - o2).abs() <= 2.0 ** -7 * o2.abs() + (2.0 ** -8 + 2.0 ** -10) * mass).all()
     assert torch.equal(l1 == -math.inf, l2 == -math.inf)      # rows in front of a shorter cache
     assert (torch.where(l1 == l2, 0.0, l1 - l2).abs() <= 2.0 ** -9).all()
+
+
+@pytest.mark.parametrize("dtype,flags", TYPES)
+def test_tables_of_many_columns(grkv_lib, dtype, flags):
+    """A table that could hold more tiles than 32 bits count gives what a short one does."""
+    g, t, page, n = 64, 2200, 128, 2300
+    c = R.Cache([n], page, dtype, 40)
+    q, _ = queries(1, g, t, dtype, 41)
+    res = []
+    for cols in (c.cols, 1 << 21):
+        p = b.cache_params(1, g, c.pages, page, cols, tokens=t, dtype=dtype, flags=flags)
+        table = torch.full((1, cols), -1, dtype=torch.int32, device="cuda")
+        table[:, :c.cols] = R.int_dev(c.table)
+        kd, vd = c.dev()
+        out, ws = torch.zeros(q.shape, dtype=q.dtype, device="cuda"), workspace(p)
+        lse = torch.zeros(q.shape[:3], dtype=torch.float32, device="cuda")
+        b.grkv_attend(p, q.cuda(), kd, vd, table, R.int_dev(c.lens), out, ws, lse=lse)
+        assert b.grkv_status(ws) == b.GRKV_OK
+        res.append((out, lse))
+    assert torch.equal(res[0][0], res[1][0]) and torch.equal(res[0][1], res[1][1])
 
 
 def test_no_units(grkv_lib):
