@@ -297,7 +297,7 @@ def test_compressed_caches_are_decoded_with_drafts(grkv_lib):
     units, g, n, w, page = 6, 4, 900, 16, 32
     budgets = [100, 64, 333, 64, 17, 250]
     gen = torch.Generator(device="cuda").manual_seed(5)
-    rnd = lambda *s: torch.randn(*s, device="cuda", generator=gen).bfloat16()
+    rnd = lambda *s: torch.randn(*s, dtype=torch.float32, device="cuda", generator=gen).bfloat16()
     q, k, v = rnd(units, g, w, D), rnd(units, n, D), rnd(units, n, D)
     p = b.params(units, g, n, w, max(budgets))
     rows = sum(budgets)
@@ -444,7 +444,7 @@ def test_pools_beyond_32_bit_offsets(grkv_lib):
     p = b.cache_params(1, 2, pages, page, 4, tokens=n)
     ws = torch.empty(b.grkv_cache_workspace_size(p), dtype=torch.uint8, device="cuda")
     gen = torch.Generator(device="cuda").manual_seed(1)
-    rnd = lambda *s: torch.randn(*s, device="cuda", generator=gen).bfloat16()
+    rnd = lambda *s: torch.randn(*s, dtype=torch.float32, device="cuda", generator=gen).bfloat16()
     kn, vn = rnd(1, n, D), rnd(1, n, D)
     b.grkv_cache_append(p, kn, vn, *pool, table, lens, ws)
     assert b.grkv_status(ws) == b.GRKV_OK
