@@ -251,7 +251,7 @@ __device__ __noinline__ void add_bad(const AttendArgs& a, const Item& it, int of
 template <int NQ>
 __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
     k_attend_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                const __grid_constant__ CUtensorMap tmV, AttendArgs a) {
+                const __grid_constant__ CUtensorMap tmV, const __grid_constant__ AttendArgs a) {
   using Lay = TcLayout<NQ>;
   extern __shared__ __align__(1024) uint8_t smraw[];
   uint8_t* sm = (uint8_t*)(((uintptr_t)smraw + 1023) & ~(uintptr_t)1023);
@@ -563,13 +563,24 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
           const bool masked = !full.has(tile);
           float sum = 0.f, f = 1.f;
           bool look = no_ref;   // rows without a reference, or whose sum left its range
-          auto mask32 = [&](int c, float* v) {   // -inf for the slots of chunk c that the row does not see
-            const uint32_t m = vis.word(tile * kSlotTile + 32 * c);
-            if (__all_sync(0xffffffffu, m == 0xffffffffu)) return;
+          if (masked) {
+            // -inf, in TMEM, for the slots that a row does not see: one chunk's code, for the
+            // chunks that some row of the warp does not see whole
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              const uint32_t m = vis.word(tile * kSlotTile + 32 * c);
+              if (__all_sync(0xffffffffu, m == 0xffffffffu)) continue;
+              float v[32];
+              tmem_ld32f(lane_addr + scol + 32 * c, v);
+              tmem_wait32(v);
 #pragma unroll
-            for (int x = 0; x < 32; ++x)
-              if (!((m >> x) & 1)) v[x] = -INFINITY;
-          };
+              for (int x = 0; x < 32; ++x)
+                if (!((m >> x) & 1)) v[x] = -INFINITY;
+              tmem_st16(lane_addr + scol + 32 * c, (uint32_t*)v);
+              tmem_st16(lane_addr + scol + 32 * c + 16, (uint32_t*)v + 16);
+            }
+            tmem_st_wait();
+          }
           auto new_ref = [&](float top) {   // such rows take the maximum
             const bool need = live && (ref == -INFINITY || !(sum < kMaxSum));
             const float to = fmaxf(ref, top * a.sl2);
@@ -590,7 +601,6 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
               float v[32];
               tmem_ld32f(lane_addr + scol + 32 * (c & 3), v);
               tmem_wait32(v);
-              if (masked) mask32(c & 3, v);
               if (c < 4) {
                 top = fmaxf(top, max32(v));
                 if (c == 3) new_ref(top);
@@ -613,15 +623,10 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
               tmem_wait32(v);
 #pragma unroll
               for (int c = 1; c < 4; ++c) tmem_ld32f(lane_addr + scol + 32 * c, v + 32 * c);
-              if (masked || look) {
+              if (look) {
 #pragma unroll
                 for (int c = 1; c < 4; ++c) tmem_wait32(v + 32 * c);
-                if (masked) {
-#pragma unroll
-                  for (int c = 0; c < 4; ++c) mask32(c, v + 32 * c);
-                }
-                if (look)
-                  new_ref(fmaxf(fmaxf(max32(v), max32(v + 32)), fmaxf(max32(v + 64), max32(v + 96))));
+                new_ref(fmaxf(fmaxf(max32(v), max32(v + 32)), fmaxf(max32(v + 64), max32(v + 96))));
               }
               const float r = ref == -INFINITY ? 0.f : ref;
               uint64_t acc[4] = {0, 0, 0, 0};
@@ -662,8 +667,11 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
       if (!ok) break;
       tc_fence_after();
       if (!warp_live) continue;
-      if (__any_sync(0xffffffffu, any_bad))
-        add_bad(a, it, sg.off, sg.cnt, vis, bad, live, lane_addr + ocol);
+      if (__any_sync(0xffffffffu, any_bad)) {
+        const Item item = it;   // copies: what a call takes by reference is in memory for good
+        const RowVis seen = vis;
+        add_bad(a, item, sg.off, sg.cnt, seen, bad, live, lane_addr + ocol);
+      }
       if (sg.whole()) {
         const float f = l == 0.f ? 0.f : 1.f / l;
         const int dst = (it.u * a.g + h) * a.t + i;   // fits 32 bits
