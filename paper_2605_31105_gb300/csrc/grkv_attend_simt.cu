@@ -6,9 +6,10 @@
 // sub-tiles of 64 slots, copied page by page to shared memory: K while the last sub-tile's
 // values are multiplied, V while the logits are, so that one buffer each does and two CTAs
 // fit an SM (one CTA with two buffers each kept the FMA pipe 48% busy with two warps a
-// scheduler: 6 units of 1203 slots, 301 queries of 7 heads, 228 us against 217).  A thread of 256 holds 4 rows x 4 slots of the logits and then 4 rows x 8
-// columns of the output; the softmax is online: reference (running maximum, log2 units) and sum per row,
-// the output rescaled when the reference grows.  Slots that a row does not see carry p = -1
+// scheduler: 6 units of 1203 slots, 301 queries of 7 heads, 228 us against 220).  A thread of
+// 256 holds 4 rows x 4 slots of the logits and then 4 rows x 8 columns of the output; the softmax
+// is online: reference (running maximum, log2 units) and sum per row, the output rescaled
+// when the reference grows.  Bound by issue (70% of the slots; shared memory reads beside the FMAs).  Slots that a row does not see carry p = -1
 // and are left out of its sums by comparison, so whatever lies there (a NaN, an infinity)
 // does not reach the row.
 #include <algorithm>
@@ -246,7 +247,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_simt(AttendArgs a) {
 // transpose-reduction of 31 shuffles leaves one to a lane, so that a step has one
 // exponential a lane.  The warps' references, sums and outputs are joined at a segment's end.
 // Up to 8 rows fit two CTAs on an SM, which keep 16 warps x 8 KB (fp32) in flight.  (64-row tiles, of which one query
-// of 4 heads fills a sixteenth: 32 units of up to 12005 slots, window 4096, 134 us.)
+// of 4 heads fills a sixteenth: 32 units of up to 12005 slots, window 4096, 134 us against 31.5,
+// 119 MB at 3.8 TB/s: starts, the latency of a run's first loads and the join are half of it.)
 constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
 
 template <int R>

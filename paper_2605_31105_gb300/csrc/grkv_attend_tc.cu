@@ -30,6 +30,12 @@
 // 680 against 624).  Items of more rows round once: trees of 65 rows over 128 units take
 // 43.7 us against 45.5.  A row's sum is taken in fp32 before that.
 //
+// What bounds it (one GB300).  Few rows over a long cache: memory, 256 units of 32768 slots in
+// 615 us, 7.0 TB/s.  Chunks of prefill: a row tile's chain of S (512 cycles), softmax (1.2 K with two
+// warps to a scheduler) and P V (512), which two row tiles overlap: 2.95 K cycles a slot tile against
+// 2 K of MMAs; 2048 queries of 32 heads over 16384 slots take 329 us, 1.57 PFLOP/s.  Windows and trees:
+// items are short, and each has a start and an end (8 K cycles) and tiles with masks (2 K more).
+//
 // Slot tiles that every row sees whole take no masks.  In the others the masks of a row are
 // four words, and V is searched for non-finite elements first: they are set to zero
 // in shared memory (0 x NaN would reach rows that do not see the slot; what was
@@ -565,7 +571,8 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
           bool look = no_ref;   // rows without a reference, or whose sum left its range
           if (masked) {
             // -inf, in TMEM, for the slots that a row does not see: one chunk's code, for the
-            // chunks that some row of the warp does not see whole
+            // chunks that some row of the warp does not see whole.  (In line with the
+            // exponentials, 128 selects more to fetch: the chunk above took 350 us, not 329.)
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
               const uint32_t m = vis.word(tile * kSlotTile + 32 * c);

@@ -369,7 +369,8 @@ __device__ __forceinline__ int rows_of(const RowMove& m, int u) {
   return min(max(n, 0), m.t);
 }
 
-// Copies of rows: a block takes 4 x 256 / kRow16 rows of one unit (grid (blocks of rows, units)),
+// Copies of rows, bound by memory (524288 kept rows of K and V, 537 MB read and written in 102 us,
+// 5.3 TB/s: reads of 256 bytes from anywhere): a block takes 4 x 256 / kRow16 rows of one unit (grid (blocks of rows, units)),
 // kRow16 lanes a row of kRow16 16-byte chunks, four rows of K and V in flight to a thread.
 constexpr int kMoveThreads = 256, kMoveUnroll = 4;
 constexpr int move_rows(int row16) { return kMoveUnroll * kMoveThreads / row16; }
