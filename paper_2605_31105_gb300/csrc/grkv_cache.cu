@@ -369,14 +369,17 @@ __device__ __forceinline__ int rows_of(const RowMove& m, int u) {
   return min(max(n, 0), m.t);
 }
 
-// Copies of rows, bound by memory (524288 kept rows of K and V, 537 MB read and written in 102 us,
-// 5.3 TB/s: reads of 256 bytes from anywhere): a block takes 4 x 256 / kRow16 rows of one unit (grid (blocks of rows, units)),
-// kRow16 lanes a row of kRow16 16-byte chunks, four rows of K and V in flight to a thread.
-constexpr int kMoveThreads = 256, kMoveUnroll = 4;
+// Copies of rows: a block takes 2 x 128 / kRow16 rows of one unit (grid (blocks of rows, units)),
+// kRow16 lanes a row of kRow16 16-byte chunks, two rows of K and V in flight to a thread.  Bound
+// by memory: 524288 kept rows of K and V (537 MB read and written, rows of 256 bytes from
+// anywhere) in 90 us, 6.0 TB/s.  Those are read once and written for later (kOnce), which loads
+// and stores say (95 us without; only one of the two 107 to 117).  256 threads 98 us, with
+// four or eight rows each 101 and 131.
+constexpr int kMoveThreads = 128, kMoveUnroll = 2;
 constexpr int move_rows(int row16) { return kMoveUnroll * kMoveThreads / row16; }
 
 // where(u, i, n, len, &from, &to): source and destination row of row i of unit u's n; false: none
-template <int kRow16, typename Where>
+template <int kRow16, bool kOnce, typename Where>
 __device__ __forceinline__ void move_block(const RowMove& m, const uint4* k_in, const uint4* v_in,
                                            uint4* k, uint4* v, Where where) {
   const int ch = threadIdx.x % kRow16, r = threadIdx.x / kRow16;
@@ -394,14 +397,21 @@ __device__ __forceinline__ void move_block(const RowMove& m, const uint4* k_in, 
         to[j] = -1;
         continue;
       }
-      x[j] = k_in[from * kRow16 + ch];
-      y[j] = v_in[from * kRow16 + ch];
+      const uint4 *pk = k_in + from * kRow16 + ch, *pv = v_in + from * kRow16 + ch;
+      x[j] = kOnce ? __ldcs(pk) : *pk;
+      y[j] = kOnce ? __ldcs(pv) : *pv;
     }
 #pragma unroll
     for (int j = 0; j < kMoveUnroll; ++j) {
       if (to[j] < 0) continue;
-      k[to[j] * kRow16 + ch] = x[j];
-      v[to[j] * kRow16 + ch] = y[j];
+      uint4 *pk = k + to[j] * kRow16 + ch, *pv = v + to[j] * kRow16 + ch;
+      if (kOnce) {
+        __stcs(pk, x[j]);
+        __stcs(pv, y[j]);
+      } else {
+        *pk = x[j];
+        *pv = y[j];
+      }
     }
   }
 }
@@ -411,7 +421,7 @@ __global__ void __launch_bounds__(kMoveThreads)
     k_cache_append(RowMove m, const uint4* __restrict__ k_new, const uint4* __restrict__ v_new,
                    const int64_t* __restrict__ first, long long new_rows,
                    const int32_t* __restrict__ table, uint4* k, uint4* v) {
-  move_block<kRow16>(m, k_new, v_new, k, v, [&](int u, int i, int n, int len, long long* from,
+  move_block<kRow16, false>(m, k_new, v_new, k, v, [&](int u, int i, int n, int len, long long* from,
                                                 long long* to) {
     const int slot = len - n + i;
     const long long f = first ? first[u] : (long long)u * m.t;
@@ -449,7 +459,7 @@ __global__ void __launch_bounds__(kMoveThreads)
     k_cache_gather(RowMove m, const int32_t* __restrict__ idx, const int32_t* __restrict__ table_in,
                    const int32_t* __restrict__ table_out, const int32_t* __restrict__ first, uint4* k,
                    uint4* v) {
-  move_block<kRow16>(m, k, v, k, v, [&](int u, int i, int, int len, long long* from, long long* to) {
+  move_block<kRow16, true>(m, k, v, k, v, [&](int u, int i, int, int len, long long* from, long long* to) {
     return kept_row(m, idx, table_in, len, table_out, first, false, u, i, from, to);
   });
 }
