@@ -9,9 +9,9 @@
 // scheduler: 6 units of 1203 slots, 301 queries of 7 heads, 228 us against 220).  A thread of
 // 256 holds 4 rows x 4 slots of the logits and then 4 rows x 8 columns of the output; the softmax
 // is online: reference (running maximum, log2 units) and sum per row, the output rescaled
-// when the reference grows.  Bound by issue (70% of the slots; shared memory reads beside the FMAs).  Slots that a row does not see carry p = -1
-// and are left out of its sums by comparison, so whatever lies there (a NaN, an infinity)
-// does not reach the row.
+// when the reference grows.  Bound by issue (70% of the slots; shared memory reads beside the
+// FMAs).  Slots that a row does not see carry p = -1 and are left out of its sums by comparison,
+// so whatever lies there (a NaN, an infinity) does not reach the row.
 #include <algorithm>
 
 #include "attend_plan.cuh"
@@ -246,9 +246,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_simt(AttendArgs a) {
 // four dimensions of all of them: R x 32 / R = 32 logits, whose sums over the lanes a
 // transpose-reduction of 31 shuffles leaves one to a lane, so that a step has one
 // exponential a lane.  The warps' references, sums and outputs are joined at a segment's end.
-// Up to 8 rows fit two CTAs on an SM, which keep 16 warps x 8 KB (fp32) in flight.  (64-row tiles, of which one query
-// of 4 heads fills a sixteenth: 32 units of up to 12005 slots, window 4096, 134 us against 31.5,
-// 119 MB at 3.8 TB/s: starts, the latency of a run's first loads and the join are half of it.)
+// Up to 8 rows fit two CTAs on an SM, which keep 16 warps x 8 KB (fp32) in flight: one query of 3
+// heads over 32 units of up to 12005 slots, window 4096, takes 31.5 us, 119 MB at 3.8 TB/s, half of
+// it starts, the latency of a run's first loads and the join.  (64-row tiles, mostly empty: 134 us.)
 constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
 
 template <int R>
@@ -425,8 +425,8 @@ __device__ __forceinline__ int split_cta(const AttendArgs& a, int G, int k) {
 }
 
 // Adds up the partial results of the split items, and writes the call's status.  Blocks
-// (c, y) take the item that starts in CTA c (kSearch: the c-th split item), a thread four columns of a row (an element).  Items
-// of up to 16 rows may have many parts: the one block's threads go over them in groups of
+// (c, y) take the item that starts in CTA c (kSearch: the c-th split item), a thread four columns
+// of a row (an element).  Items of up to 16 rows may have many parts: the one block's threads go over them in groups of
 // one thread per element.  Else a thread has one element, or four where there are only two
 // parts: eight loads of outputs are in flight.
 constexpr int kJoinFewRows = 16;
