@@ -296,7 +296,7 @@ typedef struct {
   int32_t d;          /* head dimension; 128 only                                     */
   int32_t pages;      /* P: pages of the pool, 1..2^30                                */
   int32_t page;       /* slots per page: 16, 32, 64 or 128                            */
-  int32_t max_pages;  /* columns of a table row; max_pages page <= 2^28               */
+  int32_t max_pages;  /* columns of a table row; max_pages page <= 2^28, U max_pages <= 2^30 */
   int32_t tokens;     /* t >= 1: rows per unit of q, new rows or idx (1); U g t <= 2^28 */
   int32_t window;     /* W >= 0: slots a row sees behind it, itself included; 0: all  */
   int32_t n_sink;     /* s >= 0: first slots that a window leaves visible (4)         */

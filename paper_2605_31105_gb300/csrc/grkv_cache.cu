@@ -49,9 +49,11 @@ int make_cache_shape(const grkv_cache_params* p, CacheShape* s) {
   if (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128)
     return GRKV_ERR_UNSUPPORTED;
   // pages, slots of a unit, entries of a table and rows of a call stay within 32-bit integers
+  // (rows in two steps: U g t itself may pass 64 bits)
   if (p->pages > 1 << 30) return GRKV_ERR_UNSUPPORTED;
   if ((int64_t)p->max_pages * p->page > (int64_t)1 << 28) return GRKV_ERR_UNSUPPORTED;
   if (p->tokens > 1 << 28 || (int64_t)p->units * p->max_pages > (int64_t)1 << 30 ||
+      (int64_t)p->units * p->group > (int64_t)1 << 28 ||
       (int64_t)p->units * p->group * p->tokens > (int64_t)1 << 28)
     return GRKV_ERR_UNSUPPORTED;
   s->U = p->units;
