@@ -308,6 +308,8 @@ typedef struct {
 /* Fills `p` with the defaults above for the given sizes (bf16, one token, no window). */
 void grkv_cache_params_init(grkv_cache_params* p, int32_t units, int32_t group, int32_t pages,
                             int32_t page, int32_t max_pages);
+/* The size does not grow when only `tokens` gets smaller: a workspace for the longest chunk or
+ * draft serves the shorter ones too. */
 int grkv_cache_workspace_size(const grkv_cache_params* p, size_t* bytes);
 
 /* Pages for the slots [len[u], want[u]) of every unit (none if want <= len), each held by

@@ -28,7 +28,7 @@ struct AttendIo {
 // Workspace regions of the cache calls (byte offsets, 256-byte aligned).
 struct CacheWs {
   size_t status;
-  size_t rec;    // AttendRec [CTAs]
+  size_t rec;    // AttendRec [2 kMaxAttendSms]
   size_t pml;    // float2 [2 CTAs][rows] reference and sum of a partial row
   size_t po;     // float  [2 CTAs][rows][d] its unnormalised output
   size_t list;   // int    [P] free pages found by a reserve
@@ -36,7 +36,7 @@ struct CacheWs {
   size_t total;
 };
 
-int attend_rows(const CacheShape& s, int* ctas);   // rows of a work item; the most CTAs
+size_t attend_part_rows(const CacheShape& s);      // rows of the partial results of all CTAs
 int64_t attend_tiles(const CacheShape& s);         // key tiles of a call at most
 cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, const CacheWs& L,
                           cudaStream_t st);

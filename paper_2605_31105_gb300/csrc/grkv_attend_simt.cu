@@ -586,11 +586,13 @@ static int ctas_per_sm(const CacheShape& s, int rows) {
   return (s.dtype == GRKV_F32 || s.simt) && (rows <= 8 || rows > 16) ? 2 : 1;
 }
 
-int attend_rows(const CacheShape& s, int* ctas) {
+// Two parts a CTA.  Items of 9 to 15 rows have half the CTAs of items of 8, and take what those
+// would: a call of fewer tokens never needs more.
+size_t attend_part_rows(const CacheShape& s) {
   int T, nq;
   plan_rows(s, &T, &nq);
-  *ctas = kMaxAttendSms * ctas_per_sm(s, T * nq * s.g);
-  return T * nq * s.g;
+  const int rows = T * nq * s.g, few = std::min(rows, 8);
+  return (size_t)2 * kMaxAttendSms * std::max(rows * ctas_per_sm(s, rows), few * ctas_per_sm(s, few));
 }
 
 int64_t attend_tiles(const CacheShape& s) {

@@ -79,12 +79,11 @@ CacheWs plan_cache_ws(const CacheShape& s) {
     off = align256(off + bytes);
     return at;
   };
-  int ctas;
-  const size_t rows = (size_t)attend_rows(s, &ctas);
+  const size_t rows = attend_part_rows(s);   // of the parts of all CTAs
   L.status = take(256);
-  L.rec = take((size_t)ctas * 16);
-  L.pml = take(2 * (size_t)ctas * rows * sizeof(float2));
-  L.po = take(2 * (size_t)ctas * rows * kD * sizeof(float));
+  L.rec = take((size_t)2 * kMaxAttendSms * 16);
+  L.pml = take(rows * sizeof(float2));
+  L.po = take(rows * kD * sizeof(float));
   // a reserve and an attention call do not need their parts at the same time
   const size_t attend = off;
   off = L.rec;

@@ -23,3 +23,11 @@ def test_the_largest_sizes_are_taken(lib):  # noqa: F811
     assert size(units=1 << 22, group=64, max_pages=1, tokens=1) > 0
     assert size(units=1, group=64, tokens=1 << 22) > 0
     assert size(units=1 << 28, group=1, max_pages=4, tokens=1) > 0
+
+
+@pytest.mark.parametrize("dtype,flags", [("bf16", 0), ("f32", 0), ("bf16", b.GRKV_FORCE_SIMT)])
+def test_a_workspace_serves_calls_of_fewer_tokens(lib, dtype, flags):  # noqa: F811
+    """One sized for the longest draft or chunk is large enough for every shorter one."""
+    for group in (1, 2, 3, 4, 5, 7, 8, 11, 16, 21, 32, 33, 64):
+        sizes = [size(group=group, tokens=t, dtype=dtype, flags=flags) for t in range(1, 301)]
+        assert sizes == sorted(sizes), group
