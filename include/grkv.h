@@ -324,7 +324,8 @@ int grkv_cache_reserve(const grkv_cache_params* p, int32_t* table, const int32_t
 
 /* Unit u of table_out holds the pages of unit src[u] of table_in (units_in rows), or none
  * for src[u] = -1: forks sequences, reorders beams.  No row is copied: refs gains
- * one per entry written.  len_out[u] = len_in[src[u]].  table_out is overwritten, entries
+ * one per page.  len_out[u] = len_in[src[u]].  A column without a page (in front of every
+ * window, say) has none in the fork.  table_out is overwritten, entries
  * behind the length with -1; it must hold no page (grkv_cache_trim to 0 first). */
 int grkv_cache_fork(const grkv_cache_params* p, int32_t units_in, const int32_t* src,
                     const int32_t* table_in, const int32_t* len_in, int32_t* table_out,

@@ -153,13 +153,12 @@ __global__ void __launch_bounds__(1024)
     const int len = s >= 0 ? tb.clamped(len_in[s], st.at) : 0;
     int e = -1;
     if (c << tb.shift < len) {
-      e = table_in[(size_t)s * tb.cols + c];
-      if ((unsigned)e < (unsigned)tb.P) {
-        atomicAdd(refs + e, 1);
-      } else {
+      e = max(table_in[(size_t)s * tb.cols + c], -1);   // a column may be without a page
+      if (e >= tb.P) {
         set_status(st.at, GRKV_ERR_INVALID_ARG);
         e = -1;
       }
+      if (e >= 0) atomicAdd(refs + e, 1);
     }
     table_out[x] = e;
     if (c == 0) len_out[u] = len;

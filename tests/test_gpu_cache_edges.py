@@ -1,0 +1,49 @@
+"""The paged cache's page operators where tables have holes, end, or are long."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_31105_gb300 import binding as b
+from tests import cache_ref as R
+from tests.test_gpu_cache import Dev
+
+pytestmark = pytest.mark.gpu
+D = R.D
+
+
+@pytest.mark.parametrize("cols", [12, 200])
+def test_units_without_their_first_pages_are_forked(grkv_lib, cols):
+    """Pages in front of every window may be gone, for attention and for a fork: a column without
+    a page has none in the fork either.  (One block that writes the status itself, and many.)"""
+    page, units = 16, 30
+    rng = np.random.default_rng(1)
+    c = R.Cache([int(x) for x in rng.integers(100, 11 * page, units)], page, "bf16", 2, spare=9)
+    c.table = np.concatenate([c.table, np.full((units, cols - c.cols), -1, np.int32)], 1)
+    c.cols = cols
+    for u in range(0, units, 2):
+        for col in range(1, 1 + u % 5):     # the sinks' page stays, those behind it are gone
+            c.refs[c.table[u, col]] -= 1
+            c.table[u, col] = -1 if u % 4 else -2 ** 31
+    src = [int(x) for x in rng.integers(-1, units, 17)]
+    d = Dev(c)
+    p = b.cache_params(len(src), 2, c.pages, page, cols)
+    table = torch.full((len(src), cols), 7, dtype=torch.int32, device="cuda")
+    lens = torch.full((len(src),), 7, dtype=torch.int32, device="cuda")
+    b.grkv_cache_fork(p, R.int_dev(src), d.table, d.lens, table, lens, d.refs, d.ws)
+    d.ok()
+    want = np.full((len(src), cols), -1, np.int32)
+    for u, s in enumerate(src):
+        m = R.pages_of(c.lens[s], page) if s >= 0 else 0
+        want[u, :m] = np.maximum(c.table[s, :m], -1)
+        np.add.at(c.refs, want[u][want[u] >= 0], 1)
+    assert np.array_equal(table.cpu().numpy(), want)
+    assert lens.tolist() == [c.lens[s] if s >= 0 else 0 for s in src]
+    d.same()
+    # an entry behind the pool is still reported, and taken as none
+    d.table[src[0] if src[0] >= 0 else 0, 0] = c.pages
+    c.table[src[0] if src[0] >= 0 else 0, 0] = c.pages
+    before = d.refs.clone()
+    b.grkv_cache_fork(p, R.int_dev([max(src[0], 0)] + [-1] * (len(src) - 1)), d.table, d.lens, table,
+                      lens, d.refs, d.ws)
+    d.ok(b.GRKV_ERR_INVALID_ARG)
+    assert table[0, 0].item() == -1 and (table[0] >= 0).sum().item() == (d.refs - before).sum().item()
