@@ -339,7 +339,8 @@ int grkv_cache_trim(const grkv_cache_params* p, int32_t* table, const int32_t* l
 /* Writes new rows to the last count[u] (NULL: t) of the len[u] slots of every unit: len is
  * the length with the new rows.  Row i of unit u is row u t + i of k_new, v_new
  * [U][t][d], or, with first_row, row first_row[u] + i of k_new, v_new [new_rows][d] (the
- * packed outputs of grkv_compress_ragged); new_rows is not read without first_row. */
+ * packed outputs of grkv_compress_ragged); new_rows is not read without first_row.  Rows whose
+ * slot is not in the table (a length past it) are skipped; the others go to their slots. */
 int grkv_cache_append(const grkv_cache_params* p, const void* k_new, const void* v_new,
                       const int64_t* first_row, int64_t new_rows, const int32_t* count,
                       const int32_t* table, const int32_t* len, void* k_pages, void* v_pages,

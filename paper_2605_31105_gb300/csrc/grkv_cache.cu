@@ -421,16 +421,17 @@ __global__ void __launch_bounds__(kMoveThreads)
     k_cache_append(RowMove m, const uint4* __restrict__ k_new, const uint4* __restrict__ v_new,
                    const int64_t* __restrict__ first, long long new_rows,
                    const int32_t* __restrict__ table, uint4* k, uint4* v) {
-  move_block<kRow16, false>(m, k_new, v_new, k, v, [&](int u, int i, int n, int len, long long* from,
+  move_block<kRow16, false>(m, k_new, v_new, k, v, [&](int u, int i, int n, int, long long* from,
                                                 long long* to) {
-    const int slot = len - n + i;
+    // the length as it is: clamped to the table, rows behind it would go over those before
+    const long long slot = (long long)m.len[u] - n + i;
     const long long f = first ? first[u] : (long long)u * m.t;
-    if (slot < 0 || f < 0 || f > new_rows - 1 - i) {
+    if (slot < 0 || slot >= m.tb.cols << m.tb.shift || f < 0 || f > new_rows - 1 - i) {
       set_status(m.status, GRKV_ERR_INVALID_ARG);
       return false;
     }
     *from = f + i;
-    *to = pool_row(m.tb, table, u, slot, m.status);
+    *to = pool_row(m.tb, table, u, (int)slot, m.status);
     return *to >= 0;
   });
 }

@@ -47,3 +47,26 @@ def test_units_without_their_first_pages_are_forked(grkv_lib, cols):
                       lens, d.refs, d.ws)
     d.ok(b.GRKV_ERR_INVALID_ARG)
     assert table[0, 0].item() == -1 and (table[0] >= 0).sum().item() == (d.refs - before).sum().item()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_behind_a_full_table_are_not_written_over_others(grkv_lib, dtype):
+    """A length past the table: rows that have a slot go there, the others nowhere."""
+    page, t = 16, 5
+    c = R.Cache([96, 95, 96, 40, 96], page, dtype, 3)
+    cap = c.cols * page
+    assert cap == 96
+    rng = np.random.default_rng(4)
+    kn, vn = (c.rounded(rng.standard_normal((5, t, D))) for _ in range(2))
+    d = Dev(c, tokens=t)
+    as_t = lambda x: torch.from_numpy(x).to(R.TORCH[dtype]).cuda()
+    lens, count = [97, 98, 2 ** 31 - 1, 40, 101], [1, 3, 5, 2, 5]
+    b.grkv_cache_append(d.p, as_t(kn), as_t(vn), d.k, d.v, d.table, R.int_dev(lens), d.ws,
+                        count=R.int_dev(count))
+    d.ok(b.GRKV_ERR_INVALID_ARG)
+    for u, (n, m) in enumerate(zip(lens, count)):
+        for i in range(m):
+            if n - m + i < cap:
+                at = R.at(c.table, u, n - m + i, page)
+                c.k[at], c.v[at] = kn[u, i], vn[u, i]
+    d.same()
