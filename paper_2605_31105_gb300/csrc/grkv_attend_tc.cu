@@ -20,6 +20,10 @@
 // exceeds 2^60 the row takes that tile's maximum, the tile is done again and the output
 // scaled in TMEM.  A running maximum costs 64 three-operand maxima per row and tile in front of
 // the exponentials (half their time), and now and then the output's rescaling.
+// The exponents come from one fused logit x scale - reference, in which the product is exact and the
+// reference rounded: from 2^23 on by more than 1/2, and in the end by more than an exponent
+// holds.  A row with such a reference follows the running maximum, rounded down, and its exponents are
+// bounded by 0: logits that fp32 cannot tell from the maximum weigh as much as it.
 //
 // P is rounded to bf16 for the product with V: a relative 2^-8 a term at most, of the size of
 // the output's own rounding.  The outputs of few rows may rest on few probabilities, whose
@@ -60,6 +64,7 @@ constexpr long long kWaitBudget = 1ll << 32;                  // cycles (~2 s)
 constexpr int kMaxEdges = 16;   // masked tiles of a segment: at most 4 at each end of the
                                 // window (256 tokens) and one at the sinks' end
 constexpr float kMaxSum = 0x1p60f;   // of a row's P over one tile
+constexpr float kBigRef = 0x1p23f;   // references from here on are rounded by more than 1/2
 constexpr int kFewRows = 64;   // up to which P keeps its low part in a segment's first tile
 constexpr uint32_t kColO = 256; // TMEM: two S buffers, then two outputs
 
@@ -155,6 +160,45 @@ __device__ __forceinline__ void exp32(const float* v, float sl2, float r, uint32
     if (kLow)
       pk[16 + x] = pack_bf16(p0 - __uint_as_float(pk[x] << 16), p1 - __uint_as_float(pk[x] & 0xffff0000u));
   }
+}
+
+__device__ __forceinline__ float total(const uint64_t* acc) {
+  float s0, s1;
+  unpack2(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), s0, s1);
+  return s0 + s1;
+}
+
+// P of a slot tile where some row of the warp has a large reference: every row takes the maximum
+// `top`, and P, both parts, goes over the logits that it comes from.  Exponents in rows with large
+// references are bounded by 0, a NaN stays (all lanes of the warp; rare, so not in line).
+struct Followed {
+  float sum, ref, f;   // of P; the new reference; what the row's output so far is multiplied by
+};
+__device__ __noinline__ Followed follow_row(uint32_t s_addr, float sl2, float top, float ref) {
+  float to = top * sl2;
+  if (!(fabsf(to) < kBigRef)) to = __fmul_rd(top, sl2);
+  to = fmaxf(ref, to);
+  Followed y{0.f, to, ref == -INFINITY ? 1.f : fast_exp2(ref - to)};
+  const float r = to == -INFINITY ? 0.f : to;
+  const bool big = !(fabsf(r) < kBigRef);
+#pragma unroll 1
+  for (int c = 0; c < 4; ++c) {
+    float v[32];
+    tmem_ld32f(s_addr + 32 * c, v);
+    tmem_wait32(v);
+#pragma unroll
+    for (int x = 0; x < 32; ++x) {
+      const float t = fmaf(v[x], sl2, -r);
+      v[x] = big && t > 0.f ? 0.f : t;
+    }
+    uint32_t pk[32];
+    uint64_t acc[4] = {0, 0, 0, 0};
+    exp32<true>(v, 1.f, 0.f, pk, acc);
+    y.sum += total(acc);
+    tmem_st16(s_addr + 32 * c, pk);
+    tmem_st16(s_addr + 32 * c + 16, pk + 16);
+  }
+  return y;
 }
 
 // Multiplies a row's output by f (all lanes of the warp; rare, so not in line).
@@ -550,7 +594,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
       uint4* bad = bad_all + (seg & 3) * kMaxEdges;
       float ref = -INFINITY, l = 0.f;
       int e = 0;
-      bool any_bad = false, no_ref = warp_live;   // some row has no reference yet
+      bool any_bad = false, follow = warp_live;   // some row has no reference yet, or a large one
       const uint32_t ocol = kColO + (NQ == 2 ? w : seg & 1) * kD;
       // The products of all tiles up to job `job` are in the output.  Two row tiles: S of job n has
       // been signalled after them, so only a segment's end has to wait, for its own signal.
@@ -568,7 +612,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
         if (warp_live) {
           const bool masked = !full.has(tile);
           float sum = 0.f, f = 1.f;
-          bool look = no_ref;   // rows without a reference, or whose sum left its range
+          bool look = follow;   // or a sum that left its range
           if (masked) {
             // -inf, in TMEM, for the slots that a row does not see: one chunk's code, for the
             // chunks that some row of the warp does not see whole.  (In line with the
@@ -588,17 +632,20 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
             }
             tmem_st_wait();
           }
-          auto new_ref = [&](float top) {   // such rows take the maximum
+          // Such rows take the maximum; true: some reference is large, P has been formed.
+          auto new_ref = [&](float top) -> bool {
             const bool need = live && (ref == -INFINITY || !(sum < kMaxSum));
-            const float to = fmaxf(ref, top * a.sl2);
+            const float before = ref, to = fmaxf(ref, top * a.sl2);
             if (need && ref != -INFINITY) f = fast_exp2(ref - to);
             if (need) ref = to;
-            no_ref = __any_sync(0xffffffffu, live && ref == -INFINITY);
-          };
-          auto total = [&](const uint64_t* acc) {
-            float s0, s1;
-            unpack2(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), s0, s1);
-            return s0 + s1;
+            follow = __any_sync(0xffffffffu, live && !(fabsf(ref) < kBigRef));
+            if (!follow || !__any_sync(0xffffffffu, live && ref != -INFINITY && !(fabsf(ref) < kBigRef)))
+              return false;
+            const Followed y = follow_row(lane_addr + scol, a.sl2, top, before);
+            sum = y.sum;
+            ref = y.ref;
+            f = y.f;
+            return true;
           };
           if (few && k == 0) {
             // both parts of P; a chunk at a time, over the logits that it comes from
@@ -610,7 +657,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
               tmem_wait32(v);
               if (c < 4) {
                 top = fmaxf(top, max32(v));
-                if (c == 3) new_ref(top);
+                if (c == 3 && new_ref(top)) break;
                 continue;
               }
               uint32_t pk[32];
@@ -622,6 +669,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
             }
           } else {
             uint32_t pk[64];
+            bool formed = false;   // P is in TMEM already
 #pragma unroll 1
             for (bool again = false;; again = true) {
               // the first chunk's exponentials run while the others are on their way
@@ -633,7 +681,8 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
               if (look) {
 #pragma unroll
                 for (int c = 1; c < 4; ++c) tmem_wait32(v + 32 * c);
-                new_ref(fmaxf(fmaxf(max32(v), max32(v + 32)), fmaxf(max32(v + 64), max32(v + 96))));
+                formed = new_ref(fmaxf(fmaxf(max32(v), max32(v + 32)), fmaxf(max32(v + 64), max32(v + 96))));
+                if (formed) break;
               }
               const float r = ref == -INFINITY ? 0.f : ref;
               uint64_t acc[4] = {0, 0, 0, 0};
@@ -646,8 +695,10 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
               look = __any_sync(0xffffffffu, live && !(sum < kMaxSum));
               if (again || !look) break;
             }
+            if (!formed) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_st16(lane_addr + scol + 32 * c, pk + 16 * c);
+              for (int c = 0; c < 4; ++c) tmem_st16(lane_addr + scol + 32 * c, pk + 16 * c);
+            }
           }
           if (k > 0 && __any_sync(0xffffffffu, f != 1.f)) {
             ok = done(n - NQ, false);
