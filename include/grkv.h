@@ -369,8 +369,8 @@ int grkv_cache_compact(const grkv_cache_params* p, const int32_t* idx, const int
  * t = 1 is decoding, larger t a chunk of prefill.  Sums are fp32; bf16 rounds the
  * unnormalised probabilities to bf16 for the product with V.  Where a slot that a row sees
  * holds NaN or infinity, that row's elements come out non-finite (an infinity may come out
- * as NaN).  bf16 holds unnormalised outputs of up to 2^60 times a row's values, which must
- * stay within fp32.  Results do not change from run to run.  GRKV_ERR_UNSUPPORTED for a call
+ * as NaN).  bf16 holds unnormalised outputs of up to 2^68 times a row's values (2^60 in each
+ * of a unit's parts), which must stay within fp32.  Results do not change from run to run.  GRKV_ERR_UNSUPPORTED for a call
  * that could read more than 2^36 tiles of 128 slots (items of 128 or 256 rows, fp32 64). */
 int grkv_attend(const grkv_cache_params* p, const void* q, const void* k_pages, const void* v_pages,
                 const int32_t* table, const int32_t* len, const int32_t* q_len, void* out,

@@ -16,8 +16,8 @@
 //
 // The reference of a row is the maximum of the first tile in which it sees a slot, and stays:
 // P, O and the sum are floating point, so what counts is only that nothing leaves their
-// range.  The first tile's largest P is 1, so no sum underflows; and where a later tile's sum
-// exceeds 2^60 the row takes that tile's maximum, the tile is done again and the output
+// range.  The first tile's largest P is 1, so no sum underflows; and where a later tile takes a row's
+// sum past 2^60 the row takes that tile's maximum, the tile is done again and the output
 // scaled in TMEM.  A running maximum costs 64 three-operand maxima per row and tile in front of
 // the exponentials (half their time), and now and then the output's rescaling.
 // The exponents come from one fused logit x scale - reference, in which the product is exact and the
@@ -63,7 +63,7 @@ constexpr int kRing = 4;   // tiles in flight: K in the even slots, V in the odd
 constexpr long long kWaitBudget = 1ll << 32;                  // cycles (~2 s)
 constexpr int kMaxEdges = 16;   // masked tiles of a segment: at most 4 at each end of the
                                 // window (256 tokens) and one at the sinks' end
-constexpr float kMaxSum = 0x1p60f;   // of a row's P over one tile
+constexpr float kMaxSum = 0x1p60f;   // of a row's P over a segment (a NaN stays as it is)
 constexpr float kBigRef = 0x1p23f;   // references from here on are rounded by more than 1/2
 constexpr int kFewRows = 64;   // up to which P keeps its low part in a segment's first tile
 constexpr uint32_t kColO = 256; // TMEM: two S buffers, then two outputs
@@ -634,7 +634,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
           }
           // Such rows take the maximum; true: some reference is large, P has been formed.
           auto new_ref = [&](float top) -> bool {
-            const bool need = live && (ref == -INFINITY || !(sum < kMaxSum));
+            const bool need = live && (ref == -INFINITY || sum + l >= kMaxSum);
             const float before = ref, to = fmaxf(ref, top * a.sl2);
             if (need && ref != -INFINITY) f = fast_exp2(ref - to);
             if (need) ref = to;
@@ -692,7 +692,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
 #pragma unroll
               for (int c = 1; c < 4; ++c) exp32<false>(v + 32 * c, a.sl2, r, pk + 16 * c, acc);
               sum = total(acc);
-              look = __any_sync(0xffffffffu, live && !(sum < kMaxSum));
+              look = __any_sync(0xffffffffu, live && sum + l >= kMaxSum);
               if (again || !look) break;
             }
             if (!formed) {

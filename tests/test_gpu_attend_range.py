@@ -69,3 +69,34 @@ def test_finite_logits_of_any_size(grkv_lib, dtype, flags, g, t, power, sign):
         assert (off <= tol).all(), f"cache {c}: {(~(off <= tol)).sum().item()} off"
         # scale, product, ln 2 and the sum: 8 roundings of lse itself
         assert ((lse[c::3].double() - z).abs() <= 8 * R.U32 * z.abs() + rel).all()
+
+
+@pytest.mark.parametrize("dtype,flags", TYPES)
+@pytest.mark.parametrize("g,t", ROWS)
+def test_many_tiles_of_large_probabilities(grkv_lib, dtype, flags, g, t):
+    """Outputs before their division stay within 2^60 times the values for a whole run of tiles.  Units of
+    1200 slot tiles, a few to a CTA: the first tile's logits are 0, all others' 52.5 log2 units above,
+    2^59.5 a tile, and their values 2^59: 1200 such tiles would be 2^128.7."""
+    tiles, page, units = 1200, 128, 304
+    n, dt = tiles * page, R.TORCH[dtype]
+    k = torch.zeros(2, page, D, dtype=dt, device="cuda")
+    v = torch.ones(2, page, D, dtype=dt, device="cuda")
+    k[1, :, 3], v[1] = 7, 2.0 ** 59
+    q = torch.zeros(units, g, t, D, dtype=dt, device="cuda")
+    q[..., 3] = 7.5
+    table = torch.ones(units, tiles, dtype=torch.int32, device="cuda")
+    table[:, 0] = 0
+    lens = torch.full((units,), n, dtype=torch.int32, device="cuda")
+    p = b.cache_params(units, g, 2, page, tiles, tokens=t, dtype=dtype, flags=flags,
+                       scale=math.log(2.0))
+    out, lse = torch.zeros_like(q), torch.zeros(units, g, t, dtype=torch.float32, device="cuda")
+    ws = torch.empty(b.grkv_cache_workspace_size(p), dtype=torch.uint8, device="cuda")
+    b.grkv_attend(p, q, k, v, table, lens, out, ws, lse=lse)
+    assert b.grkv_status(ws) == b.GRKV_OK
+    # logits are exact, the scale 2 u off: 2 x 37 x 2 u a probability; n fp32 sums; P and out in bf16
+    rel = 2 * 37 * 2 * R.U32 + (n + 64) * R.U32 + 2.0 ** -21
+    tol = rel + (2.0 ** -8 if dtype == "bf16" else 0) + R.ROUND[dtype]
+    assert ((out.double() / 2.0 ** 59 - 1).abs() <= tol).all()
+    seen = n - t + 1 + torch.arange(t, device="cuda", dtype=torch.float64) - page
+    z = torch.log(seen * 2.0 ** 52.5 + page)
+    assert ((lse.double() - z).abs() <= rel + 4 * R.U32 * z).all()
