@@ -105,6 +105,7 @@ extern "C" {
                                     read of q, k and v */
 #define GRKV_TEST_TIMEOUT 0x80000000u /* tests only: exercises the exit of the bounded device
                                     waits.  In the tensor-core scoring kernels (either path)
+                                    and the tensor-core attention over the paged cache
                                     the first CTA withholds one arrive and the waits' budget
                                     is cut to ~2 ms: the kernel gives up, frees its tensor
                                     memory, returns, and grkv_status reports
@@ -302,7 +303,7 @@ typedef struct {
   int32_t n_sink;     /* s >= 0: first slots that a window leaves visible (4)         */
   float   scale;      /* logit scale; 0 -> fp32(1/sqrt(d))                            */
   int32_t dtype;      /* GRKV_BF16 or GRKV_F32 for rows, queries and outputs          */
-  uint32_t flags;     /* GRKV_FORCE_SIMT                                              */
+  uint32_t flags;     /* GRKV_FORCE_SIMT, GRKV_TEST_TIMEOUT                           */
 } grkv_cache_params;
 
 /* Fills `p` with the defaults above for the given sizes (bf16, one token, no window). */

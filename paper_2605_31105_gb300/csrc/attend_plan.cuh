@@ -39,6 +39,7 @@ struct AttendArgs {
   float2* pml;
   float* po;
   int* status;
+  int withhold;   // GRKV_TEST_TIMEOUT: CTA 0 withholds one arrive (tensor cores)
 };
 
 // One item: tokens [tok0, tok0 + ntok) of unit u; the slots that its rows see are in

@@ -15,6 +15,7 @@ struct CacheShape {
   int P, page, shift, cols;   // pool pages, slots per page (1 << shift), table columns
   int W, s;                   // window (0: every earlier slot) and sinks
   int dtype, simt;
+  int test_timeout;           // GRKV_TEST_TIMEOUT (tests of the bounded-wait exit)
   float scale;
 };
 

@@ -44,7 +44,7 @@ int make_cache_shape(const grkv_cache_params* p, CacheShape* s) {
     return GRKV_ERR_INVALID_ARG;
   if (!(p->scale >= 0.f) || std::isinf(p->scale)) return GRKV_ERR_INVALID_ARG;
   if (p->dtype != GRKV_F32 && p->dtype != GRKV_BF16) return GRKV_ERR_INVALID_ARG;
-  if (p->flags & ~GRKV_FORCE_SIMT) return GRKV_ERR_INVALID_ARG;
+  if (p->flags & ~(GRKV_FORCE_SIMT | GRKV_TEST_TIMEOUT)) return GRKV_ERR_INVALID_ARG;
   if (p->d != kD || p->group > kMaxCacheGroup) return GRKV_ERR_UNSUPPORTED;
   if (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128)
     return GRKV_ERR_UNSUPPORTED;
@@ -67,6 +67,7 @@ int make_cache_shape(const grkv_cache_params* p, CacheShape* s) {
   s->s = std::min(p->n_sink, 1 << 29);
   s->dtype = p->dtype;
   s->simt = (p->flags & GRKV_FORCE_SIMT) ? 1 : 0;
+  s->test_timeout = (p->flags & GRKV_TEST_TIMEOUT) ? 1 : 0;
   s->scale = p->scale != 0.f ? p->scale : (float)(1.0 / std::sqrt((double)p->d));
   return GRKV_OK;
 }
