@@ -70,3 +70,42 @@ def test_rows_behind_a_full_table_are_not_written_over_others(grkv_lib, dtype):
                 at = R.at(c.table, u, n - m + i, page)
                 c.k[at], c.v[at] = kn[u, i], vn[u, i]
     d.same()
+
+
+@pytest.mark.parametrize("units,page", [(1, 16), (7, 16), (60, 32), (1024, 16), (1500, 16)])
+def test_reserve_of_many_columns(grkv_lib, units, page):
+    """A prompt's or a compressed cache's first reserve, and more than 32 columns behind shared pages:
+    decisions are marked in the table whatever the number of units."""
+    rng = np.random.default_rng(units)
+    cols = 90 if units <= 60 else 40
+    lens = rng.integers(0, 30 * page, units)
+    lens[::3] = 0
+    want = np.minimum(lens + rng.integers(0, (cols - 30) * page, units), cols * page)
+    want[0] = cols * page
+    table = np.full((units, cols), -1, np.int32)
+    pages = units * cols + 50
+    order = rng.permutation(pages)
+    at = 0
+    for u in range(units):
+        m = R.pages_of(int(lens[u]), page)
+        table[u, :m] = order[at:at + m]
+        at += m
+        if u % 4 == 1 and m:        # a fork of the unit before: shares what that one has
+            p = R.pages_of(int(lens[u - 1]), page)
+            lens[u] = min(lens[u - 1], want[u])
+            table[u] = -1
+            table[u, :R.pages_of(int(lens[u]), page)] = table[u - 1, :R.pages_of(int(lens[u]), page)]
+    refs = np.bincount(table[table >= 0], minlength=pages).astype(np.int32)
+    refs[rng.integers(0, pages, 20)] += 1                    # another table's
+    k = rng.integers(-50, 50, (pages, page, 4)).astype(np.float64)
+    v = k + 1
+    p = b.cache_params(units, 1, pages, page, cols)
+    ws = torch.empty(b.grkv_cache_workspace_size(p), dtype=torch.uint8, device="cuda")
+    dk, dv = (torch.from_numpy(np.repeat(x, 32, 2)).bfloat16().cuda() for x in (k, v))
+    dt, dr = R.int_dev(table), R.int_dev(refs)
+    b.grkv_cache_reserve(p, dt, R.int_dev(lens), R.int_dev(want), dr, dk, dv, ws)
+    assert b.grkv_status(ws) == b.GRKV_OK
+    assert R.reserve(table, lens, want, refs, k, v, page)
+    assert np.array_equal(dt.cpu().numpy(), table) and np.array_equal(dr.cpu().numpy(), refs)
+    assert np.array_equal(dk.double().cpu().numpy(), np.repeat(k, 32, 2))
+    assert np.array_equal(dv.double().cpu().numpy(), np.repeat(v, 32, 2))
