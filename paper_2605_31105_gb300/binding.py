@@ -290,7 +290,8 @@ def _types_of(call, dtype):
     return types
 
 
-def _fault(call, at, t, want, dev, need):
+def _fault(call, at, t, want, need):
+    import torch
     name = _CALLS[call].split()[at].split(":")[0]
     if t.dtype != want:
         return f"{name} is {t.dtype}, the call takes {want}"
@@ -298,7 +299,8 @@ def _fault(call, at, t, want, dev, need):
         return f"{name} is not contiguous"
     if t.numel() < need:
         return f"{name} holds {t.numel()} elements, the call takes {need}"
-    return f"{name} is on {t.device}, the workspace on device {dev}"
+    where = "a CUDA device" if t.get_device() < 0 else f"device {torch.cuda.current_device()}"
+    return f"{name} is on {t.device}, the call runs on {where}"
 
 
 def _addresses(call, p, ws, ws_bytes, stream, tensors, needs):
@@ -324,9 +326,9 @@ def _addresses(call, p, ws, ws_bytes, stream, tensors, needs):
     for t, want, need in zip(tensors, types, needs):
         if t is not None and type(t) is not int:
             at = t.get_device()
-            if (t.dtype is not want or at < 0 or (at != dev and dev is not None)
-                    or t.numel() < need or not t.is_contiguous()):
-                raise ValueError(_fault(call, len(out), t, want, dev, need))
+            if (t.dtype is not want or at < 0 or t.numel() < need or not t.is_contiguous()
+                    or (at != dev and (dev is not None or at != torch.cuda.current_device()))):
+                raise ValueError(_fault(call, len(out), t, want, need))
             t = t.data_ptr()
         out.append(t)
     if stream is None:

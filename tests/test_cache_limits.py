@@ -31,3 +31,39 @@ def test_a_workspace_serves_calls_of_fewer_tokens(lib, dtype, flags):  # noqa: F
     for group in (1, 2, 3, 4, 5, 7, 8, 11, 16, 21, 32, 33, 64):
         sizes = [size(group=group, tokens=t, dtype=dtype, flags=flags) for t in range(1, 301)]
         assert sizes == sorted(sizes), group
+
+
+class _OnDevice:
+    """What the binding asks of a tensor, on a device of a machine that has two."""
+
+    def __init__(self, device, dtype, n=1 << 20):
+        import torch
+        self.at, self.dtype, self.n = device, dtype, n
+        self.device = torch.device("cuda", device)
+
+    get_device = lambda self: self.at
+    numel = lambda self: self.n
+    is_contiguous = lambda self: True
+    data_ptr = lambda self: 1 << 20
+    element_size = lambda self: 1
+
+
+@pytest.mark.parametrize("ws_is_tensor", [True, False])
+def test_tensors_of_another_device_are_refused(lib, monkeypatch, ws_is_tensor):  # noqa: F811
+    """With the workspace given as a tensor, and as an address."""
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    p = b.cache_params(2, 4, 8, 64, 4)
+    ws = _OnDevice(0, torch.uint8, 1 << 30) if ws_is_tensor else 1 << 20
+    x, i = (lambda d: _OnDevice(d, torch.bfloat16)), (lambda d: _OnDevice(d, torch.int32))
+    # a workspace that is too small ends the calls that the binding lets through, on the host
+    kw = dict(ws_bytes=1, stream=0)
+    with pytest.raises(b.GrkvError):
+        b.grkv_attend(p, x(0), x(0), x(0), i(0), i(0), x(0), ws, **kw)
+    for at in range(6):
+        d = [0] * 6
+        d[at] = 1
+        with pytest.raises(ValueError, match="on cuda:1, the call runs on device 0"):
+            b.grkv_attend(p, x(d[0]), x(d[1]), x(d[2]), i(d[3]), i(d[4]), x(d[5]), ws, **kw)
+    with pytest.raises(ValueError, match="refs is on cuda:1"):
+        b.grkv_cache_trim(p, i(0), i(0), i(1), ws, **kw)
