@@ -387,14 +387,19 @@ def grkv_cache_trim(p, table, lens, refs, ws, ws_bytes=None, stream=None, check=
 
 
 def grkv_cache_append(p, k_new, v_new, k_pages, v_pages, table, lens, ws, count=None,
-                      first_row=None, ws_bytes=None, stream=None, check=True):
+                      first_row=None, ws_bytes=None, stream=None, check=True, new_rows=None):
     """New rows to the last `count` of the `lens` slots of every unit.  With first_row the rows
-    are packed: unit u's start at row first_row[u] of k_new and v_new."""
+    are packed: unit u's start at row first_row[u] of k_new and v_new, which hold new_rows of them
+    (to be given where one of the two is an address; else what both hold)."""
     u, d = p.units, p.d
-    n, need, new_rows = p.pages * p.page * d, u * p.tokens * d, 0
-    if first_row is not None:   # rows of both arrays that the packed form may name
-        new_rows = u * p.tokens if isinstance(k_new, int) else min(
-            k_new.numel(), v_new.numel()) // d
+    n, need = p.pages * p.page * d, u * p.tokens * d
+    if first_row is None:
+        new_rows = 0
+    else:
+        if new_rows is None:
+            if type(k_new) is int or type(v_new) is int:
+                raise ValueError("new_rows is not given: packed rows at an address have no size")
+            new_rows = min(k_new.numel(), v_new.numel()) // d
         need = new_rows * d
     (kn, vn, k, v, t, le, c, f), w, nb, st = _addresses(
         "append", p, ws, ws_bytes, stream,

@@ -67,3 +67,30 @@ def test_tensors_of_another_device_are_refused(lib, monkeypatch, ws_is_tensor): 
             b.grkv_attend(p, x(d[0]), x(d[1]), x(d[2]), i(d[3]), i(d[4]), x(d[5]), ws, **kw)
     with pytest.raises(ValueError, match="refs is on cuda:1"):
         b.grkv_cache_trim(p, i(0), i(0), i(1), ws, **kw)
+
+
+def test_packed_rows_at_an_address_need_their_number(lib, monkeypatch):  # noqa: F811
+    """The library bounds first_row by new_rows: a number that is not known is not made up."""
+    import ctypes
+
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    seen = []
+
+    class Lib:
+        def grkv_cache_append(self, *a):
+            seen.append(ctypes.c_int64(a[4]).value)
+            return b.GRKV_OK
+
+    p = b.cache_params(2, 4, 8, 64, 4, tokens=100)
+    monkeypatch.setattr(b, "load", lambda: Lib())
+    f, kw = 1 << 20, dict(ws_bytes=1, stream=0, first_row=1 << 20)
+    rows = lambda n: _OnDevice(0, torch.bfloat16, n * 128)
+    for k, v in ((f, f), (rows(70), f), (f, rows(70))):
+        with pytest.raises(ValueError, match="new_rows"):
+            b.grkv_cache_append(p, k, v, f, f, f, f, f, **kw)
+        b.grkv_cache_append(p, k, v, f, f, f, f, f, new_rows=64, **kw)
+    b.grkv_cache_append(p, rows(70), rows(71), f, f, f, f, f, **kw)
+    with pytest.raises(ValueError, match="v_new holds"):
+        b.grkv_cache_append(p, rows(70), rows(50), f, f, f, f, f, new_rows=64, **kw)
+    assert seen == [64, 64, 64, 70]
