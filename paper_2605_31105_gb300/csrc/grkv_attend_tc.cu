@@ -164,25 +164,17 @@ __device__ __forceinline__ void exp32(const float* v, float sl2, float r, uint32
   }
 }
 
-__device__ __forceinline__ float total(const uint64_t* acc) {
-  float s0, s1;
-  unpack2(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), s0, s1);
-  return s0 + s1;
-}
-
-// P of a slot tile where some row of the warp has a large reference: every row takes the maximum
-// `top`, and P, both parts, goes over the logits that it comes from.  Exponents in rows with large
-// references are bounded by 0, a NaN stays (all lanes of the warp; rare, so not in line).
+// Where some row of the warp has a large reference: every row takes the maximum `top`, and the logits
+// of those with large ones become their exponents, bounded by 0, over the scale, so that the code that
+// follows takes them against 0; a NaN stays (all lanes of the warp; rare, so not in line).
 struct Followed {
-  float sum, ref, f;   // of P; the new reference; what the row's output so far is multiplied by
+  float ref, f;   // the new reference; what the row's output so far is multiplied by
 };
 __device__ __noinline__ Followed follow_row(uint32_t s_addr, float sl2, float top, float ref) {
   float to = top * sl2;
   if (!(fabsf(to) < kBigRef)) to = __fmul_rd(top, sl2);
   to = fmaxf(ref, to);
-  Followed y{0.f, to, ref == -INFINITY ? 1.f : fast_exp2(ref - to)};
-  const float r = to == -INFINITY ? 0.f : to;
-  const bool big = !(fabsf(r) < kBigRef);
+  const bool big = to != -INFINITY && !(fabsf(to) < kBigRef);
 #pragma unroll 1
   for (int c = 0; c < 4; ++c) {
     float v[32];
@@ -190,18 +182,18 @@ __device__ __noinline__ Followed follow_row(uint32_t s_addr, float sl2, float to
     tmem_wait32(v);
 #pragma unroll
     for (int x = 0; x < 32; ++x) {
-      const float t = fmaf(v[x], sl2, -r);
-      v[x] = big && t > 0.f ? 0.f : t;
+      const float t = fmaf(v[x], sl2, -to);
+      if (big) v[x] = (t > 0.f ? 0.f : t) / sl2;
     }
-    uint32_t pk[32];
-    uint64_t acc[4] = {0, 0, 0, 0};
-    exp32<true>(v, 1.f, 0.f, pk, acc);
-    y.sum += total(acc);
-    tmem_st16(s_addr + 32 * c, pk);
-    tmem_st16(s_addr + 32 * c + 16, pk + 16);
+    tmem_st16(s_addr + 32 * c, (uint32_t*)v);
+    tmem_st16(s_addr + 32 * c + 16, (uint32_t*)v + 16);
   }
-  return y;
+  tmem_st_wait();
+  return Followed{to, ref == -INFINITY ? 1.f : fast_exp2(ref - to)};
 }
+
+// What the exponents are taken against: 0 for a row without a reference or with a large one.
+__device__ __forceinline__ float against(float ref) { return fabsf(ref) < kBigRef ? ref : 0.f; }
 
 // Multiplies a row's output by f (all lanes of the warp; rare, so not in line).
 __device__ __noinline__ void scale_row(uint32_t o_addr, float f) {
@@ -642,7 +634,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
             }
             tmem_st_wait();
           }
-          // Such rows take the maximum; true: some reference is large, P has been formed.
+          // Such rows take the maximum; true: some reference is large, the logits have been changed.
           auto new_ref = [&](float top) -> bool {
             const bool need = live && (ref == -INFINITY || sum + l >= kMaxSum);
             const float before = ref, to = fmaxf(ref, top * a.sl2);
@@ -652,10 +644,14 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
             if (!follow || !__any_sync(0xffffffffu, live && ref != -INFINITY && !(fabsf(ref) < kBigRef)))
               return false;
             const Followed y = follow_row(lane_addr + scol, a.sl2, top, before);
-            sum = y.sum;
             ref = y.ref;
             f = y.f;
             return true;
+          };
+          auto total = [&](const uint64_t* acc) {
+            float s0, s1;
+            unpack2(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), s0, s1);
+            return s0 + s1;
           };
           if (few && k == 0) {
             // both parts of P; a chunk at a time, over the logits that it comes from
@@ -667,19 +663,18 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
               tmem_wait32(v);
               if (c < 4) {
                 top = fmaxf(top, max32(v));
-                if (c == 3 && new_ref(top)) break;
+                if (c == 3) new_ref(top);
                 continue;
               }
               uint32_t pk[32];
               uint64_t acc[4] = {0, 0, 0, 0};
-              exp32<true>(v, a.sl2, ref == -INFINITY ? 0.f : ref, pk, acc);
+              exp32<true>(v, a.sl2, against(ref), pk, acc);
               sum += total(acc);
               tmem_st16(lane_addr + scol + 32 * (c & 3), pk);
               tmem_st16(lane_addr + scol + 32 * (c & 3) + 16, pk + 16);
             }
           } else {
             uint32_t pk[64];
-            bool formed = false;   // P is in TMEM already
 #pragma unroll 1
             for (bool again = false;; again = true) {
               // the first chunk's exponentials run while the others are on their way
@@ -691,10 +686,10 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
               if (look) {
 #pragma unroll
                 for (int c = 1; c < 4; ++c) tmem_wait32(v + 32 * c);
-                formed = new_ref(fmaxf(fmaxf(max32(v), max32(v + 32)), fmaxf(max32(v + 64), max32(v + 96))));
-                if (formed) break;
+                look = false;
+                if (new_ref(fmaxf(fmaxf(max32(v), max32(v + 32)), fmaxf(max32(v + 64), max32(v + 96))))) continue;
               }
-              const float r = ref == -INFINITY ? 0.f : ref;
+              const float r = against(ref);
               uint64_t acc[4] = {0, 0, 0, 0};
               exp32<false>(v, a.sl2, r, pk, acc);
 #pragma unroll
@@ -705,10 +700,8 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
               look = __any_sync(0xffffffffu, live && sum + l >= kMaxSum);
               if (again || !look) break;
             }
-            if (!formed) {
 #pragma unroll
-              for (int c = 0; c < 4; ++c) tmem_st16(lane_addr + scol + 32 * c, pk + 16 * c);
-            }
+            for (int c = 0; c < 4; ++c) tmem_st16(lane_addr + scol + 32 * c, pk + 16 * c);
           }
           if (k > 0 && __any_sync(0xffffffffu, f != 1.f)) {
             ok = done(n - NQ, false);
