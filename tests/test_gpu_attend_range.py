@@ -19,19 +19,23 @@ ROWS = [(5, 1), (6, 2), (50, 1), (50, 2), (60, 5)]
 @pytest.mark.parametrize("g,t", ROWS)
 @pytest.mark.parametrize("power", [22, 26, 31, 40, 100])
 @pytest.mark.parametrize("sign", [1, -1])
-def test_finite_logits_of_any_size(grkv_lib, dtype, flags, g, t, power, sign):
+@pytest.mark.parametrize("late", [False, True])
+def test_finite_logits_of_any_size(grkv_lib, dtype, flags, g, t, power, sign, late):
     """Logits of about +-2^power beside ordinary ones in the same tile.  Queries and keys have one
     element that is not zero, of 8 bits, so that fp32 holds every product exactly; the largest
     logit of a unit is apart from the next by 2^-5 of itself, so its slot (or the two that
     share it) has all the weight.  Units of 6 slot tiles, many more than there are CTAs, with that
-    slot in the first tile, in the last, or in both."""
+    slot in the first tile, in the last, or in both.  late: the first 300 slots' logits are ordinary ones
+    (below all others if those are positive, the largest if they are negative)."""
     n, page, units = 700, 64, 420
     rng = np.random.default_rng(power)
     cols = R.pages_of(n, page)
     key = 1 + rng.integers(4, 120, (3, n)) / 128.0           # in [1 + 2^-5, 2 - 2^-4]
     top = 1 if sign < 0 else 2 - 1 / 128                     # the largest times a query below or above 0
-    for c, slots in enumerate(([17], [680], [40, 690])):
+    for c, slots in enumerate(([317 if late else 17], [680], [340 if late else 40, 690])):
         key[c, slots] = top
+    if late:
+        key[:, :300] *= 2.0 ** -power
     head = 1 + rng.integers(0, 128, (units, g, t)) / 128.0
     head *= sign * 2.0 ** (power // 2)
     plain = rng.random((units, g, t)) < 0.25                 # ordinary logits
@@ -61,7 +65,7 @@ def test_finite_logits_of_any_size(grkv_lib, dtype, flags, g, t, power, sign):
         vv = v.view(3, -1, D)[c, :n].double()
         w = torch.softmax(x, -1)
         o, mass, z = w @ vv, w @ vv.abs(), torch.logsumexp(x, -1)
-        # Ordinary rows: |x| < 0.09 x 4 x 2, off by 4 u of itself; the others' weights are 0 or
+        # Ordinary logits: |x| < 0.09 x 4 x 2, off by 4 u of itself; the others' weights are 0 or
         # shared, whatever the logits' last bits.  Then the exponential, n fp32 sums, P in bf16.
         rel = 2 * 4 * R.U32 * 0.75 + (n + 64) * R.U32 + 2.0 ** -21
         tol = (rel + (2.0 ** -8 if dtype == "bf16" else 0)) * mass + R.ROUND[dtype] * o.abs()
