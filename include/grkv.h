@@ -368,10 +368,14 @@ int grkv_cache_compact(const grkv_cache_params* p, const int32_t* idx, const int
  * they were.  Slots that a row does not see do not reach it, whatever they hold,
  * and a page without a slot that some row of its unit sees is not read: its entry may be negative.
  * t = 1 is decoding, larger t a chunk of prefill.  Sums are fp32; bf16 rounds the
- * unnormalised probabilities to bf16 for the product with V.  Where a slot that a row sees
+ * unnormalised probabilities to bf16 for the product with V (by 2^-8 of each at most; with
+ * up to 64 rows g t what that leaves of the first tile of 128 slots that a CTA takes of a unit is
+ * multiplied too), which GRKV_FORCE_SIMT does not.  Where a slot that a row sees
  * holds NaN or infinity, that row's elements come out non-finite (an infinity may come out
  * as NaN).  bf16 holds unnormalised outputs of up to 2^68 times a row's values (2^60 in each
- * of a unit's parts), which must stay within fp32.  Results do not change from run to run.  GRKV_ERR_UNSUPPORTED for a call
+ * of a unit's parts), fp32 and GRKV_FORCE_SIMT of up to their number times the values, which must
+ * stay within fp32.  Results do not change from run to run; a row's last bits may change with t,
+ * g and the lengths of the other units.  GRKV_ERR_UNSUPPORTED for a call
  * that could read more than 2^36 tiles of 128 slots (items of 128 or 256 rows, fp32 64). */
 int grkv_attend(const grkv_cache_params* p, const void* q, const void* k_pages, const void* v_pages,
                 const int32_t* table, const int32_t* len, const int32_t* q_len, void* out,

@@ -23,22 +23,27 @@
 // The exponents come from one fused logit x scale - reference, in which the product is exact and the
 // reference rounded: from 2^23 on by more than 1/2, and in the end by more than an exponent
 // holds.  A row with such a reference follows the running maximum, rounded down, and its exponents are
-// bounded by 0: logits that fp32 cannot tell from the maximum weigh as much as it.
+// bounded by 0: logits that fp32 cannot tell from the maximum weigh as much as it.  That is done to the
+// logits in TMEM, by code that such rows alone reach: in line it cost windowed trees and
+// prompts 2%.  The tests and the sum over the whole run cost the chunk below 328 -> 334 us.
 //
 // P is rounded to bf16 for the product with V: a relative 2^-8 a term at most, of the size of
-// the output's own rounding.  The outputs of few rows may rest on few probabilities, whose
-// roundings do not average, and those are mostly in the tile that gave the reference (a
-// cache's sinks).  So items of up to 64 rows (every single token) take two products for the
-// first slot tile of a segment, with P's rounding and with what that left: one query over 64
-// units of up to 16384 slots takes 59 us against 57 (for every tile 65; 256 units of 32768:
-// 680 against 624).  Items of more rows round once: trees of 65 rows over 128 units take
-// 43.7 us against 45.5.  A row's sum is taken in fp32 before that.
+// the output's own rounding.  A row's sum is taken in fp32 before that.  A second product with
+// what the rounding left, 512 cycles and the packing, is made where it is nearly free: in the first
+// slot tile of a segment (with a cache's sinks, if that is where a unit starts) of items of up to
+// 64 rows, which wait for memory: one query over 64 units of up to 16384 slots took 59 us
+// against 57 (for every tile 65; 256 units of 32768: 680 against 624).  Items of more rows wait for the
+// MMAs and the softmax and round once: trees of 65 rows over 128 units took 43.7 us against
+// 45.5.  So a row's error depends on how many rows its call has a unit, and on where the split over
+// the CTAs falls: 0.0017 (both parts, the size of the output's rounding) to 0.0020 of the outputs' size, within
+// 2^-8 of sum p |v| in every case.
 //
 // What bounds it (one GB300).  Few rows over a long cache: memory, 256 units of 32768 slots in
-// 615 us, 7.0 TB/s.  Chunks of prefill: a row tile's chain of S (512 cycles), softmax (1.2 K with two
-// warps to a scheduler) and P V (512), which two row tiles overlap: 2.95 K cycles a slot tile against
-// 2 K of MMAs; 2048 queries of 32 heads over 16384 slots take 329 us, 1.57 PFLOP/s.  Windows and trees:
-// items are short, and each has a start and an end (8 K cycles) and tiles with masks (2 K more).
+// 625 us, 6.9 TB/s.  Chunks of prefill: a row tile's chain of S (512 cycles), softmax (1.2 K with two
+// warps to a scheduler) and P V (512), which two row tiles overlap: 3.0 K cycles a slot tile against
+// 2 K of MMAs; 2048 queries of 32 heads over 16384 slots take 334 us, 1.54 PFLOP/s, at 2070 MHz, and 357 us
+// call after call for a second and more, when the power limit holds the clock at 1.94 to 1.97 GHz.  Windows
+// and trees: items are short, and each has a start and an end (8 K cycles) and tiles with masks (2 K more).
 //
 // Slot tiles that every row sees whole take no masks.  In the others the masks of a row are
 // four words, and V is searched for non-finite elements first: they are set to zero
@@ -618,7 +623,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
           if (masked) {
             // -inf, in TMEM, for the slots that a row does not see: one chunk's code, for the
             // chunks that some row of the warp does not see whole.  (In line with the
-            // exponentials, 128 selects more to fetch: the chunk above took 350 us, not 329.)
+            // exponentials, 128 selects more to fetch: the chunk above took 350 us where it took 329.)
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
               const uint32_t m = vis.word(tile * kSlotTile + 32 * c);
@@ -687,7 +692,8 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
 #pragma unroll
                 for (int c = 1; c < 4; ++c) tmem_wait32(v + 32 * c);
                 look = false;
-                if (new_ref(fmaxf(fmaxf(max32(v), max32(v + 32)), fmaxf(max32(v + 64), max32(v + 96))))) continue;
+                if (new_ref(fmaxf(fmaxf(max32(v), max32(v + 32)), fmaxf(max32(v + 64), max32(v + 96)))))
+                  continue;   // with the changed logits
               }
               const float r = against(ref);
               uint64_t acc[4] = {0, 0, 0, 0};
