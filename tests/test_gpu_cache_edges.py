@@ -109,3 +109,135 @@ def test_reserve_of_many_columns(grkv_lib, units, page):
     assert np.array_equal(dt.cpu().numpy(), table) and np.array_equal(dr.cpu().numpy(), refs)
     assert np.array_equal(dk.double().cpu().numpy(), np.repeat(k, 32, 2))
     assert np.array_equal(dv.double().cpu().numpy(), np.repeat(v, 32, 2))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_units_than_a_grid_has_rows(grkv_lib, dtype):
+    """Every page operator over 70000 units (grids of 65535 rows go round), then attention."""
+    units, page, cols, spare = 70000, 16, 2, 9
+    rng = np.random.default_rng(11)
+    lens = rng.integers(0, 2 * page, units).astype(np.int32)
+    want = np.minimum(lens + rng.integers(0, 3, units), cols * page).astype(np.int32)
+    pages = units * cols + spare
+    dt = R.TORCH[dtype]
+    p = b.cache_params(units, 2, pages, page, cols, tokens=2, dtype=dtype)
+    ws = torch.empty(b.grkv_cache_workspace_size(p), dtype=torch.uint8, device="cuda")
+    ok = lambda: b.grkv_status(ws) == b.GRKV_OK
+    dk, dv = (torch.zeros(pages, page, D, dtype=dt, device="cuda") for _ in range(2))
+    table = torch.full((units, cols), -1, dtype=torch.int32, device="cuda")
+    refs = torch.zeros(pages, dtype=torch.int32, device="cuda")
+    zero, dl, dw = torch.zeros(units, dtype=torch.int32, device="cuda"), R.int_dev(lens), R.int_dev(want)
+    for have, to in ((zero, dl), (dl, dw)):
+        b.grkv_cache_reserve(p, table, have, to, refs, dk, dv, ws)
+        assert ok()
+    t_ref, r_ref = np.full((units, cols), -1, np.int32), np.zeros(pages, np.int32)
+    none = np.zeros((pages, 1, 1))
+    assert R.reserve(t_ref, np.zeros(units, int), lens, r_ref, none, none, page)
+    assert R.reserve(t_ref, lens, want, r_ref, none, none, page)
+    assert np.array_equal(table.cpu().numpy(), t_ref) and np.array_equal(refs.cpu().numpy(), r_ref)
+    # a row's elements say whose it is; its values, which of the unit's
+    slot = torch.arange(cols * page, device="cuda")
+    at = (table.long().clamp_min(0)[:, slot // page] * page + slot % page)
+    live = slot[None] < dw[:, None]
+    dk.view(-1, D)[at[live]] = (torch.arange(units, device="cuda") % 61)[:, None].expand_as(live)[live][:, None].to(dt)
+    dv.view(-1, D)[at[live]] = slot[None].expand_as(live)[live][:, None].to(dt)
+    new = torch.full((units, 2, D), 40, dtype=dt, device="cuda")
+    count = dw - dl
+    b.grkv_cache_append(p, new, new, dk, dv, table, dw, ws, count=count)
+    assert ok()
+    got = dv.view(-1, D)[at][..., 5].float()
+    assert torch.equal(got[live], torch.where(slot[None] >= dl[:, None], 40.0, slot[None].float())[live])
+    # equal logits: the mean of a unit's values
+    q = torch.zeros(units, 2, 1, D, dtype=dt, device="cuda")
+    p1 = b.cache_params(units, 2, pages, page, cols, dtype=dtype)
+    out = torch.full_like(q, 7)
+    b.grkv_attend(p1, q, dk, dv, table, dw, out, ws)
+    assert ok()
+    total = (torch.where(live, got, 0.0)).double().sum(1)
+    mean = torch.where(dw > 0, total / dw.clamp_min(1), 0.0)
+    assert ((out[:, :, 0, 77].double() - mean[:, None]).abs() <= mean[:, None] * (2.0 ** -8 + 2.0 ** -19)).all()
+    # the last slot of every unit to its first place, then the fork of all and the end of all
+    keep = (dw > 0).int()
+    b.grkv_cache_compact(p1, (dw - 1).clamp_min(0)[:, None].contiguous(), dk, dv, table, dw, table, ws, keep=keep)
+    assert ok()
+    has = dw > 0
+    last = got.gather(1, (dw.long() - 1).clamp_min(0)[:, None])[:, 0]
+    assert torch.equal(dv.view(-1, D)[at[:, 0]][:, 127].float()[has], last[has])
+    t2, l2 = torch.empty_like(table), torch.empty_like(dw)
+    b.grkv_cache_fork(p1, torch.arange(units, device="cuda").flip(0).int(), table, keep, t2, l2, refs, ws)
+    assert ok()
+    assert torch.equal(l2, keep.flip(0)) and torch.equal(t2[:, 0], torch.where(keep > 0, table[:, 0], -1).flip(0))
+    for tb in (table, t2):
+        b.grkv_cache_trim(p1, tb, zero, refs, ws)
+        assert ok() and (tb == -1).all()
+    assert (refs == 0).all()
+
+
+@pytest.mark.parametrize("dtype,flags", [("bf16", 0), ("f32", 0)])
+def test_a_captured_step_is_replayed(grkv_lib, dtype, flags):
+    """Reserve, append, attention and the lengths' step in one graph, replayed token after token, against
+    the same calls made one by one; other work of the same kind runs beside it."""
+    units, g, page, cols, steps = 6, 4, 16, 6, 20
+    start = [0, 15, 16, 31, 40, 63]
+    dt = R.TORCH[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    rnd = lambda *s: torch.randn(*s, dtype=torch.float32, device="cuda", generator=gen).to(dt)
+    kn, vn, qn = rnd(steps, units, 1, D), rnd(steps, units, 1, D), rnd(steps, units, g, 1, D)
+    pages = units * cols
+    p = b.cache_params(units, g, pages, page, cols, dtype=dtype, flags=flags)
+    k0, v0 = rnd(pages, page, D), rnd(pages, page, D)
+
+    class Side:
+        def __init__(self):
+            self.k, self.v = k0.clone(), v0.clone()
+            self.table = torch.full((units, cols), -1, dtype=torch.int32, device="cuda")
+            self.refs = torch.zeros(pages, dtype=torch.int32, device="cuda")
+            self.lens, self.now = R.int_dev(start), torch.zeros(units, dtype=torch.int32, device="cuda")
+            self.ws = torch.empty(b.grkv_cache_workspace_size(p), dtype=torch.uint8, device="cuda")
+            self.x = [torch.empty_like(t[0]) for t in (kn, vn, qn)]
+            self.out = torch.zeros_like(qn[0])
+            b.grkv_cache_reserve(p, self.table, torch.zeros_like(self.lens), self.lens, self.refs, self.k,
+                                 self.v, self.ws)
+            assert b.grkv_status(self.ws) == b.GRKV_OK
+
+        def step(self):
+            torch.add(self.lens, 1, out=self.now)
+            b.grkv_cache_reserve(p, self.table, self.lens, self.now, self.refs, self.k, self.v, self.ws)
+            b.grkv_cache_append(p, self.x[0], self.x[1], self.k, self.v, self.table, self.now, self.ws)
+            b.grkv_attend(p, self.x[2], self.k, self.v, self.table, self.now, self.out, self.ws)
+            self.lens.copy_(self.now)
+
+        def feed(self, i):
+            for to, t in zip(self.x, (kn, vn, qn)):
+                to.copy_(t[i])
+
+    eager, graphed, beside = Side(), Side(), Side()
+    stream, other = torch.cuda.Stream(), torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        graphed.step()
+    torch.cuda.synchronize()
+    for i in range(steps):
+        for side in (eager, graphed, beside):
+            side.feed(i)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            beside.step()
+        with torch.cuda.stream(stream):
+            graph.replay()
+        eager.step()
+        torch.cuda.synchronize()
+        for side in (graphed, beside):
+            assert torch.equal(side.out, eager.out) and torch.equal(side.table, eager.table)
+            assert torch.equal(side.lens, eager.lens) and torch.equal(side.refs, eager.refs)
+    for side in (eager, graphed, beside):
+        assert b.grkv_status(side.ws) == b.GRKV_OK
+    assert torch.equal(graphed.k, eager.k) and torch.equal(graphed.v, eager.v)
+    u = 3
+    rows = eager.table[u].long().repeat_interleave(page) * page + torch.arange(cols * page, device="cuda") % page
+    n = start[u] + steps
+    kk, vv = (t.view(-1, D)[rows[:n]].double().cpu().numpy() for t in (eager.k, eager.v))
+    o, _, mass, err = R.attend_unit(qn[-1, u].double().cpu().numpy(), kk, vv, 1, 0, 4)
+    tol = (2 * err + 2.0 ** -13 + 2.0 ** -8)[..., None] * mass + 2.0 ** -8 * np.abs(o)
+    assert (np.abs(eager.out[u].double().cpu().numpy() - o) <= tol).all()
