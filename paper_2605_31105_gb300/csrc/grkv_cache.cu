@@ -7,35 +7,11 @@
 #include <algorithm>
 #include <cmath>
 
-#include "cache_args.cuh"
+#include "cache_rows.cuh"
 
 using namespace grkv;
 
 namespace {
-
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-int cuda_rc(cudaError_t e) { return e == cudaSuccess ? GRKV_OK : GRKV_ERR_CUDA; }
-
-#define GRKV_TRY(expr)              \
-  do {                              \
-    const int rc_ = (expr);         \
-    if (rc_ != GRKV_OK) return rc_; \
-  } while (0)
-
-// Non-null, and aligned to `align` bytes: 16 for row data and the workspace (moved 16 bytes
-// at a time), an element for the integer arrays, so that a slice of a table or of the
-// lengths (one layer's units) can be passed as it is.
-int check_ptrs(std::initializer_list<const void*> ptrs, uintptr_t align) {
-  for (const void* p : ptrs)
-    if (!p) return GRKV_ERR_INVALID_ARG;
-  for (const void* p : ptrs)
-    if ((uintptr_t)p & (align - 1)) return GRKV_ERR_MISALIGNED;
-  return GRKV_OK;
-}
-// The same for a pointer that may be null.
-int check_optional(const void* p, uintptr_t align) {
-  return ((uintptr_t)p & (align - 1)) ? GRKV_ERR_MISALIGNED : GRKV_OK;
-}
 
 int make_cache_shape(const grkv_cache_params* p, CacheShape* s) {
   if (!p) return GRKV_ERR_INVALID_ARG;
@@ -94,46 +70,20 @@ CacheWs plan_cache_ws(const CacheShape& s) {
   return L;
 }
 
-// Checks that every cache call makes before its own.
-int begin(const grkv_cache_params* p, const void* ws, size_t ws_bytes, CacheShape* s, CacheWs* L) {
+}  // namespace
+
+namespace grkv {
+
+int cache_begin(const grkv_cache_params* p, const void* ws, size_t ws_bytes, CacheShape* s, CacheWs* L) {
   GRKV_TRY(make_cache_shape(p, s));
   *L = plan_cache_ws(*s);
   GRKV_TRY(check_ptrs({ws}, 16));
   return ws_bytes < L->total ? GRKV_ERR_WORKSPACE_TOO_SMALL : GRKV_OK;
 }
 
-int clear_status(char* ws, const CacheWs& L, cudaStream_t st) {
-  return cuda_rc(cudaMemsetAsync(ws + L.status, 0, 4, st));
-}
+}  // namespace grkv
 
-struct Table {
-  int U, cols, P, shift;
-  __host__ __device__ int page() const { return 1 << shift; }
-  // Length clamped to what the table can hold; a length outside sets the status.
-  __device__ int clamped(int len, int* status) const {
-    const int cap = cols << shift;
-    if (len < 0 || len > cap) set_status(status, GRKV_ERR_INVALID_ARG);
-    return min(max(len, 0), cap);
-  }
-};
-
-// The status of a call whose only block writes it whole (solo), which saves the call a memset,
-// or of one whose blocks add their faults to a cleared word.
-struct Status {
-  int* word;
-  int* at;   // where faults go
-  bool solo;
-  __device__ Status(int* word_, int* shared, bool solo_) : word(word_), at(solo_ ? shared : word_), solo(solo_) {
-    if (!solo) return;
-    if (threadIdx.x == 0) *at = 0;
-    __syncthreads();
-  }
-  __device__ void end() const {   // all threads of the block
-    if (!solo) return;
-    __syncthreads();
-    if (threadIdx.x == 0) *word = *at;
-  }
-};
+namespace {
 
 // ------------------------------------------------------------------- fork, trim
 // A thread per table entry.
@@ -347,31 +297,6 @@ __global__ void k_cache_copy(int U, int row16, int page, const int4* __restrict_
 }
 
 // --------------------------------------------------------------- append, compact
-struct RowMove {
-  Table tb;
-  int t;                     // rows per unit
-  const int32_t* count;      // rows of a unit, or null: t
-  const int32_t* len;        // slots of a unit
-  int* status;
-};
-
-// Row index of slot `slot` of unit u in the pool; -1 (and the status) where the table has no page.
-__device__ __forceinline__ long long pool_row(const Table& tb, const int32_t* table, int u,
-                                              int slot, int* status) {
-  const int e = table[(size_t)u * tb.cols + (slot >> tb.shift)];
-  if ((unsigned)e >= (unsigned)tb.P) {
-    set_status(status, GRKV_ERR_INVALID_ARG);
-    return -1;
-  }
-  return ((long long)e << tb.shift) + (slot & (tb.page() - 1));
-}
-__device__ __forceinline__ int rows_of(const RowMove& m, int u) {
-  if (!m.count) return m.t;
-  const int n = m.count[u];
-  if (n < 0 || n > m.t) set_status(m.status, GRKV_ERR_INVALID_ARG);
-  return min(max(n, 0), m.t);
-}
-
 // Copies of rows: a block takes 2 x 128 / kRow16 rows of one unit (grid (blocks of rows, units)),
 // kRow16 lanes a row of kRow16 16-byte chunks, two rows of K and V in flight to a thread.  Bound
 // by memory: 524288 kept rows of K and V (537 MB read and written, rows of 256 bytes from
@@ -439,24 +364,6 @@ __global__ void __launch_bounds__(kMoveThreads)
   });
 }
 
-// Where row i of unit u's kept rows comes from and goes to; false (and the status) if the
-// call's contract is broken there.
-__device__ __forceinline__ bool kept_row(const RowMove& m, const int32_t* idx,
-                                         const int32_t* table_in, int len, const int32_t* table_out,
-                                         const int32_t* first, bool in_place, int u, int i,
-                                         long long* from, long long* to) {
-  const int cap = m.tb.cols << m.tb.shift, f = first ? first[u] : 0, src = idx[(size_t)u * m.t + i];
-  const int dst = min(max(f, 0), cap) + i;
-  if (src < 0 || src >= len || f < 0 || dst >= cap ||
-      (in_place && src < dst)) {
-    set_status(m.status, GRKV_ERR_INVALID_ARG);
-    return false;
-  }
-  *from = pool_row(m.tb, table_in, u, src, m.status);
-  *to = pool_row(m.tb, table_out, u, dst, m.status);
-  return *from >= 0 && *to >= 0;
-}
-
 // To other pages: every row by itself.
 template <int kRow16>
 __global__ void __launch_bounds__(kMoveThreads)
@@ -504,7 +411,6 @@ __global__ void __launch_bounds__(kShiftThreads)
   }
 }
 
-Table table_of(const CacheShape& s) { return Table{s.U, s.cols, s.P, s.shift}; }
 int row16_of(const CacheShape& s) { return kD * (s.dtype == GRKV_F32 ? 4 : 2) / 16; }
 
 // A launch of k_cache_fork or k_cache_trim, 1024 entries a block.  Up to 2 K entries go to one
@@ -536,7 +442,7 @@ int attend(const grkv_cache_params* p, const AttendIo& io, bool tree, void* ws, 
            void* stream) {
   CacheShape s;
   CacheWs L;
-  GRKV_TRY(begin(p, ws, ws_bytes, &s, &L));
+  GRKV_TRY(cache_begin(p, ws, ws_bytes, &s, &L));
   if ((tree && s.t > kMaxTree) || attend_tiles(s) > kMaxAttendTiles) return GRKV_ERR_UNSUPPORTED;
   cudaStream_t st = (cudaStream_t)stream;
   if (s.U == 0) return clear_status((char*)ws, L, st);
@@ -597,7 +503,7 @@ int grkv_cache_fork(const grkv_cache_params* p, int32_t units_in, const int32_t*
                     int32_t* len_out, int32_t* refs, void* ws, size_t ws_bytes, void* stream) {
   CacheShape s;
   CacheWs L;
-  GRKV_TRY(begin(p, ws, ws_bytes, &s, &L));
+  GRKV_TRY(cache_begin(p, ws, ws_bytes, &s, &L));
   if (units_in < 0) return GRKV_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
   if (s.U > 0) {
@@ -614,7 +520,7 @@ int grkv_cache_trim(const grkv_cache_params* p, int32_t* table, const int32_t* l
                     void* ws, size_t ws_bytes, void* stream) {
   CacheShape s;
   CacheWs L;
-  GRKV_TRY(begin(p, ws, ws_bytes, &s, &L));
+  GRKV_TRY(cache_begin(p, ws, ws_bytes, &s, &L));
   if (s.U > 0) GRKV_TRY(check_ptrs({table, len, refs}, 4));
   cudaStream_t st = (cudaStream_t)stream;
   if (s.U == 0) return clear_status((char*)ws, L, st);
@@ -626,7 +532,7 @@ int grkv_cache_reserve(const grkv_cache_params* p, int32_t* table, const int32_t
                        size_t ws_bytes, void* stream) {
   CacheShape s;
   CacheWs L;
-  GRKV_TRY(begin(p, ws, ws_bytes, &s, &L));
+  GRKV_TRY(cache_begin(p, ws, ws_bytes, &s, &L));
   if (s.U > 0) {
     GRKV_TRY(check_ptrs({k_pages, v_pages}, 16));
     GRKV_TRY(check_ptrs({table, len, want, refs}, 4));
@@ -649,7 +555,7 @@ int grkv_cache_append(const grkv_cache_params* p, const void* k_new, const void*
                       void* ws, size_t ws_bytes, void* stream) {
   CacheShape s;
   CacheWs L;
-  GRKV_TRY(begin(p, ws, ws_bytes, &s, &L));
+  GRKV_TRY(cache_begin(p, ws, ws_bytes, &s, &L));
   if (s.U > 0) {
     GRKV_TRY(check_ptrs({k_new, v_new, k_pages, v_pages}, 16));
     GRKV_TRY(check_ptrs({table, len}, 4));
@@ -673,7 +579,7 @@ int grkv_cache_compact(const grkv_cache_params* p, const int32_t* idx, const int
                        size_t ws_bytes, void* stream) {
   CacheShape s;
   CacheWs L;
-  GRKV_TRY(begin(p, ws, ws_bytes, &s, &L));
+  GRKV_TRY(cache_begin(p, ws, ws_bytes, &s, &L));
   if (s.U > 0) {
     GRKV_TRY(check_ptrs({k_pages, v_pages}, 16));
     GRKV_TRY(check_ptrs({idx, table_in, len_in, table_out}, 4));
