@@ -391,6 +391,120 @@ int grkv_attend_tree(const grkv_cache_params* p, const void* q, const void* k_pa
                      const int32_t* q_len, const int32_t* parent, void* out, float* lse, void* ws,
                      size_t ws_bytes, void* stream);
 
+/* Attention over the whole cache of a unit, whatever it holds: an encoder's states, a document that
+ * several sequences read, a cache compressed with causal = 0.  Row i < q_len[u] (NULL: t) of unit u
+ * sees every slot j < len[u]; queries are no slots of the cache, so that q_len and len have nothing
+ * to do with each other.  window and n_sink are not read.  The rest, errors and roundings too, is
+ * grkv_attend's: a unit of length 0 gives out = 0 and lse = -inf, rows from q_len[u] on are left as
+ * they were.  Beams of a sequence, whose caches are one, go into the group. */
+int grkv_attend_cross(const grkv_cache_params* p, const void* q, const void* k_pages,
+                      const void* v_pages, const int32_t* table, const int32_t* len,
+                      const int32_t* q_len, void* out, float* lse, void* ws, size_t ws_bytes,
+                      void* stream);
+
+/* Where the new rows of every unit go.  Row i of the last count[u] (NULL: t) of the len[u] slots of
+ * unit u, len with the new rows, is at
+ *   slot[]  row of the pool, page entry x page + slot of the page; -1 (and the status) without a page
+ *   pos[]   its slot + offset[u] (NULL: 0), for instance by how much a compression shortened the unit;
+ *           with parent (as for grkv_attend_tree, t <= 256) len - count + depth + offset.  A
+ *           position outside 0..2^31 - 1 is reported and stands as -1
+ * pos int32 and slot int64 [U][t]; entries of rows that a unit does not have are -1.  With first_row
+ * (int64 [U + 1], written; U <= 2^20) rows are packed: unit u's entries start at first_row[u], the sum of
+ * the counts before it, first_row[U] is the sum of all, and the entries (of U t) behind it are -1.
+ * That is what grkv_cache_append and grkv_cache_append_rope take as first_row and pos. */
+int grkv_cache_map(const grkv_cache_params* p, const int32_t* count, const int32_t* parent,
+                   const int32_t* offset, const int32_t* table, const int32_t* len,
+                   int64_t* first_row, int32_t* pos, int64_t* slot, void* ws, size_t ws_bytes,
+                   void* stream);
+
+/* ------------------------------------------------------------ rotary positions
+ * The paper scores and merges keys as the model stores them, rotated.  What follows is how a user
+ * rotates new keys and queries for a cache whose slots are no longer positions, and turns kept
+ * keys where positions are those of slots.
+ *
+ * Pair i < rotary / 2 of a row at position p becomes
+ *   (x, y) -> a (x cos p f_i - y sin p f_i, x sin p f_i + y cos p f_i)
+ * and the dimensions from rotary on go through bit for bit.  Angles are off by 2^-28 turns
+ * at most (what fp32 leaves of an eighth of a turn) at every position, frequencies by some 2^-51 of
+ * themselves and 2^-65 turns; products and sums are fp32, rounded once to the row's type. */
+#define GRKV_ROPE_HALF  0   /* pair i: dimensions i and i + rotary / 2 */
+#define GRKV_ROPE_PAIRS 1   /* pair i: dimensions 2 i and 2 i + 1 (interleaved) */
+
+/* Frequencies, f_i = theta^(-2 i / rotary) and for contexts longer than the trained: */
+#define GRKV_ROPE_PLAIN  0
+#define GRKV_ROPE_LINEAR 1  /* f_i / factor (position interpolation) */
+#define GRKV_ROPE_NTK    2  /* theta factor^(rotary / (rotary - 2)) in theta's place */
+#define GRKV_ROPE_BANDS  3  /* f_i (k + (1 - k) / factor), k the turns over `original` positions, from
+                               low (k = 0) to high (k = 1) */
+#define GRKV_ROPE_YARN   4  /* the same with k falling in i, from the floor of the dimension that makes
+                               high turns to the ceiling of the one that makes low; a = 0.1 ln factor + 1
+                               (YaRN, arXiv 2309.00071) */
+typedef struct {
+  int32_t d;          /* head dimension; 128 only                                      */
+  int32_t rotary;     /* even, 2..d: the first dimensions, which are rotated (d)       */
+  int32_t layout;     /* GRKV_ROPE_HALF or GRKV_ROPE_PAIRS                             */
+  int32_t scaling;    /* GRKV_ROPE_PLAIN, ...                                          */
+  double theta;       /* > 1 (10000)                                                   */
+  double factor;      /* > 0 (1): by how much contexts are longer; not read by PLAIN   */
+  double low, high;   /* turns, low < high; 0: 1, and 4 (BANDS) or 32 (YARN)           */
+  double original;    /* > 0 (8192): trained positions; BANDS, YARN                    */
+  double amplitude;   /* >= 0: a; 0: 1, or YaRN's                                      */
+} grkv_rope_params;
+
+/* What the calls take, on the host: made once and kept by the caller. */
+typedef struct {
+  int32_t rotary, layout;
+  float amplitude;      /* a */
+  int32_t reserved;
+  uint64_t turns[64];   /* 2^64 f_i / (2 pi) modulo 2^64, i < rotary / 2 */
+} grkv_rope;
+
+/* Fills `p` with the defaults above (half layout, every dimension, no scaling). */
+void grkv_rope_params_init(grkv_rope_params* p);
+/* factors: HOST array [rotary / 2] by which the frequencies are divided as well, or NULL. */
+int grkv_rope_make(const grkv_rope_params* p, const double* factors, grkv_rope* rope);
+
+#define GRKV_ROPE_TRANSPOSE 0x1u /* the angles' signs turned: the gradient of the rotation's input from
+                                    that of its output; undoes the rotation where a = 1 */
+typedef struct {
+  int32_t seqs, heads, tokens;   /* S, H, t >= 0; S t <= 2^30, H <= 2^16 */
+  int32_t d;                     /* 128 */
+  int32_t dtype;
+  uint32_t flags;                /* GRKV_ROPE_TRANSPOSE */
+  int64_t in_stride[3];          /* elements from a sequence, a head, a token to the next; rows are */
+  int64_t out_stride[3];         /* contiguous and start on 16 bytes; not read where there is one */
+} grkv_rows;
+
+/* Rotates rows [S][H][t][d] of any strides into rows of any strides: from a projection's layout
+ * [S][t][H][d] into the attention's [U][g][t][d] (S H = U g), say.  Row (s, h, i) is at position
+ * pos[s][i] (int32 [S][t]), or start[s] + i (start int32 [S], NULL: 0); not both arrays.  Rows at negative
+ * positions, padding, are left as they were.  out may be in, with the same strides; otherwise
+ * they must not overlap, nor out's rows each other (GRKV_ERR_INVALID_ARG for strides that step into
+ * their own rows; an input's may be 0).  Takes no workspace and reports no status. */
+int grkv_rope_rows(const grkv_rope* rope, const grkv_rows* rows, const void* in, void* out,
+                   const int32_t* pos, const int32_t* start, void* stream);
+
+/* grkv_cache_append whose keys are rotated on their way into the pages, together with the queries
+ * of the same tokens: q, q_out [U][g][t][d] (both NULL: no queries; q_out may be q), row i < count[u] of
+ * them at the position of new row i.  pos (int32, an entry for every row of k_new) gives positions;
+ * without it a row's position is its slot + offset[u] (int32 [U], NULL: 0); not both.  Values are
+ * written as they are.  A row without a page is skipped and reported as by grkv_cache_append, its
+ * queries are rotated all the same; a negative position is reported, and nothing is written for it. */
+int grkv_cache_append_rope(const grkv_cache_params* p, const grkv_rope* rope, const void* k_new,
+                           const void* v_new, const int64_t* first_row, int64_t new_rows,
+                           const int32_t* count, const int32_t* pos, const int32_t* offset,
+                           const void* q, void* q_out, const int32_t* table, const int32_t* len,
+                           void* k_pages, void* v_pages, void* ws, size_t ws_bytes, void* stream);
+
+/* grkv_cache_compact whose keys are turned on their way, each by turn[u][i] positions (int32 [U][t],
+ * of any sign), or (turn NULL) by what its slot changes, first[u] + i - idx[u][i]: kept keys that were
+ * rotated for their slots are so again.  a is not applied again.  A key turned by 0 moves bit for
+ * bit; every other turn rounds it once to its type. */
+int grkv_cache_compact_rope(const grkv_cache_params* p, const grkv_rope* rope, const int32_t* idx,
+                            const int32_t* keep, const int32_t* first, const int32_t* turn,
+                            const int32_t* table_in, const int32_t* len_in, const int32_t* table_out,
+                            void* k_pages, void* v_pages, void* ws, size_t ws_bytes, void* stream);
+
 /* Synchronises `stream`, then stores in *device_status the device-side
  * status of the most recent call that used `ws` (GRKV_OK or one of the codes marked
  * "device" above).  Returns GRKV_ERR_CUDA if the stream reports an error. */

@@ -34,6 +34,14 @@ GRKV_ONE_READ_SCORE = 0x4
 GRKV_DETERMINISTIC = 0x8
 GRKV_CHECKS = 0x10
 GRKV_TEST_TIMEOUT = 0x80000000
+GRKV_ROPE_HALF = 0
+GRKV_ROPE_PAIRS = 1
+GRKV_ROPE_PLAIN = 0
+GRKV_ROPE_LINEAR = 1
+GRKV_ROPE_NTK = 2
+GRKV_ROPE_BANDS = 3
+GRKV_ROPE_YARN = 4
+GRKV_ROPE_TRANSPOSE = 0x1
 
 EXPORTS = ("grkv_params_init", "grkv_workspace_size", "grkv_score", "grkv_select", "grkv_merge",
            "grkv_compress", "grkv_status", "grkv_strerror", "grkv_launch_count",
@@ -41,7 +49,9 @@ EXPORTS = ("grkv_params_init", "grkv_workspace_size", "grkv_score", "grkv_select
            "grkv_compress_ragged_workspace_size", "grkv_compress_ragged",
            "grkv_cache_params_init", "grkv_cache_workspace_size", "grkv_cache_reserve",
            "grkv_cache_fork", "grkv_cache_trim", "grkv_cache_append", "grkv_cache_compact",
-           "grkv_attend", "grkv_attend_tree")
+           "grkv_attend", "grkv_attend_tree", "grkv_attend_cross", "grkv_cache_map",
+           "grkv_rope_params_init", "grkv_rope_make", "grkv_rope_rows", "grkv_cache_append_rope",
+           "grkv_cache_compact_rope")
 
 
 class grkv_params(ctypes.Structure):
@@ -62,6 +72,30 @@ class grkv_cache_params(ctypes.Structure):
         ("pages", ctypes.c_int32), ("page", ctypes.c_int32), ("max_pages", ctypes.c_int32),
         ("tokens", ctypes.c_int32), ("window", ctypes.c_int32), ("n_sink", ctypes.c_int32),
         ("scale", ctypes.c_float), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+    ]
+
+
+class grkv_rope_params(ctypes.Structure):
+    _fields_ = [
+        ("d", ctypes.c_int32), ("rotary", ctypes.c_int32), ("layout", ctypes.c_int32),
+        ("scaling", ctypes.c_int32), ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+        ("low", ctypes.c_double), ("high", ctypes.c_double), ("original", ctypes.c_double),
+        ("amplitude", ctypes.c_double),
+    ]
+
+
+class grkv_rope(ctypes.Structure):
+    _fields_ = [
+        ("rotary", ctypes.c_int32), ("layout", ctypes.c_int32), ("amplitude", ctypes.c_float),
+        ("reserved", ctypes.c_int32), ("turns", ctypes.c_uint64 * 64),
+    ]
+
+
+class grkv_rows(ctypes.Structure):
+    _fields_ = [
+        ("seqs", ctypes.c_int32), ("heads", ctypes.c_int32), ("tokens", ctypes.c_int32),
+        ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+        ("in_stride", ctypes.c_int64 * 3), ("out_stride", ctypes.c_int64 * 3),
     ]
 
 
@@ -113,6 +147,12 @@ def load():
                  "grkv_compress_ragged"):
         getattr(lib, name).restype = ctypes.c_int
     _cp, _sz, _i = ctypes.POINTER(grkv_cache_params), ctypes.c_size_t, ctypes.c_int32
+    _rp, _pp = ctypes.POINTER(grkv_rope), ctypes.POINTER(grkv_rope_params)
+    lib.grkv_rope_params_init.argtypes = [_pp]
+    lib.grkv_rope_params_init.restype = None
+    lib.grkv_rope_make.argtypes = [_pp, ctypes.POINTER(ctypes.c_double), _rp]
+    lib.grkv_rope_rows.argtypes = [_rp, ctypes.POINTER(grkv_rows), _vp, _vp, _vp, _vp, _vp]
+    lib.grkv_rope_make.restype = lib.grkv_rope_rows.restype = ctypes.c_int
     lib.grkv_cache_params_init.argtypes = [_cp, _i, _i, _i, _i, _i]
     lib.grkv_cache_params_init.restype = None
     lib.grkv_cache_workspace_size.argtypes = [_cp, ctypes.POINTER(_sz)]
@@ -120,7 +160,10 @@ def load():
                        ("grkv_cache_fork", [_i] + [_vp] * 6),
                        ("grkv_cache_append", [_vp] * 3 + [ctypes.c_int64] + [_vp] * 5),
                        ("grkv_cache_compact", [_vp] * 8), ("grkv_attend", [_vp] * 8),
-                       ("grkv_attend_tree", [_vp] * 9)):
+                       ("grkv_attend_tree", [_vp] * 9), ("grkv_attend_cross", [_vp] * 8),
+                       ("grkv_cache_map", [_vp] * 8),
+                       ("grkv_cache_append_rope", [_rp] + [_vp] * 3 + [ctypes.c_int64] + [_vp] * 9),
+                       ("grkv_cache_compact_rope", [_rp] + [_vp] * 9)):
         getattr(lib, name).argtypes = [_cp, *lead, _vp, _sz, _vp]
         getattr(lib, name).restype = ctypes.c_int
     lib.grkv_cache_workspace_size.restype = ctypes.c_int
@@ -277,6 +320,10 @@ _CALLS = {
     "trim": "table:i lens:i refs:i",
     "append": "k_new:r v_new:r k_pages:r v_pages:r table:i lens:i count:i first_row:l",
     "compact": "k_pages:r v_pages:r idx:i table_in:i lens_in:i table_out:i keep:i first:i",
+    "map": "table:i lens:i pos:i slot:l count:i parent:i offset:i first_row:l",
+    "append_rope": "k_new:r v_new:r k_pages:r v_pages:r table:i lens:i q:r q_out:r pos:i offset:i "
+                   "count:i first_row:l",
+    "compact_rope": "k_pages:r v_pages:r idx:i table_in:i lens_in:i table_out:i keep:i first:i turn:i",
 }
 _dtypes = {}   # (call, p.dtype) -> the tensors' types
 
@@ -445,6 +492,143 @@ def grkv_attend_tree(p, q, k_pages, v_pages, table, lens, parent, out, ws, q_len
         (rows * d, n, n, rows * d, u * p.max_pages, u, u, u * tokens, rows))
     rc = load().grkv_attend_tree(p, q, k, v, t, le, ql, pa, o, ls, w, nb, st)
     return _check(rc, "grkv_attend_tree", check)
+
+
+def grkv_attend_cross(p, q, k_pages, v_pages, table, lens, out, ws, q_lens=None, lse=None,
+                      ws_bytes=None, stream=None, check=True):
+    """Attention of q_lens rows of every unit over all of its lens slots."""
+    u, d = p.units, p.d
+    n, rows = p.pages * p.page * d, u * p.group * p.tokens
+    (q, k, v, o, t, le, ql, ls), w, nb, st = _addresses(
+        "attend", p, ws, ws_bytes, stream, (q, k_pages, v_pages, out, table, lens, q_lens, lse),
+        (rows * d, n, n, rows * d, u * p.max_pages, u, u, rows))
+    rc = load().grkv_attend_cross(p, q, k, v, t, le, ql, o, ls, w, nb, st)
+    return _check(rc, "grkv_attend_cross", check)
+
+
+def grkv_cache_map(p, table, lens, pos, slot, ws, count=None, parent=None, offset=None,
+                   first_row=None, ws_bytes=None, stream=None, check=True):
+    """Positions and slots of the last `count` of the `lens` slots of every unit; with first_row
+    ([U + 1], written) packed."""
+    u, rows = p.units, p.units * p.tokens
+    (t, le, po, sl, c, pa, of, f), w, nb, st = _addresses(
+        "map", p, ws, ws_bytes, stream, (table, lens, pos, slot, count, parent, offset, first_row),
+        (u * p.max_pages, u, rows, rows, u, rows, u, u + 1))
+    rc = load().grkv_cache_map(p, c, pa, of, t, le, f, po, sl, w, nb, st)
+    return _check(rc, "grkv_cache_map", check)
+
+
+# -------------------------------------------------------------- rotary positions
+_ROPE_NAMES = {
+    "layout": {"half": GRKV_ROPE_HALF, "pairs": GRKV_ROPE_PAIRS},
+    "scaling": {"plain": GRKV_ROPE_PLAIN, "linear": GRKV_ROPE_LINEAR, "ntk": GRKV_ROPE_NTK,
+                "bands": GRKV_ROPE_BANDS, "yarn": GRKV_ROPE_YARN},
+}
+
+
+def rope_params(**kw) -> grkv_rope_params:
+    """grkv_rope_params with the library defaults, then any field overridden by name (layout and
+    scaling may be given as "half", "pairs", "plain", "linear", "ntk", "bands", "yarn")."""
+    p = grkv_rope_params()
+    load().grkv_rope_params_init(ctypes.byref(p))
+    for key, val in kw.items():
+        if isinstance(val, str):
+            val = _ROPE_NAMES[key][val]
+        setattr(p, key, val)
+    return p
+
+
+def grkv_rope_make(p: grkv_rope_params, factors=None) -> grkv_rope:
+    """The plan that the calls take; factors: [rotary / 2] by which frequencies are divided."""
+    rope = grkv_rope()
+    if factors is not None:
+        if len(factors) != p.rotary // 2:
+            raise ValueError(f"{len(factors)} factors, the plan has {p.rotary // 2} pairs")
+        factors = (ctypes.c_double * len(factors))(*[float(x) for x in factors])
+    _check(load().grkv_rope_make(ctypes.byref(p), factors, ctypes.byref(rope)), "grkv_rope_make", True)
+    return rope
+
+
+def grkv_rope_rows(rope, x, out, pos=None, start=None, transpose=False, stream=None, check=True):
+    """Rotates rows x [S, H, t, 128] into out, both of any strides; pos [S, t] or start [S]."""
+    import torch
+    shape = x.shape
+    if len(shape) != 4 or out.shape != shape:
+        raise ValueError(f"x is {tuple(shape)}, out {tuple(out.shape)}: the call takes two [S, H, t, d]")
+    s, h, t, d = shape
+    dtype = x.dtype
+    code = _ROW_TYPES.get(dtype) if _ROW_TYPES else _row_types().get(dtype)
+    if code is None or out.dtype is not dtype:
+        raise ValueError(f"x is {dtype}, out {out.dtype}: the call takes bfloat16 or float32")
+    a, b, c, e = x.stride()
+    oa, ob, oc, oe = out.stride()
+    if x.numel() and (e != 1 or oe != 1):
+        raise ValueError("the rows of x and out are not contiguous")
+    dev = x.get_device()
+    if dev < 0 or dev != torch.cuda.current_device() or out.get_device() != dev:
+        raise ValueError(f"x is on {x.device}, out on {out.device}, the call runs on the current CUDA device")
+    where = []
+    for name, i, need in (("pos", pos, s * t), ("start", start, s)):
+        if i is not None and type(i) is not int:
+            if (i.dtype is not torch.int32 or i.get_device() != dev or i.numel() < need
+                    or not i.is_contiguous()):
+                raise ValueError(f"{name} is {i.dtype} {tuple(i.shape)} on {i.device}: the call takes {need} "
+                                 f"contiguous int32 on {x.device}")
+            i = i.data_ptr()
+        where.append(i)
+    rows = grkv_rows(s, h, t, d, code, GRKV_ROPE_TRANSPOSE if transpose else 0, (a, b, c), (oa, ob, oc))
+    if stream is None:
+        stream = _raw_stream(dev)
+    elif type(stream) is not int:
+        stream = stream.cuda_stream
+    rc = load().grkv_rope_rows(rope, rows, x.data_ptr(), out.data_ptr(), where[0], where[1], stream)
+    return _check(rc, "grkv_rope_rows", check)
+
+
+_ROW_TYPES = {}
+
+
+def _row_types():
+    import torch
+    _ROW_TYPES.update({torch.bfloat16: GRKV_BF16, torch.float32: GRKV_F32})
+    return _ROW_TYPES
+
+
+def grkv_cache_append_rope(p, rope, k_new, v_new, k_pages, v_pages, table, lens, ws, q=None,
+                           q_out=None, pos=None, offset=None, count=None, first_row=None,
+                           ws_bytes=None, stream=None, check=True, new_rows=None):
+    """grkv_cache_append with rotated keys, and the same tokens' queries rotated into q_out."""
+    u, d = p.units, p.d
+    n, need = p.pages * p.page * d, u * p.tokens * d
+    if first_row is None:
+        new_rows = 0
+    else:
+        if new_rows is None:
+            if type(k_new) is int or type(v_new) is int:
+                raise ValueError("new_rows is not given: packed rows at an address have no size")
+            new_rows = min(k_new.numel(), v_new.numel()) // d
+        need = new_rows * d
+    queries = u * p.group * p.tokens * d
+    (kn, vn, k, v, t, le, qi, qo, po, of, c, f), w, nb, st = _addresses(
+        "append_rope", p, ws, ws_bytes, stream,
+        (k_new, v_new, k_pages, v_pages, table, lens, q, q_out, pos, offset, count, first_row),
+        (need, need, n, n, u * p.max_pages, u, queries, queries, need // d, u, u, u))
+    rc = load().grkv_cache_append_rope(p, rope, kn, vn, f, new_rows, c, po, of, qi, qo, t, le, k, v,
+                                       w, nb, st)
+    return _check(rc, "grkv_cache_append_rope", check)
+
+
+def grkv_cache_compact_rope(p, rope, idx, k_pages, v_pages, table_in, lens_in, table_out, ws,
+                            keep=None, first=None, turn=None, ws_bytes=None, stream=None, check=True):
+    """grkv_cache_compact with keys turned by `turn` [U, t], or by what their slots change."""
+    u = p.units
+    n, m = p.pages * p.page * p.d, u * p.max_pages
+    (k, v, i, ti, li, to, ke, f, tu), w, nb, st = _addresses(
+        "compact_rope", p, ws, ws_bytes, stream,
+        (k_pages, v_pages, idx, table_in, lens_in, table_out, keep, first, turn),
+        (n, n, u * p.tokens, m, u, m, u, u, u * p.tokens))
+    rc = load().grkv_cache_compact_rope(p, rope, i, ke, f, tu, ti, li, to, k, v, w, nb, st)
+    return _check(rc, "grkv_cache_compact_rope", check)
 
 
 def grkv_launch_count() -> int:

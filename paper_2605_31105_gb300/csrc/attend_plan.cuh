@@ -34,6 +34,7 @@ struct AttendArgs {
   int rows;    // rows of an item, nq * T * g
   int extra;   // tiles' worth of work of an item besides its tiles
   int wide;    // there may be 2^30 of them or more
+  int cross;   // every row sees the whole unit: its slots end at base, rows are none of them
   float sl2;   // scale * log2(e)
   AttendRec* rec;
   float2* pml;
@@ -57,12 +58,12 @@ __device__ __forceinline__ Item make_item(const AttendArgs& a, int u, int qb, in
   Item it;
   it.u = u;
   it.L = L;
-  it.base = L - T;
+  it.base = a.cross ? L : L - T;
   it.tok0 = qb * a.nq * a.T;
   it.ntok = max(0, min(T - it.tok0, a.nq * a.T));
   const bool tree = a.parent != nullptr;
   const int p0 = it.base + (tree ? 0 : it.tok0);   // the first position of a row
-  it.hi = max(0, it.base + it.tok0 + it.ntok);
+  it.hi = a.cross ? L : max(0, it.base + it.tok0 + it.ntok);
   it.lo = a.W ? min(max(0, p0 - a.W + 1), it.hi) : 0;
   it.sink_end = a.W ? min(a.s, it.lo) : 0;
   it.lo_tile = it.lo / kSlotTile;
@@ -89,7 +90,7 @@ __device__ __forceinline__ Item make_item(const AttendArgs& a, int u, int qb) {
 struct FullTiles {
   int end, sinks, window;
   __device__ FullTiles(const AttendArgs& a, const Item& it, int t0, int n) {
-    end = max(0, a.parent ? it.base : it.base + t0 + 1) / kSlotTile;
+    end = max(0, a.parent || a.cross ? it.base : it.base + t0 + 1) / kSlotTile;
     sinks = a.W ? a.s / kSlotTile : 0;
     window = a.W ? (max(0, it.base + t0 + n - a.W) + kSlotTile - 1) / kSlotTile : 0;
   }
@@ -164,7 +165,7 @@ __device__ __forceinline__ RowVis row_vis(const AttendArgs& a, const Item& it, i
         x = __ldg(par + x);
       }
   }
-  if (a.parent) r.hi = it.base;
+  if (a.parent || a.cross) r.hi = it.base;
   r.hi = max(r.hi, 0);
   r.lo = a.W ? min(max(0, p - a.W + 1), r.hi) : 0;
   r.end_s = min(a.s, r.lo);

@@ -24,6 +24,7 @@ struct AttendIo {
   const int32_t *table, *len, *qlen, *parent;   // qlen, parent may be null
   void* out;
   float* lse;   // may be null
+  bool cross;   // every row sees every slot of its unit
 };
 
 // Workspace regions of the cache calls (byte offsets, 256-byte aligned).

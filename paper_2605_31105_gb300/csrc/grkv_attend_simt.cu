@@ -626,6 +626,7 @@ cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, con
   a.W = s.W;
   a.s = s.s;
   a.withhold = s.test_timeout;
+  a.cross = io.cross;
   a.sl2 = (float)((double)s.scale * 1.4426950408889634);
   a.rec = (AttendRec*)(ws + L.rec);
   a.pml = (float2*)(ws + L.pml);

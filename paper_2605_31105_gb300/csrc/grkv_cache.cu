@@ -443,6 +443,7 @@ int attend(const grkv_cache_params* p, const AttendIo& io, bool tree, void* ws, 
   CacheShape s;
   CacheWs L;
   GRKV_TRY(cache_begin(p, ws, ws_bytes, &s, &L));
+  if (io.cross) s.W = 0;
   if ((tree && s.t > kMaxTree) || attend_tiles(s) > kMaxAttendTiles) return GRKV_ERR_UNSUPPORTED;
   cudaStream_t st = (cudaStream_t)stream;
   if (s.U == 0) return clear_status((char*)ws, L, st);
@@ -486,7 +487,7 @@ int grkv_cache_workspace_size(const grkv_cache_params* p, size_t* bytes) {
 int grkv_attend(const grkv_cache_params* p, const void* q, const void* k_pages, const void* v_pages,
                 const int32_t* table, const int32_t* len, const int32_t* q_len, void* out,
                 float* lse, void* ws, size_t ws_bytes, void* stream) {
-  const AttendIo io{q, k_pages, v_pages, table, len, q_len, nullptr, out, lse};
+  const AttendIo io{q, k_pages, v_pages, table, len, q_len, nullptr, out, lse, false};
   return attend(p, io, false, ws, ws_bytes, stream);
 }
 
@@ -494,8 +495,16 @@ int grkv_attend_tree(const grkv_cache_params* p, const void* q, const void* k_pa
                      const void* v_pages, const int32_t* table, const int32_t* len,
                      const int32_t* q_len, const int32_t* parent, void* out, float* lse, void* ws,
                      size_t ws_bytes, void* stream) {
-  const AttendIo io{q, k_pages, v_pages, table, len, q_len, parent, out, lse};
+  const AttendIo io{q, k_pages, v_pages, table, len, q_len, parent, out, lse, false};
   return attend(p, io, true, ws, ws_bytes, stream);
+}
+
+int grkv_attend_cross(const grkv_cache_params* p, const void* q, const void* k_pages,
+                      const void* v_pages, const int32_t* table, const int32_t* len,
+                      const int32_t* q_len, void* out, float* lse, void* ws, size_t ws_bytes,
+                      void* stream) {
+  const AttendIo io{q, k_pages, v_pages, table, len, q_len, nullptr, out, lse, true};
+  return attend(p, io, false, ws, ws_bytes, stream);
 }
 
 int grkv_cache_fork(const grkv_cache_params* p, int32_t units_in, const int32_t* src,

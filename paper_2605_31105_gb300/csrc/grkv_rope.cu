@@ -1,0 +1,431 @@
+// Rotary positions: of rows on their way from a projection to attention, of new keys on their way
+// into the pages, of kept keys that change their slots.
+//
+// All of them move rows (256 bytes of bf16, 512 of fp32) and turn a row's pairs in between: bound
+// by memory, for a few tokens by latency.  A thread holds two 16-byte vectors of a row, which
+// hold whole pairs, and the cosines and sines of those pairs, which all heads of a token share.
+#include <algorithm>
+#include <cmath>
+
+#include "cache_rows.cuh"
+#include "rope.cuh"
+
+using namespace grkv;
+
+namespace {
+
+// ---------------------------------------------------------------------- the plan
+int make_rope(const grkv_rope_params* p, const double* factors, grkv_rope* rope) {
+  if (!p || !rope) return GRKV_ERR_INVALID_ARG;
+  if (p->d < 1 || p->rotary < 2 || p->rotary > p->d || p->rotary % 2) return GRKV_ERR_INVALID_ARG;
+  if (p->layout != GRKV_ROPE_HALF && p->layout != GRKV_ROPE_PAIRS) return GRKV_ERR_INVALID_ARG;
+  if (p->scaling < GRKV_ROPE_PLAIN || p->scaling > GRKV_ROPE_YARN) return GRKV_ERR_INVALID_ARG;
+  auto positive = [](double x) { return x > 0 && std::isfinite(x); };
+  if (!(p->theta > 1) || !std::isfinite(p->theta)) return GRKV_ERR_INVALID_ARG;
+  if (p->scaling != GRKV_ROPE_PLAIN && !positive(p->factor)) return GRKV_ERR_INVALID_ARG;
+  if (!(p->amplitude >= 0) || !std::isfinite(p->amplitude)) return GRKV_ERR_INVALID_ARG;
+  const bool ramp = p->scaling == GRKV_ROPE_BANDS || p->scaling == GRKV_ROPE_YARN;
+  if (ramp && (!positive(p->original) || !(p->low >= 0) || !(p->high >= 0) || !std::isfinite(p->high)))
+    return GRKV_ERR_INVALID_ARG;
+  if (p->d != kD) return GRKV_ERR_UNSUPPORTED;
+  const double pi2 = 6.283185307179586476925, r = p->rotary;
+  const double low = p->low != 0 ? p->low : 1;
+  const double high = p->high != 0 ? p->high : p->scaling == GRKV_ROPE_YARN ? 32 : 4;
+  if (ramp && !(low < high)) return GRKV_ERR_INVALID_ARG;
+  double theta = p->theta;
+  if (p->scaling == GRKV_ROPE_NTK && p->rotary > 2) theta *= std::pow(p->factor, r / (r - 2));
+  auto dim = [&](double turns) {   // the pair that makes `turns` turns over the trained positions
+    return r * std::log(p->original / (pi2 * turns)) / (2 * std::log(p->theta));
+  };
+  double from = 0, to = 1;
+  if (p->scaling == GRKV_ROPE_YARN) {
+    from = std::max(std::floor(dim(high)), 0.0);
+    to = std::min(std::ceil(dim(low)), r - 1);
+    to = from + std::max(to - from, 0.001);
+  }
+  grkv_rope out{};
+  out.rotary = p->rotary;
+  out.layout = p->layout;
+  out.amplitude = (float)(p->amplitude != 0 ? p->amplitude
+                          : p->scaling == GRKV_ROPE_YARN && p->factor > 1 ? 0.1 * std::log(p->factor) + 1
+                                                                          : 1.0);
+  for (int i = 0; i < p->rotary / 2; ++i) {
+    double f = std::pow(theta, -2.0 * i / r), keep = 1;
+    if (p->scaling == GRKV_ROPE_LINEAR) f /= p->factor;
+    if (p->scaling == GRKV_ROPE_BANDS) keep = (p->original * f / pi2 - low) / (high - low);
+    if (p->scaling == GRKV_ROPE_YARN) keep = 1 - (i - from) / (to - from);
+    if (ramp) {
+      keep = std::min(std::max(keep, 0.0), 1.0);
+      f *= keep + (1 - keep) / p->factor;
+    }
+    if (factors) {
+      if (!positive(factors[i])) return GRKV_ERR_INVALID_ARG;
+      f /= factors[i];
+    }
+    double t = f / pi2;
+    t = std::ldexp(t - std::floor(t), 64);   // at most 2^64 - 2^11: the fraction has 53 bits
+    out.turns[i] = (uint64_t)std::round(t);
+  }
+  if (!(out.amplitude > 0) || std::isinf(out.amplitude)) return GRKV_ERR_INVALID_ARG;
+  *rope = out;
+  return GRKV_OK;
+}
+
+int check_rope(const grkv_rope* r, RopeArgs* a) {
+  if (!r || r->rotary < 2 || r->rotary > kD || r->rotary % 2) return GRKV_ERR_INVALID_ARG;
+  if (r->layout != GRKV_ROPE_HALF && r->layout != GRKV_ROPE_PAIRS) return GRKV_ERR_INVALID_ARG;
+  if (!(r->amplitude > 0) || std::isinf(r->amplitude)) return GRKV_ERR_INVALID_ARG;
+  a->half = r->rotary / 2;
+  a->amp = r->amplitude;
+  for (int i = 0; i < kD / 2; ++i) a->turns[i] = i < a->half ? r->turns[i] : 0;
+  return GRKV_OK;
+}
+
+// A call f(T, Hold) for the type and layout.
+template <typename F>
+cudaError_t dispatch(int dtype, const grkv_rope* r, F f) {
+  const int vec = dtype == GRKV_F32 ? 4 : 8;
+  auto of_type = [&](auto zero) {
+    if (r->layout == GRKV_ROPE_PAIRS) return f(zero, std::integral_constant<Hold, Hold::Pairs>{});
+    if (r->rotary / 2 % vec == 0) return f(zero, std::integral_constant<Hold, Hold::Half>{});
+    return f(zero, std::integral_constant<Hold, Hold::Single>{});
+  };
+  return dtype == GRKV_F32 ? of_type(0.f) : of_type(__nv_bfloat16());
+}
+
+// -------------------------------------------------------------------------- rows
+struct RowsArgs {
+  const void* in;
+  void* out;
+  int64_t is[3], os[3];   // strides of sequence, head, token, in elements
+  const int32_t *pos, *start;
+  int S, H, t;
+  int heads;              // of a block's
+  float sign;             // -1: transposed
+};
+
+constexpr int kRowThreads = 256;
+
+template <typename T, Hold H>
+__global__ void __launch_bounds__(kRowThreads)
+    k_rope_rows(const __grid_constant__ RopeArgs r, const __grid_constant__ RowsArgs a) {
+  constexpr int kThr = Pair<T, H>::kThreads;
+  const int64_t n = (int64_t)blockIdx.x * (kRowThreads / kThr) + threadIdx.x / kThr;
+  if (n >= (int64_t)a.S * a.t) return;
+  const int s = (int)(n / a.t), i = (int)(n - (int64_t)s * a.t);
+  const int64_t p = a.pos ? a.pos[n] : (int64_t)(a.start ? a.start[s] : 0) + i;
+  if (p < 0) return;
+  const Place<T, H> at(threadIdx.x % kThr, r.half);
+  const Angles<T, H> an = angles<T, H>(r, at, p, r.amp, a.sign);
+  const T* in = (const T*)a.in + s * a.is[0] + i * a.is[2];
+  T* out = (T*)a.out + s * a.os[0] + i * a.os[2];
+  const int h1 = min(a.H, (int)(blockIdx.y + 1) * a.heads);
+  for (int h0 = blockIdx.y * a.heads; h0 < h1; h0 += 4) {
+    Raw<T, H> x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (h0 + j < h1) x[j] = load_pair<T, H>(in + (h0 + j) * a.is[1], at);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (h0 + j < h1) store_pair<T, H>(out + (h0 + j) * a.os[1], at, rotate<T, H>(x[j], at, an));
+  }
+}
+
+// Whether rows of the strides (elements) are whole vectors apart, and, for outputs, apart at all.
+int check_strides(const int64_t* stride, const int64_t* n, int vec, bool apart) {
+  for (int x = 0; x < 3; ++x)
+    if (n[x] > 1 && stride[x] % vec) return GRKV_ERR_MISALIGNED;
+  for (int x = 0; x < 3; ++x)
+    if (n[x] > 1 && (stride[x] < 0 || stride[x] > (int64_t)1 << 40)) return GRKV_ERR_INVALID_ARG;
+  if (!apart) return GRKV_OK;
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + 3, [&](int x, int y) { return stride[x] < stride[y]; });
+  int64_t end = kD;   // what the dimensions so far reach over
+  for (int x : order) {
+    if (n[x] <= 1) continue;
+    if (stride[x] < end) return GRKV_ERR_INVALID_ARG;
+    // an outer dimension must step over all of the inner ones
+    end += stride[x] * (n[x] - 1);
+  }
+  return GRKV_OK;
+}
+
+// ------------------------------------------------------------------------ append
+struct AppendRopeArgs {
+  RowMove m;
+  const void *k_new, *v_new, *q;   // q may be null
+  void *q_out, *k, *v;
+  const int64_t* first;
+  long long new_rows;
+  const int32_t *table, *pos, *offset;
+  int g;
+};
+
+constexpr int kAppendThreads = 128;
+
+// kThreads threads a token: its new key and value, and its queries.
+template <typename T, Hold H>
+__global__ void __launch_bounds__(kAppendThreads)
+    k_append_rope(const __grid_constant__ RopeArgs r, const __grid_constant__ AppendRopeArgs a) {
+  constexpr int kThr = Pair<T, H>::kThreads;
+  const RowMove& m = a.m;
+  const int64_t n = (int64_t)blockIdx.x * (kAppendThreads / kThr) + threadIdx.x / kThr;
+  if (n >= (int64_t)m.tb.U * m.t) return;
+  const int u = (int)(n / m.t), i = (int)(n - (int64_t)u * m.t);
+  const int cnt = rows_of(m, u);
+  if (i >= cnt) return;
+  const Place<T, H> at(threadIdx.x % kThr, r.half);
+  // the length as it is: clamped to the table, rows behind it would go over those before
+  const long long slot = (long long)m.len[u] - cnt + i;
+  const long long f = a.first ? a.first[u] : (long long)u * m.t;
+  const bool has = f >= 0 && f <= a.new_rows - 1 - i;
+  int64_t p = slot + (a.offset ? a.offset[u] : 0);
+  if (a.pos) p = has ? a.pos[f + i] : -1;
+  long long to = -1;
+  if (has && p >= 0 && slot >= 0 && slot < m.tb.cols << m.tb.shift)
+    to = pool_row(m.tb, a.table, u, (int)slot, m.status);
+  else
+    set_status(m.status, GRKV_ERR_INVALID_ARG);
+  if (p < 0) return;
+  const Angles<T, H> an = angles<T, H>(r, at, p, r.amp, 1.f);
+  if (to >= 0) {
+    const Raw<T, H> k = load_pair<T, H>((const T*)a.k_new + (f + i) * kD, at);
+    const Raw<T, H> v = load_pair<T, H>((const T*)a.v_new + (f + i) * kD, at);
+    store_pair<T, H>((T*)a.k + to * kD, at, rotate<T, H>(k, at, an));
+    store_pair<T, H>((T*)a.v + to * kD, at, v);
+  }
+  if (!a.q) return;
+  const int64_t row = ((int64_t)u * a.g * m.t + i) * kD, step = (int64_t)m.t * kD;
+  for (int h0 = 0; h0 < a.g; h0 += 4) {
+    Raw<T, H> x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (h0 + j < a.g) x[j] = load_pair<T, H>((const T*)a.q + row + (h0 + j) * step, at);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (h0 + j < a.g)
+        store_pair<T, H>((T*)a.q_out + row + (h0 + j) * step, at, rotate<T, H>(x[j], at, an));
+  }
+}
+
+// ----------------------------------------------------------------------- compact
+struct CompactRopeArgs {
+  RowMove m;
+  const int32_t *idx, *table_in, *table_out, *first, *turn;
+  void *k, *v;
+};
+
+// By how many positions the key of row i of unit u is turned.
+__device__ __forceinline__ int64_t turn_of(const CompactRopeArgs& a, int u, int i) {
+  const size_t x = (size_t)u * a.m.t + i;
+  return a.turn ? a.turn[x] : (int64_t)(a.first ? a.first[u] : 0) + i - a.idx[x];
+}
+
+constexpr int kTurnThreads = 128;
+
+// To other pages: every row by itself, kThreads threads a row.
+template <typename T, Hold H>
+__global__ void __launch_bounds__(kTurnThreads)
+    k_gather_rope(const __grid_constant__ RopeArgs r, const __grid_constant__ CompactRopeArgs a) {
+  constexpr int kThr = Pair<T, H>::kThreads;
+  const RowMove& m = a.m;
+  const Place<T, H> at(threadIdx.x % kThr, r.half);
+  const int i = blockIdx.x * (kTurnThreads / kThr) + threadIdx.x / kThr;
+  for (int u = blockIdx.y; u < m.tb.U; u += gridDim.y) {
+    const int len = m.tb.clamped(m.len[u], m.status);
+    long long from, to;
+    if (i >= rows_of(m, u) ||
+        !kept_row(m, a.idx, a.table_in, len, a.table_out, a.first, false, u, i, &from, &to))
+      continue;
+    Raw<T, H> k = load_pair<T, H>((const T*)a.k + from * kD, at);
+    const Raw<T, H> v = load_pair<T, H>((const T*)a.v + from * kD, at);
+    const int64_t p = turn_of(a, u, i);
+    if (p != 0) k = rotate<T, H>(k, at, angles<T, H>(r, at, p, 1.f, 1.f));
+    store_pair<T, H>((T*)a.k + to * kD, at, k);
+    store_pair<T, H>((T*)a.v + to * kD, at, v);
+  }
+}
+
+// In place: a row only moves down, so chunks of rows in ascending order, each read as a whole
+// before it is written, never overwrite a row that is still to be read.  A block owns the same
+// few pairs of every row of one unit's keys or values (grid (U, 2, parts)).
+constexpr int kShiftRopeThreads = 256, kShiftRopeUnroll = 4;
+template <typename T, Hold H>
+struct ShiftPart {
+  // threads of a row in a block: 64 bytes of it
+  static constexpr int kThr = H == Hold::Single ? 32 / (int)sizeof(T) : 2;
+  static constexpr int kParts = Pair<T, H>::kThreads / kThr;
+};
+template <typename T, Hold H>
+__global__ void __launch_bounds__(kShiftRopeThreads)
+    k_shift_rope(const __grid_constant__ RopeArgs r, const __grid_constant__ CompactRopeArgs a) {
+  constexpr int kThr = ShiftPart<T, H>::kThr, kRows = kShiftRopeThreads / kThr;
+  const RowMove& m = a.m;
+  const int u = blockIdx.x, r0 = threadIdx.x / kThr;
+  const bool keys = blockIdx.y == 0;
+  T* pool = (T*)(keys ? a.k : a.v);
+  const Place<T, H> at(blockIdx.z * kThr + threadIdx.x % kThr, r.half);
+  const int n = rows_of(m, u), len = m.tb.clamped(m.len[u], m.status);
+  for (int base = 0; base < n; base += kRows * kShiftRopeUnroll) {
+    Raw<T, H> x[kShiftRopeUnroll];
+    long long to[kShiftRopeUnroll];
+#pragma unroll
+    for (int j = 0; j < kShiftRopeUnroll; ++j) {
+      const int i = base + j * kRows + r0;
+      long long from;
+      to[j] = -1;
+      if (i < n && kept_row(m, a.idx, a.table_in, len, a.table_in, a.first, true, u, i, &from, &to[j])) {
+        const int64_t p = keys ? turn_of(a, u, i) : 0;
+        if (from == to[j] && p == 0) {
+          to[j] = -1;
+          continue;
+        }
+        x[j] = load_pair<T, H>(pool + from * kD, at);
+        if (p != 0) x[j] = rotate<T, H>(x[j], at, angles<T, H>(r, at, p, 1.f, 1.f));
+      } else {
+        to[j] = -1;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kShiftRopeUnroll; ++j)
+      if (to[j] >= 0) store_pair<T, H>(pool + to[j] * kD, at, x[j]);
+    __syncthreads();
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+void grkv_rope_params_init(grkv_rope_params* p) {
+  if (!p) return;
+  *p = grkv_rope_params{kD, kD, GRKV_ROPE_HALF, GRKV_ROPE_PLAIN, 10000.0, 1.0, 0.0, 0.0, 8192.0, 0.0};
+}
+
+int grkv_rope_make(const grkv_rope_params* p, const double* factors, grkv_rope* rope) {
+  return make_rope(p, factors, rope);
+}
+
+int grkv_rope_rows(const grkv_rope* rope, const grkv_rows* s, const void* in, void* out,
+                   const int32_t* pos, const int32_t* start, void* stream) {
+  RopeArgs r;
+  GRKV_TRY(check_rope(rope, &r));
+  if (!s || s->seqs < 0 || s->heads < 0 || s->tokens < 0 || s->d < 1) return GRKV_ERR_INVALID_ARG;
+  if (s->dtype != GRKV_F32 && s->dtype != GRKV_BF16) return GRKV_ERR_INVALID_ARG;
+  if (s->flags & ~GRKV_ROPE_TRANSPOSE) return GRKV_ERR_INVALID_ARG;
+  if (pos && start) return GRKV_ERR_INVALID_ARG;
+  if (s->d != kD || (int64_t)s->seqs * s->tokens > (int64_t)1 << 30 || s->heads > 1 << 16)
+    return GRKV_ERR_UNSUPPORTED;
+  const int64_t n[3] = {s->seqs, s->heads, s->tokens};
+  if (n[0] == 0 || n[1] == 0 || n[2] == 0) return GRKV_OK;
+  GRKV_TRY(check_ptrs({in, out}, 16));
+  GRKV_TRY(check_optional(pos, 4));
+  GRKV_TRY(check_optional(start, 4));
+  const int vec = s->dtype == GRKV_F32 ? 4 : 8;
+  GRKV_TRY(check_strides(s->in_stride, n, vec, false));
+  GRKV_TRY(check_strides(s->out_stride, n, vec, true));
+  if (in == out)
+    for (int x = 0; x < 3; ++x)
+      if (n[x] > 1 && s->in_stride[x] != s->out_stride[x]) return GRKV_ERR_INVALID_ARG;
+  RowsArgs a{};
+  a.in = in;
+  a.out = out;
+  for (int x = 0; x < 3; ++x) {
+    a.is[x] = n[x] > 1 ? s->in_stride[x] : 0;
+    a.os[x] = n[x] > 1 ? s->out_stride[x] : 0;
+  }
+  a.pos = pos;
+  a.start = start;
+  a.S = s->seqs;
+  a.H = s->heads;
+  a.t = s->tokens;
+  a.sign = (s->flags & GRKV_ROPE_TRANSPOSE) ? -1.f : 1.f;
+  return cuda_rc(dispatch(s->dtype, rope, [&](auto zero, auto hold) {
+    using T = decltype(zero);
+    constexpr Hold H = decltype(hold)::value;
+    const int per = kRowThreads / Pair<T, H>::kThreads;
+    const int64_t blocks = ((int64_t)a.S * a.t + per - 1) / per;
+    a.heads = a.H;
+    count_launches(1);
+    return launch_kernel(false, 1, k_rope_rows<T, H>,
+                         dim3((unsigned)blocks, (unsigned)((a.H + a.heads - 1) / a.heads)), kRowThreads, 0,
+                         (cudaStream_t)stream, r, a);
+  }));
+}
+
+int grkv_cache_append_rope(const grkv_cache_params* p, const grkv_rope* rope, const void* k_new,
+                           const void* v_new, const int64_t* first_row, int64_t new_rows,
+                           const int32_t* count, const int32_t* pos, const int32_t* offset,
+                           const void* q, void* q_out, const int32_t* table, const int32_t* len,
+                           void* k_pages, void* v_pages, void* ws, size_t ws_bytes, void* stream) {
+  CacheShape s;
+  CacheWs L;
+  RopeArgs r;
+  GRKV_TRY(cache_begin(p, ws, ws_bytes, &s, &L));
+  GRKV_TRY(check_rope(rope, &r));
+  if (s.U > 0) {
+    GRKV_TRY(check_ptrs({k_new, v_new, k_pages, v_pages}, 16));
+    GRKV_TRY(check_ptrs({table, len}, 4));
+  }
+  GRKV_TRY(check_optional(first_row, 8));
+  if (first_row && new_rows < 0) return GRKV_ERR_INVALID_ARG;
+  if (pos && offset) return GRKV_ERR_INVALID_ARG;
+  if (!q != !q_out) return GRKV_ERR_INVALID_ARG;
+  GRKV_TRY(check_optional(count, 4));
+  GRKV_TRY(check_optional(pos, 4));
+  GRKV_TRY(check_optional(offset, 4));
+  GRKV_TRY(check_optional(q, 16));
+  GRKV_TRY(check_optional(q_out, 16));
+  cudaStream_t st = (cudaStream_t)stream;
+  GRKV_TRY(clear_status((char*)ws, L, st));
+  if (s.U == 0) return GRKV_OK;
+  const RowMove m{table_of(s), s.t, count, len, (int*)((char*)ws + L.status)};
+  const AppendRopeArgs a{m, k_new, v_new, q, q_out, k_pages, v_pages, first_row,
+                         first_row ? (long long)new_rows : (long long)s.U * s.t, table, pos, offset, s.g};
+  return cuda_rc(dispatch(s.dtype, rope, [&](auto zero, auto hold) {
+    using T = decltype(zero);
+    constexpr Hold H = decltype(hold)::value;
+    const int per = kAppendThreads / Pair<T, H>::kThreads;
+    count_launches(1);
+    return launch_kernel(false, 1, k_append_rope<T, H>,
+                         dim3((unsigned)(((int64_t)s.U * s.t + per - 1) / per)), kAppendThreads, 0, st, r, a);
+  }));
+}
+
+int grkv_cache_compact_rope(const grkv_cache_params* p, const grkv_rope* rope, const int32_t* idx,
+                            const int32_t* keep, const int32_t* first, const int32_t* turn,
+                            const int32_t* table_in, const int32_t* len_in, const int32_t* table_out,
+                            void* k_pages, void* v_pages, void* ws, size_t ws_bytes, void* stream) {
+  CacheShape s;
+  CacheWs L;
+  RopeArgs r;
+  GRKV_TRY(cache_begin(p, ws, ws_bytes, &s, &L));
+  GRKV_TRY(check_rope(rope, &r));
+  if (s.U > 0) {
+    GRKV_TRY(check_ptrs({k_pages, v_pages}, 16));
+    GRKV_TRY(check_ptrs({idx, table_in, len_in, table_out}, 4));
+  }
+  GRKV_TRY(check_optional(keep, 4));
+  GRKV_TRY(check_optional(first, 4));
+  GRKV_TRY(check_optional(turn, 4));
+  cudaStream_t st = (cudaStream_t)stream;
+  GRKV_TRY(clear_status((char*)ws, L, st));
+  if (s.U == 0) return GRKV_OK;
+  const RowMove m{table_of(s), s.t, keep, len_in, (int*)((char*)ws + L.status)};
+  const CompactRopeArgs a{m, idx, table_in, table_out, first, turn, k_pages, v_pages};
+  return cuda_rc(dispatch(s.dtype, rope, [&](auto zero, auto hold) {
+    using T = decltype(zero);
+    constexpr Hold H = decltype(hold)::value;
+    count_launches(1);
+    if (table_in == table_out)
+      return launch_kernel(false, 1, k_shift_rope<T, H>, dim3(s.U, 2, ShiftPart<T, H>::kParts),
+                           kShiftRopeThreads, 0, st, r, a);
+    const int per = kTurnThreads / Pair<T, H>::kThreads;
+    return launch_kernel(false, 1, k_gather_rope<T, H>,
+                         dim3((unsigned)((s.t + per - 1) / per), (unsigned)std::min(s.U, 65535)),
+                         kTurnThreads, 0, st, r, a);
+  }));
+}
+
+}  // extern "C"

@@ -1,0 +1,184 @@
+// Rotary positions on the device: angles, and the pairs of a row that a thread holds.
+//
+// Pair i of a row at position p is turned by p f_i.  The frequency is kept in turns a position, as
+// a 64-bit fraction of one (grkv_rope.turns): p times it, modulo 2^64, is the exact fraction of a
+// turn that the angle comes to, for any 32-bit position, with two integer multiplications and no
+// range reduction.  (An fp32 product is off by p f 2^-24 radians: 0.008 at position 131072.)
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "grkv_internal.cuh"
+#include "sm100.cuh"
+
+namespace grkv {
+
+struct RopeArgs {
+  uint64_t turns[kD / 2];   // by pair; 0 behind the rotated ones
+  float amp;                // factor of cosine and sine
+  int half;                 // pairs that are rotated, rotary / 2
+};
+
+// How a thread holds its pairs.  Half, Pairs: a pair of 16-byte vectors, a and b: pairs (a[i], b[i])
+// of the half layout, or neighbours in a, then in b, of the interleaved one.  Single: one pair of
+// elements, for half layouts whose two halves are not whole vectors (rotary / 2 not a multiple of
+// 8 in bf16, 4 in fp32).
+enum class Hold { Half, Pairs, Single };
+
+template <typename T, Hold H>
+struct Pair {
+  static constexpr int kVec = H == Hold::Single ? 1 : 16 / (int)sizeof(T);   // pairs of a thread
+  static constexpr int kThreads = kD / 2 / kVec;                            // of a row
+};
+
+template <typename T, Hold H>
+struct Raw {
+  uint4 a, b;
+};
+template <typename T>
+struct Raw<T, Hold::Single> {
+  T a, b;
+};
+
+// Thread s of a row's kThreads: where its two vectors start, its first pair, and how many of its
+// pairs are rotated.  What lies behind the rotated dimensions goes through as it is.
+template <typename T, Hold H>
+struct Place {
+  int a, b, pair, on;
+  __device__ __forceinline__ Place(int s, int half) {
+    constexpr int V = Pair<T, H>::kVec;
+    pair = s * V;
+    on = min(max(half - pair, 0), V);
+    // (pair - half pairs behind the rotated 2 half elements: element 2 pair)
+    const bool split = H != Hold::Pairs && pair < half;
+    a = split ? pair : 2 * pair;
+    b = split ? half + pair : a + V;
+  }
+};
+
+template <typename T, Hold H>
+struct Angles {
+  float c[Pair<T, H>::kVec], s[Pair<T, H>::kVec];
+};
+
+// Cosine and sine of p turns, times amp.  The fraction's upper 32 bits (error 2^-33 turns) are split
+// into the nearest quarter and a rest of at most an eighth of a turn, which fp32 holds to 2^-27:
+// the angle is off by 2.4e-8 at most.
+__device__ __forceinline__ void turn(uint64_t per_position, int64_t p, float amp, float* c, float* s) {
+  const int32_t f = (int32_t)((per_position * (uint64_t)p + 0x80000000u) >> 32);
+  const int32_t quarter = (int32_t)(((uint32_t)f + (1u << 29)) >> 30);   // 0..3
+  const int32_t rest = (int32_t)((uint32_t)f - ((uint32_t)quarter << 30));
+  float x, y;
+  sincospif((float)rest * 0x1p-31f, &y, &x);
+  const bool odd = quarter & 1;
+  const float cc = odd ? y : x, ss = odd ? x : y;
+  *c = amp * (((quarter + 1) & 2) ? -cc : cc);
+  *s = amp * ((quarter & 2) ? -ss : ss);
+}
+
+template <typename T, Hold H>
+__device__ __forceinline__ Angles<T, H> angles(const RopeArgs& r, const Place<T, H>& at, int64_t p,
+                                               float amp, float sign) {
+  Angles<T, H> x;
+#pragma unroll
+  for (int i = 0; i < Pair<T, H>::kVec; ++i) {
+    turn(r.turns[at.pair + i], p, amp, &x.c[i], &x.s[i]);
+    x.s[i] *= sign;
+  }
+  return x;
+}
+
+template <typename T, Hold H>
+__device__ __forceinline__ Raw<T, H> load_pair(const T* row, const Place<T, H>& at) {
+  Raw<T, H> r;
+  if constexpr (H == Hold::Single) {
+    r.a = row[at.a];
+    r.b = row[at.b];
+  } else {
+    r.a = *(const uint4*)(row + at.a);
+    r.b = *(const uint4*)(row + at.b);
+  }
+  return r;
+}
+template <typename T, Hold H>
+__device__ __forceinline__ void store_pair(T* row, const Place<T, H>& at, const Raw<T, H>& r) {
+  if constexpr (H == Hold::Single) {
+    row[at.a] = r.a;
+    row[at.b] = r.b;
+  } else {
+    *(uint4*)(row + at.a) = r.a;
+    *(uint4*)(row + at.b) = r.b;
+  }
+}
+
+__device__ __forceinline__ void rotate2(float& x, float& y, float c, float s) {
+  const float u = fmaf(x, c, -(y * s)), v = fmaf(x, s, y * c);
+  x = u;
+  y = v;
+}
+
+// The thread's rotated pairs, products and sums in fp32, rounded once; the others bit for bit.
+template <typename T, Hold H>
+__device__ __forceinline__ Raw<T, H> rotate(const Raw<T, H>& in, const Place<T, H>& at,
+                                            const Angles<T, H>& an) {
+  if (at.on == 0) return in;
+  Raw<T, H> out = in;
+  if constexpr (H == Hold::Single) {
+    float x = (float)in.a, y = (float)in.b;
+    rotate2(x, y, an.c[0], an.s[0]);
+    out.a = (T)x;
+    out.b = (T)y;
+  } else {
+    const uint32_t a[4] = {in.a.x, in.a.y, in.a.z, in.a.w}, b[4] = {in.b.x, in.b.y, in.b.z, in.b.w};
+    uint32_t oa[4], ob[4];
+    if constexpr (sizeof(T) == 4) {
+      if constexpr (H == Hold::Half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = __uint_as_float(a[i]), y = __uint_as_float(b[i]);
+          rotate2(x, y, an.c[i], an.s[i]);
+          oa[i] = __float_as_uint(x);
+          ob[i] = __float_as_uint(y);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t* w = i < 2 ? a + 2 * i : b + 2 * i - 4;
+          uint32_t* o = i < 2 ? oa + 2 * i : ob + 2 * i - 4;
+          float x = __uint_as_float(w[0]), y = __uint_as_float(w[1]);
+          rotate2(x, y, an.c[i], an.s[i]);
+          o[0] = i < at.on ? __float_as_uint(x) : w[0];
+          o[1] = i < at.on ? __float_as_uint(y) : w[1];
+        }
+      }
+    } else {
+      auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
+      auto hi = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
+      if constexpr (H == Hold::Half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x0 = lo(a[i]), x1 = hi(a[i]), y0 = lo(b[i]), y1 = hi(b[i]);
+          rotate2(x0, y0, an.c[2 * i], an.s[2 * i]);
+          rotate2(x1, y1, an.c[2 * i + 1], an.s[2 * i + 1]);
+          oa[i] = sm100::pack_bf16(x0, x1);
+          ob[i] = sm100::pack_bf16(y0, y1);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t w = i < 4 ? a[i & 3] : b[i & 3];
+          float x = lo(w), y = hi(w);
+          rotate2(x, y, an.c[i], an.s[i]);
+          const uint32_t o = i < at.on ? sm100::pack_bf16(x, y) : w;
+          if (i < 4) oa[i & 3] = o;
+          else ob[i & 3] = o;
+        }
+      }
+    }
+    out.a = make_uint4(oa[0], oa[1], oa[2], oa[3]);
+    out.b = make_uint4(ob[0], ob[1], ob[2], ob[3]);
+  }
+  return out;
+}
+
+}  // namespace grkv
