@@ -7,6 +7,7 @@ library; there is no fallback, and `load()` raises if the library is absent.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 
@@ -576,13 +577,18 @@ def grkv_rope_rows(rope, x, out, pos=None, start=None, transpose=False, stream=N
                                  f"contiguous int32 on {x.device}")
             i = i.data_ptr()
         where.append(i)
-    rows = grkv_rows(s, h, t, d, code, GRKV_ROPE_TRANSPOSE if transpose else 0, (a, b, c), (oa, ob, oc))
+    rows = _rows(s, h, t, d, code, GRKV_ROPE_TRANSPOSE if transpose else 0, a, b, c, oa, ob, oc)
     if stream is None:
         stream = _raw_stream(dev)
     elif type(stream) is not int:
         stream = stream.cuda_stream
     rc = load().grkv_rope_rows(rope, rows, x.data_ptr(), out.data_ptr(), where[0], where[1], stream)
     return _check(rc, "grkv_rope_rows", check)
+
+
+@functools.lru_cache(1024)
+def _rows(s, h, t, d, dtype, flags, a, b, c, oa, ob, oc):   # 1.2 us a structure
+    return grkv_rows(s, h, t, d, dtype, flags, (a, b, c), (oa, ob, oc))
 
 
 _ROW_TYPES = {}

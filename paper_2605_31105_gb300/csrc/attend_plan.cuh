@@ -34,13 +34,22 @@ struct AttendArgs {
   int rows;    // rows of an item, nq * T * g
   int extra;   // tiles' worth of work of an item besides its tiles
   int wide;    // there may be 2^30 of them or more
-  int cross;   // every row sees the whole unit: its slots end at base, rows are none of them
   float sl2;   // scale * log2(e)
   AttendRec* rec;
   float2* pml;
   float* po;
   int* status;
   int withhold;   // GRKV_TEST_TIMEOUT: CTA 0 withholds one arrive (tensor cores)
+  static constexpr bool cross = false;
+  __device__ bool tree() const { return parent != nullptr; }
+};
+
+// Of attention over encoder states: every row sees the whole unit, whose slots end at the items' base;
+// rows are none of them.  A type of its own, so that the kernels of the others stay as they are
+// (asked at run time, chunks took 364 us for 360, windowed prefill 190 for 187).
+struct CrossArgs : AttendArgs {
+  static constexpr bool cross = true;
+  __device__ bool tree() const { return false; }
 };
 
 // One item: tokens [tok0, tok0 + ntok) of unit u; the slots that its rows see are in
@@ -54,18 +63,18 @@ struct Item {
 };
 
 // Item qb of a unit whose length and tokens (clamped) are known.
-__device__ __forceinline__ Item make_item(const AttendArgs& a, int u, int qb, int L, int T) {
+template <typename A>
+__device__ __forceinline__ Item make_item(const A& a, int u, int qb, int L, int T) {
   Item it;
   it.u = u;
   it.L = L;
-  it.base = a.cross ? L : L - T;
+  it.base = A::cross ? L : L - T;
   it.tok0 = qb * a.nq * a.T;
   it.ntok = max(0, min(T - it.tok0, a.nq * a.T));
-  const bool tree = a.parent != nullptr;
-  const int p0 = it.base + (tree ? 0 : it.tok0);   // the first position of a row
-  it.hi = a.cross ? L : max(0, it.base + it.tok0 + it.ntok);
-  it.lo = a.W ? min(max(0, p0 - a.W + 1), it.hi) : 0;
-  it.sink_end = a.W ? min(a.s, it.lo) : 0;
+  const int p0 = it.base + (a.tree() ? 0 : it.tok0);   // the first position of a row
+  it.hi = A::cross ? L : max(0, it.base + it.tok0 + it.ntok);
+  it.lo = !A::cross && a.W ? min(max(0, p0 - a.W + 1), it.hi) : 0;
+  it.sink_end = !A::cross && a.W ? min(a.s, it.lo) : 0;
   it.lo_tile = it.lo / kSlotTile;
   it.ns = min((it.sink_end + kSlotTile - 1) / kSlotTile, it.lo_tile);
   it.nt = it.ns + (it.hi + kSlotTile - 1) / kSlotTile - it.lo_tile;
@@ -80,7 +89,8 @@ __device__ __forceinline__ int unit_len(const AttendArgs& a, int u) {
 __device__ __forceinline__ int unit_tokens(const AttendArgs& a, int u) {
   return a.qlen ? min(max(__ldg(a.qlen + u), 0), a.t) : a.t;
 }
-__device__ __forceinline__ Item make_item(const AttendArgs& a, int u, int qb) {
+template <typename A>
+__device__ __forceinline__ Item make_item(const A& a, int u, int qb) {
   return make_item(a, u, qb, unit_len(a, u), unit_tokens(a, u));
 }
 
@@ -89,10 +99,12 @@ __device__ __forceinline__ Item make_item(const AttendArgs& a, int u, int qb) {
 // node's depth is at most its index).
 struct FullTiles {
   int end, sinks, window;
-  __device__ FullTiles(const AttendArgs& a, const Item& it, int t0, int n) {
-    end = max(0, a.parent || a.cross ? it.base : it.base + t0 + 1) / kSlotTile;
-    sinks = a.W ? a.s / kSlotTile : 0;
-    window = a.W ? (max(0, it.base + t0 + n - a.W) + kSlotTile - 1) / kSlotTile : 0;
+  template <typename A>
+  __device__ FullTiles(const A& a, const Item& it, int t0, int n) {
+    const bool window_on = !A::cross && a.W;
+    end = max(0, A::cross || a.tree() ? it.base : it.base + t0 + 1) / kSlotTile;
+    sinks = window_on ? a.s / kSlotTile : 0;
+    window = window_on ? (max(0, it.base + t0 + n - a.W) + kSlotTile - 1) / kSlotTile : 0;
   }
   __device__ bool has(int tile) const { return tile < end && (tile < sinks || tile >= window); }
 };
@@ -128,10 +140,11 @@ struct RowVis {
 // slots end before `end`.  In a tree the row's ancestor bits go to anc, 8 words that only
 // this thread writes; a bad parent sets *err and counts as none.  The walk up the tree, a
 // chain of dependent loads, is made only where a drafted slot or a window needs it.
-__device__ __forceinline__ RowVis row_vis(const AttendArgs& a, const Item& it, int i, bool live,
+template <typename A>
+__device__ __forceinline__ RowVis row_vis(const A& a, const Item& it, int i, bool live,
                                           int end, uint32_t* anc, int* err) {
   RowVis r{0, 0, 0, it.base, nullptr};
-  const bool walk = a.parent && (a.W || end > it.base);
+  const bool walk = a.tree() && (a.W || end > it.base);
   if (walk) {
 #pragma unroll
     for (int w = 0; w < kMaxTree / 32; ++w) anc[w] = 0;
@@ -165,8 +178,9 @@ __device__ __forceinline__ RowVis row_vis(const AttendArgs& a, const Item& it, i
         x = __ldg(par + x);
       }
   }
-  if (a.parent || a.cross) r.hi = it.base;
+  if (A::cross || a.tree()) r.hi = it.base;
   r.hi = max(r.hi, 0);
+  // (CrossArgs::W is 0; with a constant here ptxas 13.0.88 finds no registers for k_attend_few<bf16, 8>)
   r.lo = a.W ? min(max(0, p - a.W + 1), r.hi) : 0;
   r.end_s = min(a.s, r.lo);
   return r;
@@ -220,8 +234,8 @@ __device__ __forceinline__ long long warp_total(long long x) {
   return x;
 }
 
-template <typename I>
-__device__ __forceinline__ Run plan_run_of(const AttendArgs& a, PlanSmem* ps, int n) {
+template <typename I, typename A>
+__device__ __forceinline__ Run plan_run_of(const A& a, PlanSmem* ps, int n) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int items = a.U * a.QB;
   const int per = (items + n - 1) / n, i0 = min(items, tid * per), i1 = min(items, i0 + per);
@@ -312,15 +326,17 @@ __device__ __forceinline__ Run plan_run_of(const AttendArgs& a, PlanSmem* ps, in
 // Every thread of the block takes part (n threads, a multiple of 32).  Returns the CTA's run
 // (left == 0: none); ps->rec holds the split item that starts in it, ps->err any fault of
 // the lengths.
-__device__ __forceinline__ Run plan_run(const AttendArgs& a, PlanSmem* ps, int n) {
+template <typename A>
+__device__ __forceinline__ Run plan_run(const A& a, PlanSmem* ps, int n) {
   return a.wide ? plan_run_of<long long>(a, ps, n) : plan_run_of<int>(a, ps, n);
 }
 
 // A CTA's segments in order: each is a run of tiles of one item.
+template <typename A>
 struct Segments {
   Item it;
   int qb, off, cnt, left, L, T;
-  __device__ Segments(const AttendArgs& a, const Run& r) : qb(r.qb), off(r.off), left(r.left) {
+  __device__ Segments(const A& a, const Run& r) : qb(r.qb), off(r.off), left(r.left) {
     it.u = r.u;
     if (left > 0) {
       unit(a);
@@ -331,7 +347,7 @@ struct Segments {
     L = unit_len(a, it.u);
     T = unit_tokens(a, it.u);
   }
-  __device__ void load(const AttendArgs& a) {
+  __device__ void load(const A& a) {
     it = make_item(a, it.u, qb, L, T);
     cnt = min(left, it.nt - off);
   }
@@ -339,7 +355,7 @@ struct Segments {
   __device__ bool whole() const { return off == 0 && cnt == it.nt; }
   __device__ int end() const { return (it.tile(off + cnt - 1) + 1) * kSlotTile; }
   __device__ int slot(int cta) const { return off == 0 ? 2 * cta + 1 : 2 * cta; }
-  __device__ void next(const AttendArgs& a) {
+  __device__ void next(const A& a) {
     left -= cnt;
     off = 0;
     if (left <= 0) return;
@@ -397,6 +413,6 @@ __device__ __forceinline__ void store_row4(__nv_bfloat16* p, float4 x) {
   *(uint2*)p = v;
 }
 
-cudaError_t launch_attend_tc(const CacheShape& s, const AttendArgs& a, int G, cudaStream_t st);
+cudaError_t launch_attend_tc(const CacheShape& s, const AttendArgs& a, bool cross, int G, cudaStream_t st);
 
 }  // namespace grkv

@@ -67,6 +67,50 @@ struct Status {
     if (threadIdx.x == 0) *word = *at;
   }
 };
+// The status of a call whose blocks are one cluster of up to kMaxSolo, of which the first writes it whole,
+// which saves small calls the memset in front of them (`solo`, the cluster's blocks); or, with 0, of one
+// whose blocks add their faults to a cleared word.  Every thread of the block runs to end().
+constexpr int kMaxSolo = 8;
+struct ClusterStatus {
+  struct Smem {
+    int err, all[kMaxSolo];
+  };
+  int* word;
+  Smem* sm;
+  int solo;
+  __device__ ClusterStatus(int* word_, Smem* sm_, int solo_) : word(word_), sm(sm_), solo(solo_) {
+    if (solo == 0) return;
+    if (threadIdx.x == 0) sm->err = 0;
+    __syncthreads();
+    // every block has started once this is waited for, in end()
+    if (solo > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  }
+  __device__ int* at() const { return solo ? &sm->err : word; }   // where faults go
+  __device__ void end() const {
+    if (solo == 0) return;
+    __syncthreads();
+    if (solo == 1) {
+      if (threadIdx.x == 0) *word = sm->err;
+      return;
+    }
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    if (threadIdx.x == 0) {
+      uint32_t to;   // this block's word in the first block's shared memory
+      asm("mapa.shared::cluster.u32 %0, %1, 0;"
+          : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(&sm->all[blockIdx.x])));
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to), "r"(sm->err) : "memory");
+    }
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+      int err = 0;
+      for (int x = 0; x < solo; ++x) err = min(err, sm->all[x]);
+      *word = err;
+    }
+  }
+};
+
 inline Table table_of(const CacheShape& s) { return Table{s.U, s.cols, s.P, s.shift}; }
 
 struct RowMove {

@@ -48,8 +48,8 @@ __device__ __forceinline__ float4 ld4(const __nv_bfloat16* p) {
                      __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) k_attend_simt(AttendArgs a) {
+template <typename T, typename A>
+__global__ void __launch_bounds__(kThreads, 2) k_attend_simt(A a) {
   using Lay = SimtLayout<T>;
   extern __shared__ __align__(16) uint8_t sm[];
   float* qs = (float*)(sm + Lay::kOffQ);
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_simt(AttendArgs a) {
   const Run run = plan_run(a, plan, kThreads);
   int err = 0;
 
-  for (Segments sg(a, run); sg.more(); sg.next(a)) {
+  for (Segments<A> sg(a, run); sg.more(); sg.next(a)) {
     const Item& it = sg.it;
     const FullTiles full_tiles(a, it, it.tok0, it.ntok);
     T* const kv[2] = {(T*)(sm + Lay::kOffKv), (T*)(sm + Lay::kOffKv + Lay::kSubBytes)};
@@ -260,8 +260,8 @@ struct FewSmem {
 };
 static_assert(sizeof(FewSmem<8>) <= 113 * 1024, "two CTAs per SM");
 
-template <typename T, int R>
-__global__ void __launch_bounds__(kFewThreads, R <= 8 ? 2 : 1) k_attend_few(AttendArgs a) {
+template <typename T, int R, typename A>
+__global__ void __launch_bounds__(kFewThreads, R <= 8 ? 2 : 1) k_attend_few(A a) {
   constexpr int S = 32 / R;   // slots of a step
   extern __shared__ __align__(16) uint8_t sm_few[];
   FewSmem<R>& sm = *(FewSmem<R>*)sm_few;
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(kFewThreads, R <= 8 ? 2 : 1) k_attend_few(Atte
   const Run run = plan_run(a, &sm.plan, kFewThreads);
   int err = 0;
 
-  for (Segments sg(a, run); sg.more(); sg.next(a)) {
+  for (Segments<A> sg(a, run); sg.more(); sg.next(a)) {
     const Item& it = sg.it;
     const FullTiles full(a, it, it.tok0, it.ntok);
     float4 q[R], o[R];
@@ -562,12 +562,12 @@ cudaError_t launch_main(void (*kern)(Args...), int G, int threads, uint32_t smem
   return launch_kernel(false, 1, kern, dim3(G), threads, smem, st, args...);
 }
 
-template <typename T>
-cudaError_t launch_simt(const AttendArgs& a, int G, cudaStream_t st) {
-  if (a.rows <= 4) return launch_main(k_attend_few<T, 4>, G, kFewThreads, sizeof(FewSmem<4>), st, a);
-  if (a.rows <= 8) return launch_main(k_attend_few<T, 8>, G, kFewThreads, sizeof(FewSmem<8>), st, a);
-  if (a.rows <= 16) return launch_main(k_attend_few<T, 16>, G, kFewThreads, sizeof(FewSmem<16>), st, a);
-  return launch_main(k_attend_simt<T>, G, kThreads, SimtLayout<T>::kBytes, st, a);
+template <typename T, typename A>
+cudaError_t launch_simt(const A& a, int G, cudaStream_t st) {
+  if (a.rows <= 4) return launch_main(k_attend_few<T, 4, A>, G, kFewThreads, sizeof(FewSmem<4>), st, a);
+  if (a.rows <= 8) return launch_main(k_attend_few<T, 8, A>, G, kFewThreads, sizeof(FewSmem<8>), st, a);
+  if (a.rows <= 16) return launch_main(k_attend_few<T, 16, A>, G, kFewThreads, sizeof(FewSmem<16>), st, a);
+  return launch_main(k_attend_simt<T, A>, G, kThreads, SimtLayout<T>::kBytes, st, a);
 }
 
 }  // namespace
@@ -626,7 +626,6 @@ cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, con
   a.W = s.W;
   a.s = s.s;
   a.withhold = s.test_timeout;
-  a.cross = io.cross;
   a.sl2 = (float)((double)s.scale * 1.4426950408889634);
   a.rec = (AttendRec*)(ws + L.rec);
   a.pml = (float2*)(ws + L.pml);
@@ -642,9 +641,12 @@ cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, con
   if (sms <= 0 || sms > kMaxAttendSms) return cudaErrorInvalidDevice;
   const int G = sms * ctas_per_sm(s, a.rows);
   const bool f32 = s.dtype == GRKV_F32;
-  cudaError_t e = f32      ? launch_simt<float>(a, G, st)
-                  : s.simt ? launch_simt<__nv_bfloat16>(a, G, st)
-                           : launch_attend_tc(s, a, G, st);
+  auto simt = [&](const auto& x) {
+    return f32 ? launch_simt<float>(x, G, st) : launch_simt<__nv_bfloat16>(x, G, st);
+  };
+  const cudaError_t e = !f32 && !s.simt ? launch_attend_tc(s, a, io.cross, G, st)
+                        : io.cross      ? simt(CrossArgs{a})
+                                        : simt(a);
   if (e != cudaSuccess) return e;
   return f32 ? launch_join<float>(a, G, st) : launch_join<__nv_bfloat16>(a, G, st);
 }

@@ -261,7 +261,8 @@ __device__ __forceinline__ bool clean_row(uint8_t* tile, int row) {
 
 // Adds the non-finite values of the slots that a row sees to its output in TMEM (all lanes of the
 // warp).  A function of its own: the epilogue's registers stay registers.
-__device__ __noinline__ void add_bad(const AttendArgs& a, const Item& it, int off, int cnt,
+template <typename A>
+__device__ __noinline__ void add_bad(const A& a, const Item& it, int off, int cnt,
                                      const RowVis& vis, const uint4* bad, bool live, uint32_t taddr) {
   int err = 0;
   for (int c0 = 0; c0 < kD; c0 += 32) {
@@ -297,10 +298,10 @@ __device__ __noinline__ void add_bad(const AttendArgs& a, const Item& it, int of
   tmem_st_wait();
 }
 
-template <int NQ>
+template <int NQ, typename A>
 __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
     k_attend_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                const __grid_constant__ CUtensorMap tmV, const __grid_constant__ AttendArgs a) {
+                const __grid_constant__ CUtensorMap tmV, const __grid_constant__ A a) {
   using Lay = TcLayout<NQ>;
   extern __shared__ __align__(1024) uint8_t smraw[];
   uint8_t* sm = (uint8_t*)(((uintptr_t)smraw + 1023) & ~(uintptr_t)1023);
@@ -341,7 +342,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
     int seg = 0;
     Ring pos;
     bool ok = true;
-    for (Segments sg(a, run); ok && sg.more(); sg.next(a), ++seg) {
+    for (Segments<A> sg(a, run); ok && sg.more(); sg.next(a), ++seg) {
       const Item& it = sg.it;
       const int qb = seg % Lay::kQBufs, quse = seg / Lay::kQBufs;
       if (quse >= 1) ok = wait_warp(&bars->q_empty[qb], (quse - 1) & 1, abort_flag);
@@ -414,7 +415,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
     const uint64_t v_desc = sw128_desc(smem_u32(sm + Lay::kOffRing + kTileBytes), kTileBytes / 2, 1024);
     auto wait = [&](uint64_t* bar, uint32_t parity) { return wait_warp(bar, parity, abort_flag); };
     // segments: the S products' (ahead), and the lengths of those the output's have yet to start
-    Segments qs(a, run);
+    Segments<A> qs(a, run);
     int q_left = 0, q_seg = -1, v_left = 0, v_seg = -1, next1 = 0, next2 = 0;
     uint32_t qb = 0;
     bool v_first = false;
@@ -552,7 +553,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
       withhold = false;
     };
     bool ok = true;
-    for (Segments sg(a, run); ok && sg.more(); sg.next(a), ++seg) {
+    for (Segments<A> sg(a, run); ok && sg.more(); sg.next(a), ++seg) {
       const Item& it = sg.it;
       const FullTiles full(a, it, it.tok0, it.ntok);
       int e = 0;
@@ -590,7 +591,7 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
     uint32_t n = w, edges = 0;
     int seg = 0;
     bool ok = true;
-    for (Segments sg(a, run); ok && sg.more(); sg.next(a), ++seg) {
+    for (Segments<A> sg(a, run); ok && sg.more(); sg.next(a), ++seg) {
       const Item& it = sg.it;
       int h, i;
       const bool live = row_of(a, it, w, row, &h, &i);
@@ -793,10 +794,10 @@ __global__ void __launch_bounds__(TcLayout<NQ>::kThreads, 1)
   }
 }
 
-template <int NQ>
-cudaError_t launch_tc(const AttendArgs& a, const CUtensorMap& mq, const CUtensorMap& mk,
+template <int NQ, typename A>
+cudaError_t launch_tc(const A& a, const CUtensorMap& mq, const CUtensorMap& mk,
                       const CUtensorMap& mv, int G, cudaStream_t st) {
-  auto kern = k_attend_tc<NQ>;
+  auto kern = k_attend_tc<NQ, A>;
   const uint32_t smem = TcLayout<NQ>::kBytes;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
@@ -806,13 +807,16 @@ cudaError_t launch_tc(const AttendArgs& a, const CUtensorMap& mq, const CUtensor
 
 }  // namespace
 
-cudaError_t launch_attend_tc(const CacheShape& s, const AttendArgs& a, int G, cudaStream_t st) {
+cudaError_t launch_attend_tc(const CacheShape& s, const AttendArgs& a, bool cross, int G, cudaStream_t st) {
   CUtensorMap mq, mk, mv;
   if (!encode_bf16_3d(&mq, a.q, kD, s.t, (uint64_t)s.U * s.g, 64, a.T, s.g) ||
       !encode_bf16_3d(&mk, a.k, kD, s.page, s.P, 64, s.page) ||
       !encode_bf16_3d(&mv, a.v, kD, s.page, s.P, 64, s.page))
     return cudaErrorInvalidValue;
-  return a.nq == 1 ? launch_tc<1>(a, mq, mk, mv, G, st) : launch_tc<2>(a, mq, mk, mv, G, st);
+  auto launch = [&](const auto& x) {
+    return a.nq == 1 ? launch_tc<1>(x, mq, mk, mv, G, st) : launch_tc<2>(x, mq, mk, mv, G, st);
+  };
+  return cross ? launch(CrossArgs{a}) : launch(a);
 }
 
 }  // namespace grkv

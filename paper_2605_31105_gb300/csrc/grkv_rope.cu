@@ -104,30 +104,39 @@ struct RowsArgs {
   float sign;             // -1: transposed
 };
 
-constexpr int kRowThreads = 256;
+constexpr int kRowThreads = 256, kRowHeads = 4;   // heads in flight to a thread
 
+// kThreads threads a token.  The first heads' rows are on their way while the angles are formed.
 template <typename T, Hold H>
 __global__ void __launch_bounds__(kRowThreads)
     k_rope_rows(const __grid_constant__ RopeArgs r, const __grid_constant__ RowsArgs a) {
   constexpr int kThr = Pair<T, H>::kThreads;
   const int64_t n = (int64_t)blockIdx.x * (kRowThreads / kThr) + threadIdx.x / kThr;
   if (n >= (int64_t)a.S * a.t) return;
-  const int s = (int)(n / a.t), i = (int)(n - (int64_t)s * a.t);
+  const int s = (int)n / a.t, i = (int)n - s * a.t;   // S t <= 2^30
   const int64_t p = a.pos ? a.pos[n] : (int64_t)(a.start ? a.start[s] : 0) + i;
-  if (p < 0) return;
   const Place<T, H> at(threadIdx.x % kThr, r.half);
-  const Angles<T, H> an = angles<T, H>(r, at, p, r.amp, a.sign);
   const T* in = (const T*)a.in + s * a.is[0] + i * a.is[2];
   T* out = (T*)a.out + s * a.os[0] + i * a.os[2];
-  const int h1 = min(a.H, (int)(blockIdx.y + 1) * a.heads);
-  for (int h0 = blockIdx.y * a.heads; h0 < h1; h0 += 4) {
-    Raw<T, H> x[4];
+  int h = blockIdx.y * a.heads;
+  const int h1 = min(a.H, h + a.heads);
+  Raw<T, H> x[kRowHeads];
+  auto load = [&]() {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (h0 + j < h1) x[j] = load_pair<T, H>(in + (h0 + j) * a.is[1], at);
+    for (int j = 0; j < kRowHeads; ++j)
+      if (h + j < h1) x[j] = load_pair<T, H>(in + (h + j) * a.is[1], at);
+  };
+  load();
+  Angles<T, H> an(r, at);
+  if (p < 0) return;
+  an.set(turn_by(p, r.amp, a.sign));
+  while (true) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (h0 + j < h1) store_pair<T, H>(out + (h0 + j) * a.os[1], at, rotate<T, H>(x[j], at, an));
+    for (int j = 0; j < kRowHeads; ++j)
+      if (h + j < h1) store_pair<T, H>(out + (h + j) * a.os[1], at, rotate<T, H>(x[j], at, an));
+    h += kRowHeads;
+    if (h >= h1) break;
+    load();
   }
 }
 
@@ -161,51 +170,67 @@ struct AppendRopeArgs {
   int g;
 };
 
-constexpr int kAppendThreads = 128;
+constexpr int kAppendThreads = 128, kAppendHeads = 4;
 
-// kThreads threads a token: its new key and value, and its queries.
+// kThreads threads a token: its new key and value, and its queries.  Rows are asked for before the
+// table's entry that says where they go.
 template <typename T, Hold H>
 __global__ void __launch_bounds__(kAppendThreads)
-    k_append_rope(const __grid_constant__ RopeArgs r, const __grid_constant__ AppendRopeArgs a) {
+    k_append_rope(const __grid_constant__ RopeArgs r, const __grid_constant__ AppendRopeArgs a, int* word,
+                  int solo) {
+  __shared__ ClusterStatus::Smem shared;
+  const ClusterStatus st(word, &shared, solo);
   constexpr int kThr = Pair<T, H>::kThreads;
-  const RowMove& m = a.m;
-  const int64_t n = (int64_t)blockIdx.x * (kAppendThreads / kThr) + threadIdx.x / kThr;
-  if (n >= (int64_t)m.tb.U * m.t) return;
-  const int u = (int)(n / m.t), i = (int)(n - (int64_t)u * m.t);
-  const int cnt = rows_of(m, u);
-  if (i >= cnt) return;
-  const Place<T, H> at(threadIdx.x % kThr, r.half);
-  // the length as it is: clamped to the table, rows behind it would go over those before
-  const long long slot = (long long)m.len[u] - cnt + i;
-  const long long f = a.first ? a.first[u] : (long long)u * m.t;
-  const bool has = f >= 0 && f <= a.new_rows - 1 - i;
-  int64_t p = slot + (a.offset ? a.offset[u] : 0);
-  if (a.pos) p = has ? a.pos[f + i] : -1;
-  long long to = -1;
-  if (has && p >= 0 && slot >= 0 && slot < m.tb.cols << m.tb.shift)
-    to = pool_row(m.tb, a.table, u, (int)slot, m.status);
-  else
-    set_status(m.status, GRKV_ERR_INVALID_ARG);
-  if (p < 0) return;
-  const Angles<T, H> an = angles<T, H>(r, at, p, r.amp, 1.f);
-  if (to >= 0) {
-    const Raw<T, H> k = load_pair<T, H>((const T*)a.k_new + (f + i) * kD, at);
-    const Raw<T, H> v = load_pair<T, H>((const T*)a.v_new + (f + i) * kD, at);
-    store_pair<T, H>((T*)a.k + to * kD, at, rotate<T, H>(k, at, an));
-    store_pair<T, H>((T*)a.v + to * kD, at, v);
-  }
-  if (!a.q) return;
-  const int64_t row = ((int64_t)u * a.g * m.t + i) * kD, step = (int64_t)m.t * kD;
-  for (int h0 = 0; h0 < a.g; h0 += 4) {
-    Raw<T, H> x[4];
+  RowMove m = a.m;
+  m.status = st.at();
+  const int n = blockIdx.x * (kAppendThreads / kThr) + threadIdx.x / kThr;   // U t <= 2^28
+  const int u = n / m.t, i = n - u * m.t;
+  const int cnt = u < m.tb.U ? rows_of(m, u) : 0;
+  if (i < cnt) {
+    const Place<T, H> at(threadIdx.x % kThr, r.half);
+    // the length as it is: clamped to the table, rows behind it would go over those before
+    const long long slot = (long long)m.len[u] - cnt + i;
+    const long long f = a.first ? a.first[u] : (long long)u * m.t;
+    const bool has = f >= 0 && f <= a.new_rows - 1 - i;
+    Raw<T, H> k, v, x[kAppendHeads];
+    if (has) {
+      k = load_pair<T, H>((const T*)a.k_new + (f + i) * kD, at);
+      v = load_pair<T, H>((const T*)a.v_new + (f + i) * kD, at);
+    }
+    const int64_t row = ((int64_t)u * a.g * m.t + i) * kD, step = (int64_t)m.t * kD;
+    const int g = a.q ? a.g : 0;
+    int h = 0;
+    auto load = [&]() {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (h0 + j < a.g) x[j] = load_pair<T, H>((const T*)a.q + row + (h0 + j) * step, at);
+      for (int j = 0; j < kAppendHeads; ++j)
+        if (h + j < g) x[j] = load_pair<T, H>((const T*)a.q + row + (h + j) * step, at);
+    };
+    load();
+    int64_t p = slot + (a.offset ? a.offset[u] : 0);
+    if (a.pos) p = has ? a.pos[f + i] : -1;
+    long long to = -1;
+    if (has && p >= 0 && slot >= 0 && slot < m.tb.cols << m.tb.shift)
+      to = pool_row(m.tb, a.table, u, (int)slot, m.status);
+    else
+      set_status(m.status, GRKV_ERR_INVALID_ARG);
+    if (p >= 0) {
+      Angles<T, H> an(r, at);
+      an.set(turn_by(p, r.amp, 1.f));
+      if (to >= 0) {
+        store_pair<T, H>((T*)a.k + to * kD, at, rotate<T, H>(k, at, an));
+        store_pair<T, H>((T*)a.v + to * kD, at, v);
+      }
+      while (h < g) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (h0 + j < a.g)
-        store_pair<T, H>((T*)a.q_out + row + (h0 + j) * step, at, rotate<T, H>(x[j], at, an));
+        for (int j = 0; j < kAppendHeads; ++j)
+          if (h + j < g)
+            store_pair<T, H>((T*)a.q_out + row + (h + j) * step, at, rotate<T, H>(x[j], at, an));
+        h += kAppendHeads;
+        load();
+      }
+    }
   }
+  st.end();
 }
 
 // ----------------------------------------------------------------------- compact
@@ -221,28 +246,44 @@ __device__ __forceinline__ int64_t turn_of(const CompactRopeArgs& a, int u, int 
   return a.turn ? a.turn[x] : (int64_t)(a.first ? a.first[u] : 0) + i - a.idx[x];
 }
 
-constexpr int kTurnThreads = 128;
+constexpr int kTurnThreads = 128, kTurnUnroll = 2;
 
-// To other pages: every row by itself, kThreads threads a row.
+// To other pages: every row by itself, kThreads threads a row, two rows in flight to a thread.
 template <typename T, Hold H>
 __global__ void __launch_bounds__(kTurnThreads)
     k_gather_rope(const __grid_constant__ RopeArgs r, const __grid_constant__ CompactRopeArgs a) {
-  constexpr int kThr = Pair<T, H>::kThreads;
+  constexpr int kThr = Pair<T, H>::kThreads, kRows = kTurnThreads / kThr;
   const RowMove& m = a.m;
   const Place<T, H> at(threadIdx.x % kThr, r.half);
-  const int i = blockIdx.x * (kTurnThreads / kThr) + threadIdx.x / kThr;
+  Angles<T, H> an(r, at);
+  const int i0 = blockIdx.x * (kRows * kTurnUnroll) + threadIdx.x / kThr;
   for (int u = blockIdx.y; u < m.tb.U; u += gridDim.y) {
-    const int len = m.tb.clamped(m.len[u], m.status);
-    long long from, to;
-    if (i >= rows_of(m, u) ||
-        !kept_row(m, a.idx, a.table_in, len, a.table_out, a.first, false, u, i, &from, &to))
-      continue;
-    Raw<T, H> k = load_pair<T, H>((const T*)a.k + from * kD, at);
-    const Raw<T, H> v = load_pair<T, H>((const T*)a.v + from * kD, at);
-    const int64_t p = turn_of(a, u, i);
-    if (p != 0) k = rotate<T, H>(k, at, angles<T, H>(r, at, p, 1.f, 1.f));
-    store_pair<T, H>((T*)a.k + to * kD, at, k);
-    store_pair<T, H>((T*)a.v + to * kD, at, v);
+    const int len = m.tb.clamped(m.len[u], m.status), n = rows_of(m, u);
+    Raw<T, H> k[kTurnUnroll], v[kTurnUnroll];
+    long long to[kTurnUnroll];
+    int64_t p[kTurnUnroll];
+#pragma unroll
+    for (int j = 0; j < kTurnUnroll; ++j) {
+      const int i = i0 + j * kRows;
+      long long from;
+      if (i >= n || !kept_row(m, a.idx, a.table_in, len, a.table_out, a.first, false, u, i, &from, &to[j])) {
+        to[j] = -1;
+        continue;
+      }
+      p[j] = turn_of(a, u, i);
+      k[j] = load_pair<T, H>((const T*)a.k + from * kD, at);
+      v[j] = load_pair<T, H>((const T*)a.v + from * kD, at);
+    }
+#pragma unroll
+    for (int j = 0; j < kTurnUnroll; ++j) {
+      if (to[j] < 0) continue;
+      store_pair<T, H>((T*)a.v + to[j] * kD, at, v[j]);
+      if (p[j] != 0) {
+        an.set(turn_by(p[j], 1.f, 1.f));
+        k[j] = rotate<T, H>(k[j], at, an);
+      }
+      store_pair<T, H>((T*)a.k + to[j] * kD, at, k[j]);
+    }
   }
 }
 
@@ -266,9 +307,11 @@ __global__ void __launch_bounds__(kShiftRopeThreads)
   T* pool = (T*)(keys ? a.k : a.v);
   const Place<T, H> at(blockIdx.z * kThr + threadIdx.x % kThr, r.half);
   const int n = rows_of(m, u), len = m.tb.clamped(m.len[u], m.status);
+  Angles<T, H> an(r, at);
   for (int base = 0; base < n; base += kRows * kShiftRopeUnroll) {
     Raw<T, H> x[kShiftRopeUnroll];
     long long to[kShiftRopeUnroll];
+    int64_t by[kShiftRopeUnroll];
 #pragma unroll
     for (int j = 0; j < kShiftRopeUnroll; ++j) {
       const int i = base + j * kRows + r0;
@@ -281,15 +324,21 @@ __global__ void __launch_bounds__(kShiftRopeThreads)
           continue;
         }
         x[j] = load_pair<T, H>(pool + from * kD, at);
-        if (p != 0) x[j] = rotate<T, H>(x[j], at, angles<T, H>(r, at, p, 1.f, 1.f));
+        by[j] = p;
       } else {
         to[j] = -1;
       }
     }
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kShiftRopeUnroll; ++j)
-      if (to[j] >= 0) store_pair<T, H>(pool + to[j] * kD, at, x[j]);
+    for (int j = 0; j < kShiftRopeUnroll; ++j) {
+      if (to[j] < 0) continue;
+      if (by[j] != 0) {
+        an.set(turn_by(by[j], 1.f, 1.f));
+        x[j] = rotate<T, H>(x[j], at, an);
+      }
+      store_pair<T, H>(pool + to[j] * kD, at, x[j]);
+    }
     __syncthreads();
   }
 }
@@ -346,7 +395,8 @@ int grkv_rope_rows(const grkv_rope* rope, const grkv_rows* s, const void* in, vo
     constexpr Hold H = decltype(hold)::value;
     const int per = kRowThreads / Pair<T, H>::kThreads;
     const int64_t blocks = ((int64_t)a.S * a.t + per - 1) / per;
-    a.heads = a.H;
+    // all heads of a token by one thread's angles, or four, where that leaves SMs without work
+    a.heads = blocks * ((a.H + kRowHeads - 1) / kRowHeads) <= 1216 ? kRowHeads : a.H;
     count_launches(1);
     return launch_kernel(false, 1, k_rope_rows<T, H>,
                          dim3((unsigned)blocks, (unsigned)((a.H + a.heads - 1) / a.heads)), kRowThreads, 0,
@@ -378,18 +428,22 @@ int grkv_cache_append_rope(const grkv_cache_params* p, const grkv_rope* rope, co
   GRKV_TRY(check_optional(q, 16));
   GRKV_TRY(check_optional(q_out, 16));
   cudaStream_t st = (cudaStream_t)stream;
-  GRKV_TRY(clear_status((char*)ws, L, st));
-  if (s.U == 0) return GRKV_OK;
-  const RowMove m{table_of(s), s.t, count, len, (int*)((char*)ws + L.status)};
+  if (s.U == 0) return clear_status((char*)ws, L, st);
+  const RowMove m{table_of(s), s.t, count, len, nullptr};
   const AppendRopeArgs a{m, k_new, v_new, q, q_out, k_pages, v_pages, first_row,
                          first_row ? (long long)new_rows : (long long)s.U * s.t, table, pos, offset, s.g};
   return cuda_rc(dispatch(s.dtype, rope, [&](auto zero, auto hold) {
     using T = decltype(zero);
     constexpr Hold H = decltype(hold)::value;
-    const int per = kAppendThreads / Pair<T, H>::kThreads;
+    const int per = kAppendThreads / Pair<T, H>::kThreads, blocks = (int)(((int64_t)s.U * s.t + per - 1) / per);
+    const int solo = blocks <= kMaxSolo ? blocks : 0;
+    if (!solo) {
+      const cudaError_t e = cudaMemsetAsync((char*)ws + L.status, 0, 4, st);
+      if (e != cudaSuccess) return e;
+    }
     count_launches(1);
-    return launch_kernel(false, 1, k_append_rope<T, H>,
-                         dim3((unsigned)(((int64_t)s.U * s.t + per - 1) / per)), kAppendThreads, 0, st, r, a);
+    return launch_kernel(false, solo, k_append_rope<T, H>, dim3((unsigned)blocks), kAppendThreads, 0, st, r, a,
+                         (int*)((char*)ws + L.status), solo);
   }));
 }
 
@@ -421,7 +475,7 @@ int grkv_cache_compact_rope(const grkv_cache_params* p, const grkv_rope* rope, c
     if (table_in == table_out)
       return launch_kernel(false, 1, k_shift_rope<T, H>, dim3(s.U, 2, ShiftPart<T, H>::kParts),
                            kShiftRopeThreads, 0, st, r, a);
-    const int per = kTurnThreads / Pair<T, H>::kThreads;
+    const int per = kTurnUnroll * kTurnThreads / Pair<T, H>::kThreads;
     return launch_kernel(false, 1, k_gather_rope<T, H>,
                          dim3((unsigned)((s.t + per - 1) / per), (unsigned)std::min(s.U, 65535)),
                          kTurnThreads, 0, st, r, a);

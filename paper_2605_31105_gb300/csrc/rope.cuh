@@ -56,37 +56,65 @@ struct Place {
   }
 };
 
+// By how many positions a row is turned: `by` forwards, or backwards where sin is negative, which is a's
+// factor of the sines; cos, that of the cosines, is a.
+struct Turn {
+  uint32_t by;
+  float cos, sin;
+};
+__device__ __forceinline__ Turn turn_by(int64_t p, float amp, float sign) {
+  return Turn{(uint32_t)(p < 0 ? -p : p), amp, p < 0 ? -amp * sign : amp * sign};
+}
+
+// Cosine and sine of the fraction f 2^-32 of a turn.  fp32: the nearest quarter, and a rest of at most an
+// eighth of a turn, which fp32 holds to 2^-28, through the Taylor polynomials of both to the 9th
+// and 10th power (the next terms are below 2^-28): off by 2^-23 at most.
+__device__ __forceinline__ void cos_sin(uint32_t f, float* c, float* s) {
+  const uint32_t quarter = (f + (1u << 29)) >> 30;   // 0..3
+  const float x = (float)(int32_t)(f - (quarter << 30)) * 1.46291807926715968e-9f;   // 2 pi 2^-32
+  const float z = x * x;
+  float a = fmaf(z, 2.75573192e-6f, -1.98412698e-4f);
+  a = fmaf(z, a, 8.33333333e-3f);
+  a = fmaf(z, a, -1.66666667e-1f);
+  a = fmaf(x * z, a, x);
+  float b = fmaf(z, -2.75573192e-7f, 2.48015873e-5f);
+  b = fmaf(z, b, -1.38888889e-3f);
+  b = fmaf(z, b, 4.16666667e-2f);
+  b = fmaf(z, b, -0.5f);
+  b = fmaf(z, b, 1.f);
+  const bool odd = quarter & 1;
+  *c = __uint_as_float(__float_as_uint(odd ? a : b) ^ (((quarter + 1) & 2) << 30));
+  *s = __uint_as_float(__float_as_uint(odd ? b : a) ^ ((quarter & 2) << 30));
+}
+// bf16: the special function unit's, over one turn around 0, off by 2^-20.5 at most (2^-21.2 of its
+// own, the rest the angle's rounding), a 2000th of the output's.  Kept rows turn by angles of their own, and
+// with the polynomials issue slots bound them beside memory.
+__device__ __forceinline__ void cos_sin_bf16(uint32_t f, float* c, float* s) {
+  __sincosf((float)(int32_t)f * 1.46291807926715968e-9f, s, c);
+}
+
 template <typename T, Hold H>
 struct Angles {
-  float c[Pair<T, H>::kVec], s[Pair<T, H>::kVec];
-};
+  static constexpr int kVec = Pair<T, H>::kVec;
+  uint64_t turns[kVec];   // a position
+  float c[kVec], s[kVec];
 
-// Cosine and sine of p turns, times amp.  The fraction's upper 32 bits (error 2^-33 turns) are split
-// into the nearest quarter and a rest of at most an eighth of a turn, which fp32 holds to 2^-27:
-// the angle is off by 2.4e-8 at most.
-__device__ __forceinline__ void turn(uint64_t per_position, int64_t p, float amp, float* c, float* s) {
-  const int32_t f = (int32_t)((per_position * (uint64_t)p + 0x80000000u) >> 32);
-  const int32_t quarter = (int32_t)(((uint32_t)f + (1u << 29)) >> 30);   // 0..3
-  const int32_t rest = (int32_t)((uint32_t)f - ((uint32_t)quarter << 30));
-  float x, y;
-  sincospif((float)rest * 0x1p-31f, &y, &x);
-  const bool odd = quarter & 1;
-  const float cc = odd ? y : x, ss = odd ? x : y;
-  *c = amp * (((quarter + 1) & 2) ? -cc : cc);
-  *s = amp * ((quarter & 2) ? -ss : ss);
-}
-
-template <typename T, Hold H>
-__device__ __forceinline__ Angles<T, H> angles(const RopeArgs& r, const Place<T, H>& at, int64_t p,
-                                               float amp, float sign) {
-  Angles<T, H> x;
+  __device__ __forceinline__ Angles(const RopeArgs& r, const Place<T, H>& at) {
 #pragma unroll
-  for (int i = 0; i < Pair<T, H>::kVec; ++i) {
-    turn(r.turns[at.pair + i], p, amp, &x.c[i], &x.s[i]);
-    x.s[i] *= sign;
+    for (int i = 0; i < kVec; ++i) turns[i] = r.turns[at.pair + i];
   }
-  return x;
-}
+  __device__ __forceinline__ void set(const Turn& t) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      // (the lower half rounds the upper one: 2^-33 turns)
+      const uint32_t f = (uint32_t)((turns[i] * t.by + 0x80000000u) >> 32);
+      if (sizeof(T) == 4) cos_sin(f, &c[i], &s[i]);
+      else cos_sin_bf16(f, &c[i], &s[i]);
+      c[i] *= t.cos;
+      s[i] *= t.sin;
+    }
+  }
+};
 
 template <typename T, Hold H>
 __device__ __forceinline__ Raw<T, H> load_pair(const T* row, const Place<T, H>& at) {

@@ -2,9 +2,12 @@
 
 An angle is held to pi 2^-27 radians (a rest of at most an eighth of a turn in fp32) and 2^-32 turns
 (the upper half of the 64-bit fraction) and its frequency to some 2^-51 of itself, so to
-delta = 2^-25 + p f 2^-50.  Cosine and sine add 2 units in the last place, 2^-23; times a (itself
-rounded) 2 x 2^-24; the two products and their sum 2 x 2^-24 of |x| + |y|.  So an output is off by
+delta = 2^-25 + p f 2^-50.  Cosine and sine add 2^-23; times a (itself rounded) 2 x 2^-24; the two
+products and their sum 2 x 2^-24 of |x| + |y|.  So an output is off by
   (delta + 2^-23 + 4 x 2^-24) a (|x| + |y|) + half a step of its type.
+In bf16 the angle lies within half a turn, which fp32 rounds by pi 2^-24 twice (from 32 bits, and times
+2 pi), and the special function unit's documented errors are 2^-21.41 and 2^-21.19: together 2^-20 in the
+place of 2^-25 + 2^-23.
 """
 import math
 
@@ -13,6 +16,7 @@ import numpy as np
 from tests.cache_ref import D, ROUND
 
 BIG = 2.0 ** -25 + 2.0 ** -23 + 4 * 2.0 ** -24
+MORE_BF16 = 2.0 ** -20 - 2.0 ** -25 - 2.0 ** -23
 
 
 def freqs(rotary=D, scaling="plain", theta=10000.0, factor=1.0, low=0.0, high=0.0, original=8192.0,
@@ -48,7 +52,7 @@ def pairs(rotary, layout):
     return (i, i + rotary // 2) if layout == "half" else (2 * i, 2 * i + 1)
 
 
-def rotate(x, pos, layout="half", transpose=False, amplitude=None, **kw):
+def rotate(x, pos, layout="half", transpose=False, amplitude=None, dtype="f32", **kw):
     """x [..., D] float64 at positions pos [...] -> rotated, and a bound of the error before the
     output's own rounding."""
     f, a = freqs(**kw)
@@ -61,7 +65,10 @@ def rotate(x, pos, layout="half", transpose=False, amplitude=None, **kw):
         u, v = x[..., i], x[..., j]
         out[..., i] = a * (u * np.cos(ang) - v * np.sin(ang))
         out[..., j] = a * (u * np.sin(ang) + v * np.cos(ang))
-        e = (BIG + np.abs(p * f) * 2.0 ** -50) * a * (np.abs(u) + np.abs(v))
+        both = a * (np.abs(u) + np.abs(v))
+        e = (BIG + np.abs(p * f) * 2.0 ** -50) * both
+        if dtype == "bf16":
+            e = e + MORE_BF16 * both
     err[..., i] = err[..., j] = e
     return out, err
 

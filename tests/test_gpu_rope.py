@@ -41,7 +41,7 @@ def test_rows(grkv_lib, dtype, layout, rotary, transpose):
     pos[1, 2] = pos[2, 6] = -1
     out = torch.full((3, 5, 7, D), 7.0, dtype=C.TORCH[dtype], device="cuda")
     b.grkv_rope_rows(plan(layout, **kw), x.cuda(), out, pos=C.int_dev(pos), transpose=transpose)
-    want, err = R.rotate(x.double().numpy(), pos[:, None], layout, transpose, **kw)
+    want, err = R.rotate(x.double().numpy(), pos[:, None], layout, transpose, dtype=dtype, **kw)
     skip = np.broadcast_to((pos < 0)[:, None, :, None], want.shape)
     want, err = np.where(skip, 7.0, want), np.where(skip, 0.0, err)
     R.check(host(out), want, err, dtype)
@@ -62,12 +62,12 @@ def test_sizes_and_starts(grkv_lib, dtype, s, h, t):
         out = torch.empty(s, h, t, D, dtype=C.TORCH[dtype], device="cuda")
         b.grkv_rope_rows(plan("pairs"), x.cuda(), out, **({name: kw} if name else {}))
         at = p if name else np.broadcast_to(np.arange(t), (s, t))
-        R.check(host(out), *R.rotate(x.double().numpy(), at[:, None], "pairs"), dtype)
+        R.check(host(out), *R.rotate(x.double().numpy(), at[:, None], "pairs", dtype=dtype), dtype)
 
 
 def test_starts_before_the_first_token_and_past_the_last_position(grkv_lib):
     x = normal(np.random.default_rng(1), "f32", 2, 1, 9, D)
-    out = torch.full((2, 1, 9, D), 7.0, device="cuda")
+    out = torch.full((2, 1, 9, D), 7.0, dtype=torch.float32, device="cuda")
     b.grkv_rope_rows(plan(), x.cuda(), out, start=C.int_dev([-4, 2 ** 31 - 3]))
     p = np.array([[-4], [2 ** 31 - 3]]) + np.arange(9)      # not wrapped around
     want, err = R.rotate(x.double().numpy(), p[:, None])
@@ -85,7 +85,7 @@ def test_strides(grkv_lib, dtype, layout, rotary):
     whole = normal(rng, dtype, s, t, 3 * h, D).cuda()
     x = whole[:, :, h:2 * h].transpose(1, 2)
     pos = rng.integers(0, 5000, (s, t))
-    want, err = R.rotate(host(x), pos[:, None], layout, rotary=rotary)
+    want, err = R.rotate(host(x), pos[:, None], layout, rotary=rotary, dtype=dtype)
     out = torch.empty(s, h, t, D, dtype=x.dtype, device="cuda")
     b.grkv_rope_rows(rope, x, out, pos=C.int_dev(pos))
     R.check(host(out), want, err, dtype)
@@ -131,9 +131,9 @@ def test_the_transposed_product_is_the_gradient(grkv_lib, layout, rotary):
     rope = plan(layout, rotary=rotary, amplitude=1.25)
     rng = np.random.default_rng(7)
     up = normal(rng, "f32", 1, 1, 1, D).cuda()
-    grad, zero = torch.empty_like(up), torch.zeros(1, 1, 1, D, device="cuda")
+    grad, zero = torch.empty_like(up), torch.zeros(1, 1, 1, D, dtype=torch.float32, device="cuda")
     b.grkv_rope_rows(rope, up, grad, start=C.int_dev([777]), transpose=True)
-    eye = torch.eye(D, device="cuda").view(1, D, 1, D).contiguous()
+    eye = torch.eye(D, dtype=torch.float32, device="cuda").view(1, D, 1, D).contiguous()
     moved, base = torch.empty_like(eye), torch.empty_like(zero)
     b.grkv_rope_rows(rope, eye, moved, start=C.int_dev([777]))
     b.grkv_rope_rows(rope, zero, base, start=C.int_dev([777]))
@@ -147,7 +147,7 @@ def test_rows_further_apart_than_32_bits(grkv_lib):
     x = torch.zeros(n + D, dtype=torch.bfloat16, device="cuda")
     rows = x.as_strided((1, 2, 1, D), (0, n, 0, 1))
     rows.normal_()
-    want, err = R.rotate(host(rows), np.full((1, 2, 1), 99), "half")
+    want, err = R.rotate(host(rows), np.full((1, 2, 1), 99), "half", dtype="bf16")
     b.grkv_rope_rows(plan(), rows, rows, start=C.int_dev([99]))
     R.check(host(rows), want, err, "bf16")
 
@@ -238,9 +238,9 @@ def test_append(grkv_lib, dtype, layout, rotary, g, t, page, where):
             slot = c.lens[x] - count[x] + i
             at, row = C.at(c.table, x, slot, page), first[x] + i
             p = given[row] if where in ("pos", "packed") else slot + offset[x]
-            c.k[at], err[at] = R.rotate(k_new[row].double().numpy(), p, layout, **kw)
+            c.k[at], err[at] = R.rotate(k_new[row].double().numpy(), p, layout, dtype=dtype, **kw)
             c.v[at] = v_new[row].double().numpy()
-            want_q[x, :, i], err_q[x, :, i] = R.rotate(q[x, :, i].double().numpy(), np.full(g, p), layout, **kw)
+            want_q[x, :, i], err_q[x, :, i] = R.rotate(q[x, :, i].double().numpy(), np.full(g, p), layout, dtype=dtype, **kw)
     d.same(err)
     R.check(host(q_out), want_q, err_q, dtype)
 
@@ -292,7 +292,7 @@ def test_append_reports_rows_without_a_place(grkv_lib):
         d.lens = C.int_dev(lens)
         rng = np.random.default_rng(6)
         k_new, v_new, q = normal(rng, dtype, 12, D), normal(rng, dtype, 12, D), normal(rng, dtype, u, 2, t, D)
-        q_out = torch.full(q.shape, 7.0, device="cuda")
+        q_out = torch.full(q.shape, 7.0, dtype=torch.float32, device="cuda")
         b.grkv_cache_append_rope(
             d.p, plan(), k_new.cuda(), v_new.cuda(), d.k, d.v, d.table, d.lens, d.ws, q=q.cuda(), q_out=q_out,
             pos=None if pos is None else C.int_dev(pos), first_row=torch.tensor(first).cuda(),
@@ -364,7 +364,7 @@ def test_compact(grkv_lib, dtype, layout, rotary, page, place, given):
         for i in range(keep[x]):
             src, dst = C.at(c.table, x, idx[x, i], page), C.at(table_out, x, first[x] + i, page)
             by = turn[x, i] if given else first[x] + i - idx[x, i]
-            c.k[dst], err[dst] = R.rotate(before_k[src], by, layout, amplitude=1.0, **kw)
+            c.k[dst], err[dst] = R.rotate(before_k[src], by, layout, amplitude=1.0, dtype=dtype, **kw)
             if by == 0:
                 c.k[dst], err[dst], exact[dst] = before_k[src], 0.0, True
             c.v[dst] = before_v[src]
@@ -436,7 +436,7 @@ def test_numbers_of_units(grkv_lib, u):
     p = b.cache_params(u, g, pages, page, 1)
     k = torch.zeros(pages, page, D, dtype=torch.bfloat16, device="cuda")
     v, rope = torch.zeros_like(k), plan()
-    k_new = torch.randn(u, 1, D, device="cuda").bfloat16()
+    k_new = torch.randn(u, 1, D, dtype=torch.float32, device="cuda").bfloat16()
     table = torch.arange(u, dtype=torch.int32, device="cuda")
     lens = torch.full((u,), 9, dtype=torch.int32, device="cuda")
     ws = torch.full((b.grkv_cache_workspace_size(p),), 0xFF, dtype=torch.uint8, device="cuda")

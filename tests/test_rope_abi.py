@@ -187,7 +187,7 @@ def test_tensors_are_checked_by_the_binding(lib):  # noqa: F811
     with pytest.raises(ValueError, match="pos is torch.int64"):
         b.grkv_cache_append_rope(p, plan(), *[f] * 7, pos=i32.long(), **kw)
     with pytest.raises(ValueError, match="q_out is torch.float32"):
-        b.grkv_cache_append_rope(p, plan(), *[f] * 7, q=f, q_out=torch.zeros(8, 4, 1, 128), **kw)
+        b.grkv_cache_append_rope(p, plan(), *[f] * 7, q=f, q_out=torch.zeros(8, 4, 1, 128, dtype=torch.float32), **kw)
     with pytest.raises(ValueError, match="turn is torch.int64"):
         b.grkv_cache_compact_rope(p, plan(), *[f] * 7, turn=i32.long(), **kw)
     with pytest.raises(ValueError, match="slot is torch.int32"):
