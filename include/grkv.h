@@ -498,7 +498,7 @@ int grkv_cache_append_rope(const grkv_cache_params* p, const grkv_rope* rope, co
 
 /* grkv_cache_compact whose keys are turned on their way, each by turn[u][i] positions (int32 [U][t],
  * of any sign), or (turn NULL) by what its slot changes, first[u] + i - idx[u][i]: kept keys that were
- * rotated for their slots are so again.  a is not applied again.  A key turned by 0 moves bit for
+ * rotated for their slots are so again (in place U <= 2^26).  a is not applied again.  A key turned by 0 moves bit for
  * bit; every other turn rounds it once to its type. */
 int grkv_cache_compact_rope(const grkv_cache_params* p, const grkv_rope* rope, const int32_t* idx,
                             const int32_t* keep, const int32_t* first, const int32_t* turn,

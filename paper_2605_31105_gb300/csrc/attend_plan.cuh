@@ -413,6 +413,10 @@ __device__ __forceinline__ void store_row4(__nv_bfloat16* p, float4 x) {
   *(uint2*)p = v;
 }
 
+// Attention over encoder states for few rows and small caches (grkv_attend_cross.cu).
+bool cross_is_few(const CacheShape& s, int sms);
+cudaError_t launch_cross_few(const CacheShape& s, const AttendArgs& a, int sms, cudaStream_t st);
+
 cudaError_t launch_attend_tc(const CacheShape& s, const AttendArgs& a, bool cross, int G, cudaStream_t st);
 
 }  // namespace grkv

@@ -639,6 +639,7 @@ cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, con
   a.wide = attend_tiles(s) + (int64_t)s.U * a.QB * a.extra >= 1 << 30;
   const int sms = sm_count();
   if (sms <= 0 || sms > kMaxAttendSms) return cudaErrorInvalidDevice;
+  if (io.cross && cross_is_few(s, sms)) return launch_cross_few(s, a, sms, st);
   const int G = sms * ctas_per_sm(s, a.rows);
   const bool f32 = s.dtype == GRKV_F32;
   auto simt = [&](const auto& x) {

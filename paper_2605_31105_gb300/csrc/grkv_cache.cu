@@ -85,6 +85,11 @@ int cache_begin(const grkv_cache_params* p, const void* ws, size_t ws_bytes, Cac
 
 namespace {
 
+__global__ void k_clear_status(int* word) {
+  asm volatile("griddepcontrol.launch_dependents;");
+  *word = 0;
+}
+
 // ------------------------------------------------------------------- fork, trim
 // A thread per table entry.
 __global__ void __launch_bounds__(1024)
@@ -456,6 +461,11 @@ int attend(const grkv_cache_params* p, const AttendIo& io, bool tree, void* ws, 
 }
 
 }  // namespace
+
+cudaError_t grkv::launch_clear_status(int* word, cudaStream_t st) {
+  count_launches(1);
+  return launch_kernel(false, 1, k_clear_status, dim3(1), 1, 0, st, word);
+}
 
 extern "C" {
 

@@ -30,11 +30,12 @@ __device__ __forceinline__ int block_total(int x, int* sm) {
 }
 
 __global__ void __launch_bounds__(kMapThreads)
-    k_cache_map(const __grid_constant__ MapArgs a, int* word, bool solo) {
-  __shared__ int shared, sums[32], firsts[kMapThreads + 1], up[2][kMapThreads], depth[2][kMapThreads];
-  const Status st(word, &shared, solo);
+    k_cache_map(const __grid_constant__ MapArgs a, int* word, int solo) {
+  __shared__ CallStatus::Smem shared;
+  __shared__ int sums[32], firsts[kMapThreads + 1], up[2][kMapThreads], depth[2][kMapThreads];
+  const CallStatus st(word, &shared, solo);
   RowMove m = a.m;
-  m.status = st.at;
+  m.status = st.at();
   const int tid = threadIdx.x, U = m.tb.U, t = m.t;
   const int rows = U * t, n0 = blockIdx.x * a.per, n = n0 + tid;
   const bool mine = tid < a.per && n < rows;
@@ -144,10 +145,5 @@ extern "C" int grkv_cache_map(const grkv_cache_params* p, const int32_t* count, 
   const RowMove m{table_of(s), s.t, count, len, nullptr};
   const MapArgs a{m, table, parent, offset, first_row, pos, slot,
                   s.t <= kMapThreads ? kMapThreads / s.t * s.t : kMapThreads};
-  const int blocks = (rows + a.per - 1) / a.per;
-  const bool solo = blocks == 1;
-  if (!solo) GRKV_TRY(clear_status(w, L, st));
-  count_launches(1);
-  return cuda_rc(launch_kernel(false, 1, k_cache_map, dim3((unsigned)blocks), kMapThreads, 0, st, a,
-                               (int*)(w + L.status), solo));
+  return cuda_rc(launch_call(k_cache_map, (rows + a.per - 1) / a.per, kMapThreads, (size_t)rows * 12, (int*)(w + L.status), st, a));
 }

@@ -127,9 +127,9 @@ __global__ void __launch_bounds__(kRowThreads)
       if (h + j < h1) x[j] = load_pair<T, H>(in + (h + j) * a.is[1], at);
   };
   load();
-  Angles<T, H> an(r, at);
+  Angles<T, H> an;
   if (p < 0) return;
-  an.set(turn_by(p, r.amp, a.sign));
+  an.set(r.turns + at.pair, turn_by(p, r.amp, a.sign));
   while (true) {
 #pragma unroll
     for (int j = 0; j < kRowHeads; ++j)
@@ -170,7 +170,7 @@ struct AppendRopeArgs {
   int g;
 };
 
-constexpr int kAppendThreads = 128, kAppendHeads = 4;
+constexpr int kAppendThreads = 128, kAppendHeads = 2;
 
 // kThreads threads a token: its new key and value, and its queries.  Rows are asked for before the
 // table's entry that says where they go.
@@ -178,8 +178,8 @@ template <typename T, Hold H>
 __global__ void __launch_bounds__(kAppendThreads)
     k_append_rope(const __grid_constant__ RopeArgs r, const __grid_constant__ AppendRopeArgs a, int* word,
                   int solo) {
-  __shared__ ClusterStatus::Smem shared;
-  const ClusterStatus st(word, &shared, solo);
+  __shared__ CallStatus::Smem shared;
+  const CallStatus st(word, &shared, solo);
   constexpr int kThr = Pair<T, H>::kThreads;
   RowMove m = a.m;
   m.status = st.at();
@@ -214,8 +214,8 @@ __global__ void __launch_bounds__(kAppendThreads)
     else
       set_status(m.status, GRKV_ERR_INVALID_ARG);
     if (p >= 0) {
-      Angles<T, H> an(r, at);
-      an.set(turn_by(p, r.amp, 1.f));
+      Angles<T, H> an;
+      an.set(r.turns + at.pair, turn_by(p, r.amp, 1.f));
       if (to >= 0) {
         store_pair<T, H>((T*)a.k + to * kD, at, rotate<T, H>(k, at, an));
         store_pair<T, H>((T*)a.v + to * kD, at, v);
@@ -246,51 +246,66 @@ __device__ __forceinline__ int64_t turn_of(const CompactRopeArgs& a, int u, int 
   return a.turn ? a.turn[x] : (int64_t)(a.first ? a.first[u] : 0) + i - a.idx[x];
 }
 
-constexpr int kTurnThreads = 128, kTurnUnroll = 2;
+constexpr int kTurnThreads = 128, kTurnRows = 128, kTurnUnroll = 2;
 
-// To other pages: every row by itself, kThreads threads a row, two rows in flight to a thread.
+// To other pages.  A block takes up to kTurnRows rows of one unit: a thread a row looks up where it
+// comes from and goes to, then kThreads threads a row move them, two rows in flight to a thread.
+// (Places looked up by each row's threads, two rows a block's only work: 106 us for 524288 rows.)
 template <typename T, Hold H>
 __global__ void __launch_bounds__(kTurnThreads)
-    k_gather_rope(const __grid_constant__ RopeArgs r, const __grid_constant__ CompactRopeArgs a) {
-  constexpr int kThr = Pair<T, H>::kThreads, kRows = kTurnThreads / kThr;
-  const RowMove& m = a.m;
+    k_gather_rope(const __grid_constant__ RopeArgs r, const __grid_constant__ CompactRopeArgs a, int rows,
+                  int* word, int solo) {
+  constexpr int kThr = Pair<T, H>::kThreads, kStep = kTurnThreads / kThr;
+  __shared__ CallStatus::Smem shared;
+  __shared__ long long from[kTurnRows], to[kTurnRows];
+  __shared__ int by[kTurnRows];
+  const CallStatus st(word, &shared, solo);
+  RowMove m = a.m;
+  m.status = st.at();
+  const int per = (m.t + rows - 1) / rows, u = blockIdx.x / per, i0 = (blockIdx.x - u * per) * rows;
+  const int len = m.tb.clamped(m.len[u], m.status), n = min(rows, rows_of(m, u) - i0);
+  for (int x = threadIdx.x; x < n; x += kTurnThreads) {
+    if (!kept_row(m, a.idx, a.table_in, len, a.table_out, a.first, false, u, i0 + x, &from[x], &to[x])) to[x] = -1;
+    else by[x] = (int)turn_of(a, u, i0 + x);
+  }
   const Place<T, H> at(threadIdx.x % kThr, r.half);
-  Angles<T, H> an(r, at);
-  const int i0 = blockIdx.x * (kRows * kTurnUnroll) + threadIdx.x / kThr;
-  for (int u = blockIdx.y; u < m.tb.U; u += gridDim.y) {
-    const int len = m.tb.clamped(m.len[u], m.status), n = rows_of(m, u);
+  Angles<T, H> an;
+  uint64_t turns[Pair<T, H>::kVec];
+#pragma unroll
+  for (int x = 0; x < Pair<T, H>::kVec; ++x) turns[x] = r.turns[at.pair + x];
+  __syncthreads();
+  for (int x0 = threadIdx.x / kThr; x0 < n; x0 += kStep * kTurnUnroll) {
     Raw<T, H> k[kTurnUnroll], v[kTurnUnroll];
-    long long to[kTurnUnroll];
-    int64_t p[kTurnUnroll];
+    bool has[kTurnUnroll];
 #pragma unroll
     for (int j = 0; j < kTurnUnroll; ++j) {
-      const int i = i0 + j * kRows;
-      long long from;
-      if (i >= n || !kept_row(m, a.idx, a.table_in, len, a.table_out, a.first, false, u, i, &from, &to[j])) {
-        to[j] = -1;
-        continue;
-      }
-      p[j] = turn_of(a, u, i);
-      k[j] = load_pair<T, H>((const T*)a.k + from * kD, at);
-      v[j] = load_pair<T, H>((const T*)a.v + from * kD, at);
+      const int x = x0 + j * kStep;
+      has[j] = x < n && to[x] >= 0;
+      if (!has[j]) continue;
+      k[j] = load_once<T, H>((const T*)a.k + from[x] * kD, at);
+      v[j] = load_once<T, H>((const T*)a.v + from[x] * kD, at);
     }
 #pragma unroll
     for (int j = 0; j < kTurnUnroll; ++j) {
-      if (to[j] < 0) continue;
-      store_pair<T, H>((T*)a.v + to[j] * kD, at, v[j]);
-      if (p[j] != 0) {
-        an.set(turn_by(p[j], 1.f, 1.f));
+      const int x = x0 + j * kStep;
+      if (!has[j]) continue;
+      store_once<T, H>((T*)a.v + to[x] * kD, at, v[j]);
+      if (by[x] != 0) {
+        an.set(turns, turn_by(by[x], 1.f, 1.f));
         k[j] = rotate<T, H>(k[j], at, an);
       }
-      store_pair<T, H>((T*)a.k + to[j] * kD, at, k[j]);
+      store_once<T, H>((T*)a.k + to[x] * kD, at, k[j]);
     }
   }
+  st.end();
 }
 
 // In place: a row only moves down, so chunks of rows in ascending order, each read as a whole
-// before it is written, never overwrite a row that is still to be read.  A block owns the same
-// few pairs of every row of one unit's keys or values (grid (U, 2, parts)).
-constexpr int kShiftRopeThreads = 256, kShiftRopeUnroll = 4;
+// before it is written, never overwrite a row that is still to be read; a chunk's rows lie behind the
+// places of the one before, and are read while that is written.  A block owns the same few pairs
+// of every row of one unit's keys or values; with few units, whose SMs hold one block, of more rows at
+// a time.  Bound by a chunk's latency, 1.5 us.
+constexpr int kMaxShiftUnits = 1 << 26;   // 16 blocks a unit
 template <typename T, Hold H>
 struct ShiftPart {
   // threads of a row in a block: 64 bytes of it
@@ -298,49 +313,54 @@ struct ShiftPart {
   static constexpr int kParts = Pair<T, H>::kThreads / kThr;
 };
 template <typename T, Hold H>
-__global__ void __launch_bounds__(kShiftRopeThreads)
-    k_shift_rope(const __grid_constant__ RopeArgs r, const __grid_constant__ CompactRopeArgs a) {
-  constexpr int kThr = ShiftPart<T, H>::kThr, kRows = kShiftRopeThreads / kThr;
-  const RowMove& m = a.m;
-  const int u = blockIdx.x, r0 = threadIdx.x / kThr;
-  const bool keys = blockIdx.y == 0;
+__global__ void __launch_bounds__(1024)
+    k_shift_rope(const __grid_constant__ RopeArgs r, const __grid_constant__ CompactRopeArgs a, int* word,
+                 int solo) {
+  constexpr int kThr = ShiftPart<T, H>::kThr, kParts = ShiftPart<T, H>::kParts;
+  __shared__ CallStatus::Smem shared;
+  const CallStatus st(word, &shared, solo);
+  RowMove m = a.m;
+  m.status = st.at();
+  const int u = blockIdx.x / (2 * kParts), part = blockIdx.x % kParts, rows = blockDim.x / kThr;
+  const bool keys = blockIdx.x / kParts % 2 == 0;
   T* pool = (T*)(keys ? a.k : a.v);
-  const Place<T, H> at(blockIdx.z * kThr + threadIdx.x % kThr, r.half);
+  const Place<T, H> at(part * kThr + threadIdx.x % kThr, r.half);
   const int n = rows_of(m, u), len = m.tb.clamped(m.len[u], m.status);
-  Angles<T, H> an(r, at);
-  for (int base = 0; base < n; base += kRows * kShiftRopeUnroll) {
-    Raw<T, H> x[kShiftRopeUnroll];
-    long long to[kShiftRopeUnroll];
-    int64_t by[kShiftRopeUnroll];
-#pragma unroll
-    for (int j = 0; j < kShiftRopeUnroll; ++j) {
-      const int i = base + j * kRows + r0;
-      long long from;
-      to[j] = -1;
-      if (i < n && kept_row(m, a.idx, a.table_in, len, a.table_in, a.first, true, u, i, &from, &to[j])) {
-        const int64_t p = keys ? turn_of(a, u, i) : 0;
-        if (from == to[j] && p == 0) {
-          to[j] = -1;
-          continue;
-        }
-        x[j] = load_pair<T, H>(pool + from * kD, at);
-        by[j] = p;
-      } else {
-        to[j] = -1;
-      }
+  Angles<T, H> an;
+  struct Row {
+    Raw<T, H> x;
+    T* to;   // null: none
+    int by;
+  };
+  auto load = [&](int base, Row* row) {
+    const int i = base + threadIdx.x / kThr;
+    long long from, to;
+    row->to = nullptr;
+    if (i >= n || !kept_row(m, a.idx, a.table_in, len, a.table_in, a.first, true, u, i, &from, &to)) return;
+    row->by = keys ? (int)turn_of(a, u, i) : 0;
+    if (from == to && row->by == 0) return;
+    row->x = load_pair<T, H>(pool + from * kD, at);
+    row->to = pool + to * kD;
+  };
+  auto store = [&](Row* row) {
+    if (!row->to) return;
+    if (row->by != 0) {
+      an.set(r.turns + at.pair, turn_by(row->by, 1.f, 1.f));
+      row->x = rotate<T, H>(row->x, at, an);
     }
+    store_pair<T, H>(row->to, at, row->x);
+  };
+  Row even, odd;
+  load(0, &even);
+  for (int base = 0; base < n; base += 2 * rows) {
+    load(base + rows, &odd);
+    __syncthreads();   // the even chunk has been read, by all
+    store(&even);
+    load(base + 2 * rows, &even);
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kShiftRopeUnroll; ++j) {
-      if (to[j] < 0) continue;
-      if (by[j] != 0) {
-        an.set(turn_by(by[j], 1.f, 1.f));
-        x[j] = rotate<T, H>(x[j], at, an);
-      }
-      store_pair<T, H>(pool + to[j] * kD, at, x[j]);
-    }
-    __syncthreads();
+    store(&odd);
   }
+  st.end();
 }
 
 }  // namespace
@@ -436,14 +456,8 @@ int grkv_cache_append_rope(const grkv_cache_params* p, const grkv_rope* rope, co
     using T = decltype(zero);
     constexpr Hold H = decltype(hold)::value;
     const int per = kAppendThreads / Pair<T, H>::kThreads, blocks = (int)(((int64_t)s.U * s.t + per - 1) / per);
-    const int solo = blocks <= kMaxSolo ? blocks : 0;
-    if (!solo) {
-      const cudaError_t e = cudaMemsetAsync((char*)ws + L.status, 0, 4, st);
-      if (e != cudaSuccess) return e;
-    }
-    count_launches(1);
-    return launch_kernel(false, solo, k_append_rope<T, H>, dim3((unsigned)blocks), kAppendThreads, 0, st, r, a,
-                         (int*)((char*)ws + L.status), solo);
+    const size_t bytes = (size_t)s.U * s.t * (4 + (q ? 2 * s.g : 0)) * kD * sizeof(T);
+    return launch_call(k_append_rope<T, H>, blocks, kAppendThreads, bytes, (int*)((char*)ws + L.status), st, r, a);
   }));
 }
 
@@ -464,21 +478,24 @@ int grkv_cache_compact_rope(const grkv_cache_params* p, const grkv_rope* rope, c
   GRKV_TRY(check_optional(first, 4));
   GRKV_TRY(check_optional(turn, 4));
   cudaStream_t st = (cudaStream_t)stream;
-  GRKV_TRY(clear_status((char*)ws, L, st));
-  if (s.U == 0) return GRKV_OK;
-  const RowMove m{table_of(s), s.t, keep, len_in, (int*)((char*)ws + L.status)};
+  if (s.U == 0) return clear_status((char*)ws, L, st);
+  if (table_in == table_out && s.U > kMaxShiftUnits) return GRKV_ERR_UNSUPPORTED;
+  int* word = (int*)((char*)ws + L.status);
+  const RowMove m{table_of(s), s.t, keep, len_in, nullptr};
   const CompactRopeArgs a{m, idx, table_in, table_out, first, turn, k_pages, v_pages};
   return cuda_rc(dispatch(s.dtype, rope, [&](auto zero, auto hold) {
     using T = decltype(zero);
     constexpr Hold H = decltype(hold)::value;
-    count_launches(1);
-    if (table_in == table_out)
-      return launch_kernel(false, 1, k_shift_rope<T, H>, dim3(s.U, 2, ShiftPart<T, H>::kParts),
-                           kShiftRopeThreads, 0, st, r, a);
-    const int per = kTurnUnroll * kTurnThreads / Pair<T, H>::kThreads;
-    return launch_kernel(false, 1, k_gather_rope<T, H>,
-                         dim3((unsigned)((s.t + per - 1) / per), (unsigned)std::min(s.U, 65535)),
-                         kTurnThreads, 0, st, r, a);
+    const size_t bytes = (size_t)s.U * s.t * 4 * kD * sizeof(T);
+    if (table_in == table_out) {
+      const int64_t blocks = (int64_t)s.U * 2 * ShiftPart<T, H>::kParts;
+      return launch_call(k_shift_rope<T, H>, blocks, blocks <= sm_count() ? 1024 : 512, bytes, word, st, r, a);
+    }
+    // rows of a block: fewer where that gives more SMs work
+    int rows = kTurnRows;
+    auto blocks = [&]() { return (int64_t)s.U * ((s.t + rows - 1) / rows); };
+    while (rows > 16 && blocks() < 912) rows /= 2;
+    return launch_call(k_gather_rope<T, H>, blocks(), kTurnThreads, bytes, word, st, r, a, rows);
   }));
 }
 

@@ -96,14 +96,9 @@ __device__ __forceinline__ void cos_sin_bf16(uint32_t f, float* c, float* s) {
 template <typename T, Hold H>
 struct Angles {
   static constexpr int kVec = Pair<T, H>::kVec;
-  uint64_t turns[kVec];   // a position
   float c[kVec], s[kVec];
-
-  __device__ __forceinline__ Angles(const RopeArgs& r, const Place<T, H>& at) {
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) turns[i] = r.turns[at.pair + i];
-  }
-  __device__ __forceinline__ void set(const Turn& t) {
+  // turns: of the thread's pairs, from RopeArgs or a copy
+  __device__ __forceinline__ void set(const uint64_t* turns, const Turn& t) {
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
       // (the lower half rounds the upper one: 2^-33 turns)
@@ -136,6 +131,25 @@ __device__ __forceinline__ void store_pair(T* row, const Place<T, H>& at, const 
   } else {
     *(uint4*)(row + at.a) = r.a;
     *(uint4*)(row + at.b) = r.b;
+  }
+}
+
+// The same for rows that are read once and written for later (as a compact's are).
+template <typename T, Hold H>
+__device__ __forceinline__ Raw<T, H> load_once(const T* row, const Place<T, H>& at) {
+  if constexpr (H == Hold::Single) {
+    return load_pair<T, H>(row, at);
+  } else {
+    return Raw<T, H>{__ldcs((const uint4*)(row + at.a)), __ldcs((const uint4*)(row + at.b))};
+  }
+}
+template <typename T, Hold H>
+__device__ __forceinline__ void store_once(T* row, const Place<T, H>& at, const Raw<T, H>& r) {
+  if constexpr (H == Hold::Single) {
+    store_pair<T, H>(row, at, r);
+  } else {
+    __stcs((uint4*)(row + at.a), r.a);
+    __stcs((uint4*)(row + at.b), r.b);
   }
 }
 

@@ -98,6 +98,86 @@ def test_random_shapes(grkv_lib, dtype, flags, seed):
              q_lens=[int(x) for x in rng.integers(0, t + 1, u)], seed=100 * seed + k)
 
 
+# rows 1 to 9 (a cluster a unit for up to 8, then tiles), clusters of 1 to 8 CTAs, status written by a unit's
+# cluster (one unit), by a scan of all, and by units into a cleared word (600 units of 16 columns)
+@pytest.mark.parametrize("dtype,flags", TYPES)
+@pytest.mark.parametrize("g,t", [(1, 1), (2, 1), (1, 2), (3, 1), (4, 1), (2, 2), (5, 1), (4, 2), (1, 7), (8, 1), (9, 1)])
+@pytest.mark.parametrize("u,n", [(1, 1), (1, 255), (1, 900), (2, 1000), (40, 300), (130, 70), (600, 256)])
+def test_few_rows(grkv_lib, dtype, flags, g, t, u, n):
+    rng = np.random.default_rng(g * t + u)
+    lens = [int(x) for x in rng.integers(0, n + 1, u)]
+    lens[-1] = n
+    q_lens = [int(x) for x in rng.integers(0, t + 1, u)]
+    q_lens[-1] = t
+    case(lens, g, t, 16, dtype, flags, q_lens=q_lens, seed=u)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("u", [1, 7, 600])
+@pytest.mark.parametrize("fault", ["page", "below", "length", "negative", "rows"])
+def test_faults_of_few_rows(grkv_lib, dtype, u, fault):
+    """Reported, whichever unit has them; the units' other results stand."""
+    rng = np.random.default_rng(u)
+    lens = [int(x) for x in rng.integers(1, 200, u)]
+    at = u // 2
+    lens[at] = 208                               # the longest: whole pages, no more columns
+    c = R.Cache(lens, 16, dtype, 40, spare=3)
+    q, q64 = queries(u, 2, 1, dtype, 41)
+    p = b.cache_params(u, 2, c.pages, 16, c.cols, dtype=dtype)
+    table, given, q_lens, want = c.table.copy(), list(lens), [1] * u, [1] * u
+    if fault in ("page", "below"):               # read as page 0
+        table[at, 5] = c.pages if fault == "page" else -1
+        c.k[0], c.v[0] = np.nan_to_num(c.k[0], nan=0.5), np.nan_to_num(c.v[0], nan=0.5)
+        c.table[at, 5] = 0
+    if fault == "length":
+        given[at] = 209 + 1000
+    if fault == "negative":
+        given[at], c.lens[at] = -3, 0
+    if fault == "rows":
+        q_lens[at] = 2
+    out, lse, status = run(c, p, q, lens=given, q_lens=q_lens, table=table)
+    assert status == b.GRKV_ERR_INVALID_ARG
+    check(c, q64, out, lse, want)
+    out, lse, status = run(c, p, q, lens=[min(max(x, 0), 208) for x in given])   # and the next call is clean
+    assert status == b.GRKV_OK
+    check(c, q64, out, lse, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_calls_of_few_rows_are_equal_and_replay_beside_others(grkv_lib, dtype):
+    """Two captured calls of one workspace one after the other, and of two workspaces at once."""
+    c = R.Cache([1500, 3, 0, 777, 1024], 32, dtype, 42)
+    q, q64 = queries(5, 2, 1, dtype, 43)
+    p = b.cache_params(5, 2, c.pages, 32, c.cols, dtype=dtype)
+    o1, l1, _ = run(c, p, q)
+    kd, vd = c.dev()
+    dq, table, lens = q.cuda(), R.int_dev(c.table), R.int_dev(c.lens)
+    ws = [workspace(p), workspace(p)]
+    outs = [(torch.zeros_like(o1), torch.zeros_like(l1)) for _ in range(3)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs = []
+    for w, (o, l) in zip((ws[0], ws[0], ws[1]), outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            b.grkv_attend_cross(p, dq, kd, vd, table, lens, o, w, lse=l)
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for o, l in outs:
+            o.zero_()
+            l.zero_()
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        graphs[1].replay()
+        with torch.cuda.stream(other):
+            graphs[2].replay()
+        torch.cuda.synchronize()
+        for o, l in outs:
+            assert torch.equal(o, o1) and torch.equal(l, l1)
+        assert b.grkv_status(ws[0]) == b.grkv_status(ws[1]) == b.GRKV_OK
+
+
 @pytest.mark.parametrize("dtype,flags", TYPES)
 def test_a_window_is_not_read(grkv_lib, dtype, flags):
     case([900, 3], 2, 9, 16, dtype, flags, seed=5, window=20, n_sink=2)
