@@ -23,15 +23,15 @@ struct Few {
   static constexpr int kDims = 16 / (int)sizeof(T);   // of a lane
   static constexpr int kLanes = kD / kDims;           // of a slot
   static constexpr int kSide = 32 / kLanes;           // slots side by side
-  static constexpr int kLoad = R <= 4 ? 8 : 4;        // slots of a lane in a step
+  static constexpr int kLoad = R <= 4 ? 8 : 4;        // slots of a lane in a step; with R, up to kLanes logits
   static constexpr int kSlots = kSide * kLoad;        // of a step: 16 at most, in one page
-  static constexpr int kSum = kLoad * R <= kLanes ? kLoad : kLanes / R;   // whose logits are summed at once
-  static constexpr int kStep = kLanes / (kSum * R);   // lanes that end with the same logit
+  static constexpr int kStep = kLanes / (kLoad * R);  // lanes that end with the same logit
+  static_assert(kStep >= 1, "a logit to a lane");
   struct Smem {
     int err;
     float ml[kWarps][R][2];
     float4 o[kWarps][R][kD / 4];
-    float part_ml[R][2];        // of the CTA
+    float2 part_ml[R];          // of the CTA
     float4 part[R][kD / 4];
   };
 };
@@ -70,7 +70,7 @@ __device__ __forceinline__ float sum_lanes(float (&x)[N], int lane) {
   return x[0];
 }
 
-__device__ __forceinline__ float4 ld_cluster(const void* p, uint32_t rank) {
+__device__ __forceinline__ float4 ld_cluster(const float4* p, uint32_t rank) {
   float4 x;
   uint32_t at;
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
@@ -78,7 +78,7 @@ __device__ __forceinline__ float4 ld_cluster(const void* p, uint32_t rank) {
                : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at) : "memory");
   return x;
 }
-__device__ __forceinline__ float2 ld_cluster2(const void* p, uint32_t rank) {
+__device__ __forceinline__ float2 ld_cluster2(const float2* p, uint32_t rank) {
   float2 x;
   uint32_t at;
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
@@ -86,7 +86,7 @@ __device__ __forceinline__ float2 ld_cluster2(const void* p, uint32_t rank) {
   return x;
 }
 
-__device__ __forceinline__ int ld_cluster1(const void* p, uint32_t rank) {
+__device__ __forceinline__ int ld_cluster1(const int* p, uint32_t rank) {
   int x;
   uint32_t at;
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
@@ -138,12 +138,12 @@ template <typename T, int R>
 __global__ void __launch_bounds__(kThreads, R <= 4 ? 2 : 1)
     k_cross_few(const __grid_constant__ AttendArgs a, int C, bool scan) {
   using F = Few<T, R>;
-  constexpr int kDims = F::kDims, kLanes = F::kLanes, kSum = F::kSum;
+  constexpr int kDims = F::kDims, kLanes = F::kLanes, kLoad = F::kLoad;
   __shared__ typename F::Smem sm;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int cluster = blockIdx.x / C, rank = blockIdx.x - cluster * C, u = cluster - scan, rows = a.g * a.t;
   const int side = lane / kLanes, off = lane % kLanes * kDims;
-  const int mine = lane % kLanes / F::kStep, my_row = mine / kSum, my_slot = mine % kSum;
+  const int mine = lane % kLanes / F::kStep, my_row = mine / kLoad, my_slot = mine % kLoad;
   if (tid == 0) sm.err = 0;
   __syncthreads();
   if (u < 0) {
@@ -164,6 +164,14 @@ __global__ void __launch_bounds__(kThreads, R <= 4 ? 2 : 1)
   auto look_up = [&](int step) {
     return step < steps ? __ldg(a.table + (size_t)u * a.cols + (step * F::kSlots >> a.shift)) : 0;
   };
+  // this lane's part of a step's slots (zeros behind the unit's last)
+  auto load = [&](const void* pool, int step, int page, uint4 (&x)[kLoad]) {
+    const int x0 = step * F::kSlots, left = L - x0 - side;
+    const T* row = (const T*)pool + (((size_t)page << a.shift) + (x0 & ((1 << a.shift) - 1)) + side) * kD + off;
+#pragma unroll
+    for (int j = 0; j < kLoad; ++j)
+      x[j] = F::kSide * j < left ? *(const uint4*)(row + (size_t)F::kSide * j * kD) : make_uint4(0, 0, 0, 0);
+  };
   int entry = look_up(k);
   float q[R][kDims], o[R][kDims];
 #pragma unroll
@@ -181,60 +189,51 @@ __global__ void __launch_bounds__(kThreads, R <= 4 ? 2 : 1)
       page = 0;
     }
     entry = look_up(k + stride);
-    const int x0 = k * F::kSlots;
-    const size_t row = (((size_t)page << a.shift) + (x0 & ((1 << a.shift) - 1)) + side) * kD + off;
-    uint4 kk[F::kLoad], vv[F::kLoad];
-    const int n = L - x0 - side;   // slots of the lane's side that the unit has: those F::kSide j < n
+    // (the next step's K asked for here already: 12.2 us -> 13.1 for one row of 128 units)
+    uint4 kk[kLoad], vv[kLoad];
+    load(a.k, k, page, kk);
+    load(a.v, k, page, vv);
+    float x[R * kLoad];
 #pragma unroll
-    for (int j = 0; j < F::kLoad; ++j)
-      kk[j] = F::kSide * j < n ? *(const uint4*)((const T*)a.k + row + (size_t)F::kSide * j * kD) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-    for (int j = 0; j < F::kLoad; ++j)
-      vv[j] = F::kSide * j < n ? *(const uint4*)((const T*)a.v + row + (size_t)F::kSide * j * kD) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-    for (int j0 = 0; j0 < F::kLoad; j0 += kSum) {
-      float x[R * kSum];
-#pragma unroll
-      for (int s = 0; s < kSum; ++s) {
-        float y[kDims];
-        widen(kk[j0 + s], y);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          float sum = q[r][0] * y[0];
-#pragma unroll
-          for (int d = 1; d < kDims; ++d) sum = fmaf(q[r][d], y[d], sum);
-          x[r * kSum + s] = sum;
-        }
-      }
-      const float dot = sum_lanes<R * kSum, kLanes>(x, lane);
-      const bool see = F::kSide * (j0 + my_slot) < n;
-      const float logit = see ? dot * a.sl2 : -INFINITY;
-      float top = logit;
-#pragma unroll
-      for (int d = kSum / 2; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d * F::kStep));
-      if (F::kSide == 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, kLanes));
-      const float M = fmaxf(m, top), ref = M == -INFINITY ? 0.f : M;
-      const float keep = fast_exp2(m - ref), p = see ? fast_exp2(logit - ref) : 0.f;
-      m = M;
-      l = l * keep + p;
-      const bool scale = __any_sync(0xffffffffu, keep != 1.f);
+    for (int s = 0; s < kLoad; ++s) {
+      float y[kDims];
+      widen(kk[s], y);
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        if (!scale) break;
-        const float f = __shfl_sync(0xffffffffu, keep, r * kSum * F::kStep);
+        float sum = q[r][0] * y[0];
 #pragma unroll
-        for (int d = 0; d < kDims; ++d) o[r][d] *= f;
+        for (int d = 1; d < kDims; ++d) sum = fmaf(q[r][d], y[d], sum);
+        x[r * kLoad + s] = sum;
       }
+    }
+    const float dot = sum_lanes<R * kLoad, kLanes>(x, lane);
+    const bool see = F::kSide * my_slot < L - k * F::kSlots - side;
+    const float logit = see ? dot * a.sl2 : -INFINITY;
+    float top = logit;
 #pragma unroll
-      for (int s = 0; s < kSum; ++s) {
-        float y[kDims];
-        widen(vv[j0 + s], y);
+    for (int d = kLoad / 2; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d * F::kStep));
+    if (F::kSide == 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, kLanes));
+    const float M = fmaxf(m, top), ref = M == -INFINITY ? 0.f : M;
+    const float keep = fast_exp2(m - ref), p = see ? fast_exp2(logit - ref) : 0.f;
+    m = M;
+    l = l * keep + p;
+    const bool scale = __any_sync(0xffffffffu, keep != 1.f);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          const float w = __shfl_sync(0xffffffffu, p, side * kLanes + (r * kSum + s) * F::kStep);
+    for (int r = 0; r < R; ++r) {
+      if (!scale) break;
+      const float f = __shfl_sync(0xffffffffu, keep, r * kLoad * F::kStep);
 #pragma unroll
-          for (int d = 0; d < kDims; ++d) o[r][d] = fmaf(w, y[d], o[r][d]);
-        }
+      for (int d = 0; d < kDims; ++d) o[r][d] *= f;
+    }
+#pragma unroll
+    for (int s = 0; s < kLoad; ++s) {
+      float y[kDims];
+      widen(vv[s], y);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float w = __shfl_sync(0xffffffffu, p, side * kLanes + (r * kLoad + s) * F::kStep);
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) o[r][d] = fmaf(w, y[d], o[r][d]);
       }
     }
   }
@@ -242,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, R <= 4 ? 2 : 1)
 
   // the warp's rows: their sums over the lanes and sides, outputs over the sides
 #pragma unroll
-  for (int d = kSum / 2; d >= 1; d /= 2) l += __shfl_xor_sync(0xffffffffu, l, d * F::kStep);
+  for (int d = kLoad / 2; d >= 1; d /= 2) l += __shfl_xor_sync(0xffffffffu, l, d * F::kStep);
   if (F::kSide == 2) {
     l += __shfl_xor_sync(0xffffffffu, l, kLanes);
 #pragma unroll
@@ -287,8 +286,7 @@ __global__ void __launch_bounds__(kThreads, R <= 4 ? 2 : 1)
     if (r < R) {
       sm.part[r][lane] = y;
       if (lane == 0) {
-        sm.part_ml[r][0] = M;
-        sm.part_ml[r][1] = sum;
+        sm.part_ml[r] = make_float2(M, sum);
       }
     }
     cluster_ready();
@@ -299,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, R <= 4 ? 2 : 1)
 #pragma unroll
       for (int c = 1; c < 8; ++c) {
         if (c >= C) break;
-        ml[c] = ld_cluster2(sm.part_ml[r], c);
+        ml[c] = ld_cluster2(&sm.part_ml[r], c);
         x[c] = ld_cluster(&sm.part[r][lane], c);
       }
       float top = M;
@@ -338,40 +336,302 @@ __global__ void __launch_bounds__(kThreads, R <= 4 ? 2 : 1)
   }
 }
 
-template <typename T>
-cudaError_t launch_few(const AttendArgs& a, int C, bool scan, cudaStream_t st) {
-  const int rows = a.g * a.t;
-  auto go = [&](auto kern) {
-    count_launches(1);
-    return launch_kernel(false, C, kern, dim3((unsigned)(a.U + scan) * (unsigned)C), kThreads, 0, st, a, C, scan);
+// -------------------------------------------------- 3 to 16 rows of bf16: warp-level products
+// More rows than a lane's FMAs keep up with go through m16n8k16 products of each warp's own 16 slots, whose
+// operands are read from the cache straight into the fragments: a call waits for memory, and has nothing to
+// fill the 128-row tiles and the pipeline of the tcgen05 kernel with.  The 16 side of a product are slots (S^T =
+// K Q^T) and dimensions (O^T = V^T P^T), the 8 side rows, of which there are few: a product takes an SM's
+// quarter some 44 cycles, and with the sides the other way round eight rows took twice as many.
+// Fragments.  K: a lane's part of a slot are 16-byte chunks, so that the products' order of dimensions is not
+// theirs, but the queries' is the same.  V: a lane reads the same chunk of its four slots and pairs them up by
+// permutes; an output fragment's rows are a chunk's elements.  P goes from S^T's fragment to a right operand
+// by a transposition of 8 x 8.  Up to eight rows P is multiplied in two parts, its bf16 and what that
+// leaves, and all that is rounded is the output; with more, products bound the call, and P is rounded once.
+constexpr int kMmaThreads = 128, kMmaWarps = kMmaThreads / 32, kMmaRows = 16;
+template <int NT>   // row tiles of 8
+struct MmaSmem {
+  int err;
+  float2 ml[kMmaWarps][8 * NT], part_ml[8 * NT];
+  float4 o[kMmaWarps][8 * NT][kD / 4];   // the first warp's becomes the CTA's
+};
+
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                         uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t word(const uint4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
+
+// grid as k_cross_few's
+template <int NT>
+__global__ void __launch_bounds__(kMmaThreads, NT == 1 ? 4 : 3)
+    k_cross_mma(const __grid_constant__ AttendArgs a, int C, bool scan) {
+  __shared__ MmaSmem<NT> sm;
+  typedef __nv_bfloat16 T;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int cluster = blockIdx.x / C, rank = blockIdx.x - cluster * C, u = cluster - scan, rows = a.g * a.t;
+  const int i = lane >> 2, c = lane & 3;   // a fragment's row (a right operand's column) and place in it
+  if (tid == 0) sm.err = 0;
+  __syncthreads();
+  if (u < 0) {
+    const int fault = scan_faults(a, rank * kMmaThreads + tid, C * kMmaThreads);
+    if (fault) sm.err = fault;
+    __syncthreads();
+    const int all = cluster_min(&sm.err, C, rank);
+    if (rank == 0 && tid == 0) *a.status = all;
+    return;
+  }
+  const int L = unit_len(a, u), tokens = unit_tokens(a, u);
+  int err = 0;
+  if (L != __ldg(a.len + u) || (a.qlen && tokens != __ldg(a.qlen + u))) err = GRKV_ERR_INVALID_ARG;
+  const int steps = tokens > 0 ? (L + 15) / 16 : 0, stride = C * kMmaWarps;
+  int k = rank * kMmaWarps + warp;
+  auto look_up = [&](int step) {
+    return step < steps ? __ldg(a.table + (size_t)u * a.cols + (step * 16 >> a.shift)) : 0;
   };
-  return rows == 1 ? go(k_cross_few<T, 1>) : rows == 2 ? go(k_cross_few<T, 2>)
-         : rows <= 4 ? go(k_cross_few<T, 4>) : go(k_cross_few<T, 8>);
+  int entry = look_up(k);
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  uint4 q[NT][4];   // row 8 x + i, chunks of 8 dimensions 4 j + c
+#pragma unroll
+  for (int x = 0; x < NT; ++x)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = 8 * x + i;
+      q[x][j] = r < rows ? *(const uint4*)((const T*)a.q + ((size_t)u * rows + r) * kD + (4 * j + c) * 8) : zero;
+    }
+  // of rows 8 x + 2 c + e: the output, dimension 64 (j / 4) + 8 i + 2 (j % 4) + h in o[x][j][2 h + e]; the
+  // reference; the sum of this lane's slots
+  float o[NT][8][4], m[NT][2], l[NT][2];
+#pragma unroll
+  for (int x = 0; x < NT; ++x) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[x][j][e] = 0.f;
+    m[x][0] = m[x][1] = -INFINITY;
+    l[x][0] = l[x][1] = 0.f;
+  }
+  for (; k < steps; k += stride) {
+    int page = entry;
+    if ((unsigned)page >= (unsigned)a.P) {
+      err = GRKV_ERR_INVALID_ARG;
+      page = 0;
+    }
+    entry = look_up(k + stride);
+    const int x0 = k * 16, n = L - x0;   // slots of the step that the unit has
+    const size_t base = (((size_t)page << a.shift) + (x0 & ((1 << a.shift) - 1))) * kD;
+    uint4 kk[2][4], vv[4][2];   // K of slots i, i + 8, chunks 4 j + c; V of slots 2 c + {0, 1, 8, 9}, chunks i, i + 8
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        kk[t][j] = 8 * t + i < n ? *(const uint4*)((const T*)a.k + base + (8 * t + i) * kD + (4 * j + c) * 8) : zero;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int slot = 2 * c + (x & 1) + 8 * (x >> 1);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        vv[x][h] = slot < n ? *(const uint4*)((const T*)a.v + base + slot * kD + h * 64 + i * 8) : zero;
+    }
+    float s[NT][4];   // slots i (0, 1) and i + 8 (2, 3), rows 2 c + {0, 1}
+#pragma unroll
+    for (int x = 0; x < NT; ++x) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[x][e] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int w = 0; w < 4; w += 2)
+          mma16816(s[x], word(kk[0][j], w), word(kk[1][j], w), word(kk[0][j], w + 1), word(kk[1][j], w + 1),
+                   word(q[x][j], w), word(q[x][j], w + 1));
+    }
+    uint32_t hi[NT][2], lo[NT][2];   // P of slots 0-7 and 8-15: column i, slots 2 c + {0, 1}
+#pragma unroll
+    for (int x = 0; x < NT; ++x) {
+      float keep[2], p[4];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float x0 = i < n ? s[x][e] * a.sl2 : -INFINITY, x1 = i + 8 < n ? s[x][2 + e] * a.sl2 : -INFINITY;
+        float top = fmaxf(x0, x1);
+#pragma unroll
+        for (int d = 4; d <= 16; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const float M = fmaxf(m[x][e], top), ref = M == -INFINITY ? 0.f : M;
+        keep[e] = fast_exp2(m[x][e] - ref);
+        m[x][e] = M;
+        p[e] = i < n ? fast_exp2(x0 - ref) : 0.f;
+        p[2 + e] = i + 8 < n ? fast_exp2(x1 - ref) : 0.f;
+        l[x][e] = l[x][e] * keep[e] + (p[e] + p[2 + e]);
+      }
+      if (__any_sync(0xffffffffu, keep[0] != 1.f || keep[1] != 1.f)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[x][j][e] *= keep[e & 1];
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        hi[x][t] = pack_bf16(p[2 * t], p[2 * t + 1]);
+        if (NT == 1)
+          lo[x][t] = transposed8(pack_bf16(p[2 * t] - __uint_as_float(hi[x][t] << 16),
+                                           p[2 * t + 1] - __uint_as_float(hi[x][t] & 0xffff0000u)));
+        hi[x][t] = transposed8(hi[x][t]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int h = j >> 2, w = j & 3;   // elements 2 w, 2 w + 1 of chunks i + 8 h
+      const uint32_t v[4] = {word(vv[0][h], w), word(vv[1][h], w), word(vv[2][h], w), word(vv[3][h], w)};
+      const uint32_t a0 = __byte_perm(v[0], v[1], 0x5410), a1 = __byte_perm(v[0], v[1], 0x7632);
+      const uint32_t a2 = __byte_perm(v[2], v[3], 0x5410), a3 = __byte_perm(v[2], v[3], 0x7632);
+#pragma unroll
+      for (int x = 0; x < NT; ++x) {
+        mma16816(o[x][j], a0, a1, a2, a3, hi[x][0], hi[x][1]);
+        if (NT == 1) mma16816(o[x][j], a0, a1, a2, a3, lo[x][0], lo[x][1]);
+      }
+    }
+  }
+  if (err) sm.err = err;
+
+  // the warp's rows
+#pragma unroll
+  for (int x = 0; x < NT; ++x)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int d = 4; d <= 16; d *= 2) l[x][e] += __shfl_xor_sync(0xffffffffu, l[x][e], d);
+      const int r = 8 * x + 2 * c + e;
+      if (r >= rows) continue;
+      if (i == 0) sm.ml[warp][r] = make_float2(m[x][e], l[x][e]);
+#pragma unroll
+      for (int j = 0; j < 8; j += 2)
+        sm.o[warp][r][16 * (j >> 2) + 2 * i + (j >> 1 & 1)] =
+            make_float4(o[x][j][e], o[x][j][2 + e], o[x][j + 1][e], o[x][j + 1][2 + e]);
+    }
+  __syncthreads();
+  err = sm.err;
+  auto add = [](float4* y, float f, const float4& x) {
+    y->x = fmaf(f, x.x, y->x);
+    y->y = fmaf(f, x.y, y->y);
+    y->z = fmaf(f, x.z, y->z);
+    y->w = fmaf(f, x.w, y->w);
+  };
+  auto store = [&](int r, const float4& y, float M, float sum) {
+    if (r % a.t >= tokens) return;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const size_t dst = (size_t)u * rows + r;
+    store_row4((T*)a.out + dst * kD + lane * 4, make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv));
+    if (a.lse && lane == 0) a.lse[dst] = row_lse(M, sum);
+  };
+  // the CTA's, a warp a row
+  for (int r = warp; r < rows; r += kMmaWarps) {
+    float M = -INFINITY, sum = 0.f;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kMmaWarps; ++w) M = fmaxf(M, sm.ml[w][r].x);
+#pragma unroll
+    for (int w = 0; w < kMmaWarps; ++w) {
+      const float f = weight_of(sm.ml[w][r].x, M);
+      sum += f * sm.ml[w][r].y;
+      add(&y, f, sm.o[w][r][lane]);
+    }
+    if (C == 1) {
+      store(r, y, M, sum);
+      continue;
+    }
+    sm.o[0][r][lane] = y;
+    if (lane == 0) sm.part_ml[r] = make_float2(M, sum);
+  }
+  if (C > 1) {
+    cluster_ready();
+    float used = 0.f;
+    if (rank == 0 && tid < C) err = ld_cluster1(&sm.err, tid);
+    for (int r = warp; rank == 0 && r < rows; r += kMmaWarps) {
+      float2 ml[8];
+      float4 x[8];
+#pragma unroll
+      for (int z = 0; z < 8; ++z) {
+        if (z >= C) break;
+        ml[z] = ld_cluster2(&sm.part_ml[r], z);
+        x[z] = ld_cluster(&sm.o[0][r][lane], z);
+      }
+      float M = -INFINITY, sum = 0.f;
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int z = 0; z < 8; ++z)
+        if (z < C) M = fmaxf(M, ml[z].x);
+#pragma unroll
+      for (int z = 0; z < 8; ++z) {
+        if (z >= C) break;
+        const float f = weight_of(ml[z].x, M);
+        sum += f * ml[z].y;
+        add(&y, f, x[z]);
+      }
+      store(r, y, M, sum);
+      used += y.x + y.y + y.z + y.w + sum;
+    }
+    __syncwarp();
+    err = __reduce_min_sync(0xffffffffu, err);
+    cluster_done(used + __int_as_float(err));
+  }
+  if (rank == 0 && tid == 0) {
+    if (a.U == 1) *a.status = err;
+    else if (err && !scan) set_status(a.status, err);
+  }
+}
+
+cudaError_t launch_few(const AttendArgs& a, bool f32, int C, bool scan, cudaStream_t st) {
+  const int rows = a.g * a.t;
+  auto go = [&](auto kern, int threads) {
+    count_launches(1);
+    return launch_kernel(false, C, kern, dim3((unsigned)(a.U + scan) * (unsigned)C), threads, 0, st, a, C, scan);
+  };
+  if (f32)
+    return rows == 1   ? go(k_cross_few<float, 1>, kThreads)
+           : rows == 2 ? go(k_cross_few<float, 2>, kThreads)
+           : rows <= 4 ? go(k_cross_few<float, 4>, kThreads)
+                       : go(k_cross_few<float, 8>, kThreads);
+  if (rows <= 2)
+    return rows == 1 ? go(k_cross_few<__nv_bfloat16, 1>, kThreads) : go(k_cross_few<__nv_bfloat16, 2>, kThreads);
+  return rows <= 8 ? go(k_cross_mma<1>, kMmaThreads) : go(k_cross_mma<2>, kMmaThreads);
 }
 
 }  // namespace
 
-// CTAs of a unit: three to an SM in all, 128 slots each at least.
+// CTAs of a unit: three to an SM in all (four of those with four warps), 128 slots each at least.
 static int few_ctas(const CacheShape& s, int sms) {
+  const int most = (s.dtype == GRKV_BF16 && s.g * s.t > 2 ? 4 : 3) * sms;
   int C = 1;
-  while (C < 8 && (int64_t)s.U * C * 2 <= 3 * sms && (int64_t)s.cols << s.shift > 128 * C) C *= 2;
+  while (C < 8 && (int64_t)s.U * C * 2 <= most && (int64_t)s.cols << s.shift > 128 * C) C *= 2;
   return C;
 }
 
-// Whether a cluster a unit is faster than runs that are even over the SMs, by the slots that the units
-// can have (the host does not know their lengths).  One or two rows: a CTA's run may be longer than an SM's even
-// share by what planning and joining take.  bf16, 128 units of up to 1500 slots 12.0 us for 24.0, of 30000
-// 281 for 329 (194 for 186 where their lengths lie between 1900 and 30000), one of 8000 9.5 for 11.9, of 20000 18.5 for
-// 13.3; fp32 22.6 for 28.5, one of 8000 12.3 for 11.1.  More rows are bound by issue: four of bf16 over 64
-// units of 1500 14.8 for 17.4, over 128 27.1 for 25.0; eight over 32 units of 400 7.2 for 12.7, of 1500 19.9 for 16.7;
-// fp32 four over 128 units of 1500 27.8 for 28.9, eight over 64 28.9 for 31.5, over 128 47.9 for 42.2.
+// Whether a cluster a unit is faster than runs that are even over the SMs, by the slots that units can have (the
+// host does not know their lengths): a CTA's run of them may be longer than an SM's even share by what planning
+// and joining take, 10 us, less where rows make a slot dearer; many rows are bound by the products.  us, the other
+// kernels' behind the slash (`n`: units of n / 16 to n slots, `n-`: all of n):
+//   bf16, 1 row    128 x 1500 14.5/24.5, 1 x 8000 9.5/12.0, 1 x 20000 18.5/13.3, 128 x 16000 108/107, 128 x 30000- 281/329
+//         2 rows   128 x 1500 16.0/25.3, 64 x 6000 24.8/33.5, 128 x 16000 121/107
+//         4        128 x 1500 16.3/24.9, 8 x 8000 14.6/20.5, 1 x 8000 14.5/13.3, 128 x 16000- 163/183, 512 x 8000 240/202
+//         16       64 x 1500 20.3/21.7, 128 x 1500 26.4/26.3, 64 x 6000 39.7/34.5
+//   fp32, 1        128 x 1500 22.6/28.5, 1 x 8000 12.3/11.1, 64 x 6000 39.1/45.1
+//         4        64 x 1500 15.8/21.7, 128 x 1500 27.8/28.9, 1 x 8000 19.3/12.1
+//         8        64 x 1500 28.9/31.5, 128 x 1500 47.9/42.2
 bool cross_is_few(const CacheShape& s, int sms) {
-  const int rows = s.t <= 8 ? s.g * s.t : 9, C = few_ctas(s, sms);
+  const int rows = s.t <= 16 ? s.g * s.t : 17, C = few_ctas(s, sms);
   const int64_t cap = (int64_t)s.cols << s.shift, run = cap / C, share = s.U * cap / sms;
-  const bool f32 = s.dtype == GRKV_F32;
-  if (rows <= 2) return f32 ? run <= 800 + share / 2 : run <= 1700 + share;
-  if (rows <= 4) return run <= (f32 ? 800 : 400);
-  return rows <= 8 && (f32 ? run <= 400 : run <= 200 && s.U * C <= sms);
+  if (s.dtype == GRKV_F32)
+    return rows <= 2 ? run <= 800 + share / 2 : rows <= 4 ? run <= 800 : rows <= 8 && run <= 400;
+  return rows == 1   ? run <= 1700 + share
+         : rows == 2 ? run <= 1000 + share / 2
+         : rows <= 8 ? run <= 900 + share / 4
+                     : rows <= kMmaRows && run <= 1000 && share <= 1500;
 }
 
 cudaError_t launch_cross_few(const CacheShape& s, const AttendArgs& a, int sms, cudaStream_t st) {
@@ -382,7 +642,7 @@ cudaError_t launch_cross_few(const CacheShape& s, const AttendArgs& a, int sms, 
     const cudaError_t e = cudaMemsetAsync(a.status, 0, 4, st);
     if (e != cudaSuccess) return e;
   }
-  return s.dtype == GRKV_F32 ? launch_few<float>(a, C, scan, st) : launch_few<__nv_bfloat16>(a, C, scan, st);
+  return launch_few(a, s.dtype == GRKV_F32, C, scan, st);
 }
 
 }  // namespace grkv
