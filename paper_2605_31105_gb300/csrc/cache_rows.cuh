@@ -121,11 +121,12 @@ cudaError_t launch_clear_status(int* word, cudaStream_t st);
 // word and `solo`, for a call that moves `bytes`.  Long calls clear the word beside their kernel, 2 us less
 // on the GPU and 2 us more on the host, which they hide (appends of 50 MB 12.4 -> 10.3 us);
 // short ones, which wait for the host, by a memset (64 trees of 1024 units 9.3 us a call, else 10.2).
-constexpr size_t kLongCall = (size_t)32 << 20;
+constexpr size_t kLongCall = (size_t)16 << 20;
 template <typename... Params, typename... Args>
 cudaError_t launch_call(void (*kern)(Params...), int64_t blocks, int threads, size_t bytes, int* word,
                         cudaStream_t st, Args&&... args) {
-  const int solo = blocks <= kMaxSolo ? (int)blocks : 0;
+  int solo = blocks <= kMaxSolo ? (int)blocks : 0;
+  if (solo > 1 && !cluster_fits(solo, kern, threads, 0)) solo = 0;
   const bool beside = !solo && bytes >= kLongCall;
   if (!solo) {
     const cudaError_t e = beside ? launch_clear_status(word, st) : cudaMemsetAsync(word, 0, 4, st);

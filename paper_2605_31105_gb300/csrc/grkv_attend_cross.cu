@@ -586,9 +586,16 @@ __global__ void __launch_bounds__(kMmaThreads, NT == 1 ? 4 : 3)
   }
 }
 
-cudaError_t launch_few(const AttendArgs& a, bool f32, int C, bool scan, cudaStream_t st) {
+cudaError_t launch_few(const AttendArgs& a, bool f32, int C, cudaStream_t st) {
   const int rows = a.g * a.t;
   auto go = [&](auto kern, int threads) {
+    while (C > 1 && !cluster_fits(C, kern, threads, 0)) C /= 2;
+    // the scan of a call's tables takes less than the call: up to 32 entries a thread
+    const bool scan = a.U > 1 && (int64_t)a.U * a.cols <= (int64_t)32 * C * threads;
+    if (a.U > 1 && !scan) {
+      const cudaError_t e = cudaMemsetAsync(a.status, 0, 4, st);
+      if (e != cudaSuccess) return e;
+    }
     count_launches(1);
     return launch_kernel(false, C, kern, dim3((unsigned)(a.U + scan) * (unsigned)C), threads, 0, st, a, C, scan);
   };
@@ -635,14 +642,7 @@ bool cross_is_few(const CacheShape& s, int sms) {
 }
 
 cudaError_t launch_cross_few(const CacheShape& s, const AttendArgs& a, int sms, cudaStream_t st) {
-  const int C = few_ctas(s, sms);
-  // the scan of a call's tables takes less than the call: up to 32 entries a thread
-  const bool scan = s.U > 1 && (int64_t)s.U * s.cols <= (int64_t)32 * C * kThreads;
-  if (s.U > 1 && !scan) {
-    const cudaError_t e = cudaMemsetAsync(a.status, 0, 4, st);
-    if (e != cudaSuccess) return e;
-  }
-  return launch_few(a, s.dtype == GRKV_F32, C, scan, st);
+  return launch_few(a, s.dtype == GRKV_F32, few_ctas(s, sms), st);
 }
 
 }  // namespace grkv

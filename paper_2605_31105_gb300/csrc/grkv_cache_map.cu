@@ -10,7 +10,8 @@ using namespace grkv;
 namespace {
 
 constexpr int kMapThreads = 1024;
-constexpr int kMaxPackedUnits = 1 << 20;   // each block adds up the counts of all units before its own
+constexpr int kMaxPackedUnits = 1 << 20;
+constexpr int kOwnSums = 4096;   // units up to which each block adds up the counts of those before its own
 
 struct MapArgs {
   RowMove m;
@@ -19,6 +20,7 @@ struct MapArgs {
   int32_t* pos;
   int64_t* slot;
   int per;              // rows of a block
+  bool summed;          // first_row has been written
 };
 
 __device__ __forceinline__ int block_total(int x, int* sm) {
@@ -27,6 +29,38 @@ __device__ __forceinline__ int block_total(int x, int* sm) {
   if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = x;
   __syncthreads();
   return __reduce_add_sync(0xffffffffu, sm[threadIdx.x & 31]);
+}
+
+// Exclusive sum over the block's threads, and in *total the whole.
+__device__ __forceinline__ int block_scan(int x, int* sm, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int scan = x;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, scan, d);
+    if (lane >= d) scan += y;
+  }
+  __syncthreads();
+  if (lane == 31) sm[warp] = scan;
+  __syncthreads();
+  const int sum = sm[lane];
+  *total = __reduce_add_sync(0xffffffffu, sum);
+  return __reduce_add_sync(0xffffffffu, lane < warp ? sum : 0) + scan - x;
+}
+
+// First rows of many units, by one block (counts are checked by k_cache_map).
+__global__ void __launch_bounds__(kMapThreads) k_map_first(const int32_t* __restrict__ count, int U, int t,
+                                                           int64_t* first_row) {
+  __shared__ int sums[32];
+  int before = 0;
+  for (int u0 = 0; u0 < U; u0 += kMapThreads) {
+    const int u = u0 + threadIdx.x;
+    int all;
+    const int at = block_scan(u >= U ? 0 : count ? min(max(count[u], 0), t) : t, sums, &all);
+    if (u < U) first_row[u] = before + at;
+    before += all;
+  }
+  if (threadIdx.x == 0) first_row[U] = before;
 }
 
 __global__ void __launch_bounds__(kMapThreads)
@@ -42,7 +76,10 @@ __global__ void __launch_bounds__(kMapThreads)
   const int u = mine ? n / t : 0, i = mine ? n - u * t : 0, u0 = n0 / t;
   const int cnt = mine ? rows_of(m, u) : 0;
   int first = u * t, total = rows;
-  if (a.first_row) {
+  if (a.summed) {
+    first = mine ? (int)a.first_row[u] : 0;
+    total = (int)a.first_row[U];
+  } else if (a.first_row) {
     // rows in front of the block's first unit, of all units, and in front of each of the block's
     int before = 0, all = 0;
     for (int x = tid; x < U; x += kMapThreads) {
@@ -54,17 +91,8 @@ __global__ void __launch_bounds__(kMapThreads)
     total = block_total(all, sums);
     const int mu = u0 + tid;   // a thread a unit: the block has up to 1024
     const int c = mu < U && mu * (int64_t)t < n0 + a.per ? rows_of(m, mu) : 0;
-    int scan = c;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, scan, d);
-      if ((tid & 31) >= d) scan += y;
-    }
-    __syncthreads();
-    if ((tid & 31) == 31) sums[tid >> 5] = scan;
-    __syncthreads();
-    const int warps = __reduce_add_sync(0xffffffffu, (tid & 31) < (tid >> 5) ? sums[tid & 31] : 0);
-    firsts[tid] = before + warps + scan - c;
+    int block;
+    firsts[tid] = before + block_scan(c, sums, &block);
     __syncthreads();
     first = firsts[u - (mine ? u0 : 0)];
     if (mine && i == 0) a.first_row[u] = first;
@@ -143,7 +171,12 @@ extern "C" int grkv_cache_map(const grkv_cache_params* p, const int32_t* count, 
   }
   const int rows = s.U * s.t;
   const RowMove m{table_of(s), s.t, count, len, nullptr};
+  const bool summed = first_row && s.U > kOwnSums;
   const MapArgs a{m, table, parent, offset, first_row, pos, slot,
-                  s.t <= kMapThreads ? kMapThreads / s.t * s.t : kMapThreads};
+                  s.t <= kMapThreads ? kMapThreads / s.t * s.t : kMapThreads, summed};
+  if (summed) {
+    count_launches(1);
+    GRKV_TRY(cuda_rc(launch_kernel(false, 1, k_map_first, dim3(1), kMapThreads, 0, st, count, s.U, s.t, first_row)));
+  }
   return cuda_rc(launch_call(k_cache_map, (rows + a.per - 1) / a.per, kMapThreads, (size_t)rows * 12, (int*)(w + L.status), st, a));
 }

@@ -303,8 +303,9 @@ __global__ void __launch_bounds__(kTurnThreads)
 // In place: a row only moves down, so chunks of rows in ascending order, each read as a whole
 // before it is written, never overwrite a row that is still to be read; a chunk's rows lie behind the
 // places of the one before, and are read while that is written.  A block owns the same few pairs
-// of every row of one unit's keys or values; with few units, whose SMs hold one block, of more rows at
-// a time.  Bound by a chunk's latency, 1.5 us.
+// of every row of one unit's keys or values: 128 rows a chunk, or, where SMs hold one block at most, 512.  Bound by
+// a chunk's latency: 16384 of 32768 slots of 8 units 74 us (256 rows a chunk 94), 4096 of 8192 of 64 units 70,
+// 2048 of 32768 of 256 units 137.
 constexpr int kMaxShiftUnits = 1 << 26;   // 16 blocks a unit
 template <typename T, Hold H>
 struct ShiftPart {
@@ -489,7 +490,7 @@ int grkv_cache_compact_rope(const grkv_cache_params* p, const grkv_rope* rope, c
     const size_t bytes = (size_t)s.U * s.t * 4 * kD * sizeof(T);
     if (table_in == table_out) {
       const int64_t blocks = (int64_t)s.U * 2 * ShiftPart<T, H>::kParts;
-      return launch_call(k_shift_rope<T, H>, blocks, blocks <= sm_count() ? 1024 : 512, bytes, word, st, r, a);
+      return launch_call(k_shift_rope<T, H>, blocks, blocks <= sm_count() ? 1024 : 256, bytes, word, st, r, a);
     }
     // rows of a block: fewer where that gives more SMs work
     int rows = kTurnRows;

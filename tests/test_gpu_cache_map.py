@@ -66,7 +66,7 @@ def pool(u, page, t, n, seed, spare=5):
 
 # one block and several, units of one row, of a block's rows, of more, of odd numbers
 @pytest.mark.parametrize("u,t", [(1, 1), (1, 1023), (3, 1024), (2, 1025), (2, 3000), (7, 13), (300, 5), (1023, 1),
-                                 (1025, 1), (5000, 1), (2600, 3)])
+                                 (1025, 1), (4096, 1), (4097, 1), (5000, 1), (2600, 3), (9000, 7)])
 @pytest.mark.parametrize("packed", [False, True])
 @pytest.mark.parametrize("page", [16, 128])
 def test_map(grkv_lib, u, t, packed, page):
