@@ -100,13 +100,13 @@ struct RowsArgs {
   int64_t is[3], os[3];   // strides of sequence, head, token, in elements
   const int32_t *pos, *start;
   int S, H, t;
-  int heads;              // of a block's
   float sign;             // -1: transposed
 };
 
-constexpr int kRowThreads = 256, kRowHeads = 4;   // heads in flight to a thread
-
-// kThreads threads a token.  The first heads' rows are on their way while the angles are formed.
+// kThreads threads a token and four of its heads, whose rows are on their way while the angles are formed.  Memory:
+// 32 heads of 32768 tokens from token by token to head by head, 537 MB, 79.5 us, what a copy takes; with
+// all heads of a token to a thread, and its angles formed once, 83.2 (and 8 heads of 16 tokens 2.8 us for 2.2).
+constexpr int kRowThreads = 256, kRowHeads = 4;
 template <typename T, Hold H>
 __global__ void __launch_bounds__(kRowThreads)
     k_rope_rows(const __grid_constant__ RopeArgs r, const __grid_constant__ RowsArgs a) {
@@ -116,28 +116,19 @@ __global__ void __launch_bounds__(kRowThreads)
   const int s = (int)n / a.t, i = (int)n - s * a.t;   // S t <= 2^30
   const int64_t p = a.pos ? a.pos[n] : (int64_t)(a.start ? a.start[s] : 0) + i;
   const Place<T, H> at(threadIdx.x % kThr, r.half);
-  const T* in = (const T*)a.in + s * a.is[0] + i * a.is[2];
-  T* out = (T*)a.out + s * a.os[0] + i * a.os[2];
-  int h = blockIdx.y * a.heads;
-  const int h1 = min(a.H, h + a.heads);
+  const int h0 = blockIdx.y * kRowHeads, heads = min(a.H - h0, kRowHeads);
+  const T* in = (const T*)a.in + s * a.is[0] + h0 * a.is[1] + i * a.is[2];
+  T* out = (T*)a.out + s * a.os[0] + h0 * a.os[1] + i * a.os[2];
   Raw<T, H> x[kRowHeads];
-  auto load = [&]() {
 #pragma unroll
-    for (int j = 0; j < kRowHeads; ++j)
-      if (h + j < h1) x[j] = load_pair<T, H>(in + (h + j) * a.is[1], at);
-  };
-  load();
-  Angles<T, H> an;
+  for (int j = 0; j < kRowHeads; ++j)
+    if (j < heads) x[j] = load_pair<T, H>(in + j * a.is[1], at);
   if (p < 0) return;
+  Angles<T, H> an;
   an.set(r.turns + at.pair, turn_by(p, r.amp, a.sign));
-  while (true) {
 #pragma unroll
-    for (int j = 0; j < kRowHeads; ++j)
-      if (h + j < h1) store_pair<T, H>(out + (h + j) * a.os[1], at, rotate<T, H>(x[j], at, an));
-    h += kRowHeads;
-    if (h >= h1) break;
-    load();
-  }
+  for (int j = 0; j < kRowHeads; ++j)
+    if (j < heads) store_pair<T, H>(out + j * a.os[1], at, rotate<T, H>(x[j], at, an));
 }
 
 // Whether rows of the strides (elements) are whole vectors apart, and, for outputs, apart at all.
@@ -167,13 +158,13 @@ struct AppendRopeArgs {
   const int64_t* first;
   long long new_rows;
   const int32_t *table, *pos, *offset;
-  int g;
+  int g, parts;
 };
 
-constexpr int kAppendThreads = 128, kAppendHeads = 2;
-
-// kThreads threads a token: its new key and value, and its queries.  Rows are asked for before the
-// table's entry that says where they go.
+// kThreads threads a token's new key and value and up to kPartHeads of its queries' heads, two in flight; more
+// heads are parts of their own.  Rows are asked for before the table's entry that says where they go.  Memory:
+// 32768 tokens of 4 heads, 100 MB, about 16 us; four heads in flight 18, keys and queries in blocks of their own 16.
+constexpr int kAppendThreads = 128, kAppendHeads = 2, kPartHeads = 4;
 template <typename T, Hold H>
 __global__ void __launch_bounds__(kAppendThreads)
     k_append_rope(const __grid_constant__ RopeArgs r, const __grid_constant__ AppendRopeArgs a, int* word,
@@ -183,7 +174,8 @@ __global__ void __launch_bounds__(kAppendThreads)
   constexpr int kThr = Pair<T, H>::kThreads;
   RowMove m = a.m;
   m.status = st.at();
-  const int n = blockIdx.x * (kAppendThreads / kThr) + threadIdx.x / kThr;   // U t <= 2^28
+  const int block = blockIdx.x / a.parts, part = blockIdx.x - block * a.parts;
+  const int n = block * (kAppendThreads / kThr) + threadIdx.x / kThr;   // U t <= 2^28
   const int u = n / m.t, i = n - u * m.t;
   const int cnt = u < m.tb.U ? rows_of(m, u) : 0;
   if (i < cnt) {
@@ -191,15 +183,15 @@ __global__ void __launch_bounds__(kAppendThreads)
     // the length as it is: clamped to the table, rows behind it would go over those before
     const long long slot = (long long)m.len[u] - cnt + i;
     const long long f = a.first ? a.first[u] : (long long)u * m.t;
-    const bool has = f >= 0 && f <= a.new_rows - 1 - i;
+    const bool has = f >= 0 && f <= a.new_rows - 1 - i, keys = part == 0;
     Raw<T, H> k, v, x[kAppendHeads];
-    if (has) {
+    if (has && keys) {
       k = load_pair<T, H>((const T*)a.k_new + (f + i) * kD, at);
       v = load_pair<T, H>((const T*)a.v_new + (f + i) * kD, at);
     }
     const int64_t row = ((int64_t)u * a.g * m.t + i) * kD, step = (int64_t)m.t * kD;
-    const int g = a.q ? a.g : 0;
-    int h = 0;
+    const int g = a.q ? min(a.g, (part + 1) * kPartHeads) : 0;
+    int h = part * kPartHeads;
     auto load = [&]() {
 #pragma unroll
       for (int j = 0; j < kAppendHeads; ++j)
@@ -209,10 +201,12 @@ __global__ void __launch_bounds__(kAppendThreads)
     int64_t p = slot + (a.offset ? a.offset[u] : 0);
     if (a.pos) p = has ? a.pos[f + i] : -1;
     long long to = -1;
-    if (has && p >= 0 && slot >= 0 && slot < m.tb.cols << m.tb.shift)
-      to = pool_row(m.tb, a.table, u, (int)slot, m.status);
-    else
-      set_status(m.status, GRKV_ERR_INVALID_ARG);
+    if (keys) {
+      if (has && p >= 0 && slot >= 0 && slot < m.tb.cols << m.tb.shift)
+        to = pool_row(m.tb, a.table, u, (int)slot, m.status);
+      else
+        set_status(m.status, GRKV_ERR_INVALID_ARG);
+    }
     if (p >= 0) {
       Angles<T, H> an;
       an.set(r.turns + at.pair, turn_by(p, r.amp, 1.f));
@@ -416,11 +410,9 @@ int grkv_rope_rows(const grkv_rope* rope, const grkv_rows* s, const void* in, vo
     constexpr Hold H = decltype(hold)::value;
     const int per = kRowThreads / Pair<T, H>::kThreads;
     const int64_t blocks = ((int64_t)a.S * a.t + per - 1) / per;
-    // all heads of a token by one thread's angles, or four, where that leaves SMs without work
-    a.heads = blocks * ((a.H + kRowHeads - 1) / kRowHeads) <= 1216 ? kRowHeads : a.H;
     count_launches(1);
     return launch_kernel(false, 1, k_rope_rows<T, H>,
-                         dim3((unsigned)blocks, (unsigned)((a.H + a.heads - 1) / a.heads)), kRowThreads, 0,
+                         dim3((unsigned)blocks, (unsigned)((a.H + kRowHeads - 1) / kRowHeads)), kRowThreads, 0,
                          (cudaStream_t)stream, r, a);
   }));
 }
@@ -452,11 +444,13 @@ int grkv_cache_append_rope(const grkv_cache_params* p, const grkv_rope* rope, co
   if (s.U == 0) return clear_status((char*)ws, L, st);
   const RowMove m{table_of(s), s.t, count, len, nullptr};
   const AppendRopeArgs a{m, k_new, v_new, q, q_out, k_pages, v_pages, first_row,
-                         first_row ? (long long)new_rows : (long long)s.U * s.t, table, pos, offset, s.g};
+                         first_row ? (long long)new_rows : (long long)s.U * s.t, table, pos, offset, s.g,
+                         q ? (s.g + kPartHeads - 1) / kPartHeads : 1};
   return cuda_rc(dispatch(s.dtype, rope, [&](auto zero, auto hold) {
     using T = decltype(zero);
     constexpr Hold H = decltype(hold)::value;
-    const int per = kAppendThreads / Pair<T, H>::kThreads, blocks = (int)(((int64_t)s.U * s.t + per - 1) / per);
+    const int per = kAppendThreads / Pair<T, H>::kThreads;
+    const int64_t blocks = ((int64_t)s.U * s.t + per - 1) / per * a.parts;
     const size_t bytes = (size_t)s.U * s.t * (4 + (q ? 2 * s.g : 0)) * kD * sizeof(T);
     return launch_call(k_append_rope<T, H>, blocks, kAppendThreads, bytes, (int*)((char*)ws + L.status), st, r, a);
   }));
