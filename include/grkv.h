@@ -394,8 +394,8 @@ int grkv_attend_tree(const grkv_cache_params* p, const void* q, const void* k_pa
 /* Attention over the whole cache of a unit, whatever it holds: an encoder's states, a document that
  * several sequences read, a cache compressed with causal = 0.  Row i < q_len[u] (NULL: t) of unit u
  * sees every slot j < len[u]; queries are no slots of the cache, so that q_len and len have nothing
- * to do with each other.  window and n_sink are not read.  The rest, errors and roundings too, is
- * grkv_attend's: a unit of length 0 gives out = 0 and lse = -inf, rows from q_len[u] on are left as
+ * to do with each other.  window and n_sink are not read.  The rest, errors and roundings too (up to 8
+ * rows g t of bf16 may be rounded less), is grkv_attend's: a unit of length 0 gives out = 0 and lse = -inf, rows from q_len[u] on are left as
  * they were.  Beams of a sequence, whose caches are one, go into the group. */
 int grkv_attend_cross(const grkv_cache_params* p, const void* q, const void* k_pages,
                       const void* v_pages, const int32_t* table, const int32_t* len,

@@ -635,6 +635,7 @@ bool cross_is_few(const CacheShape& s, int sms) {
   const int64_t cap = (int64_t)s.cols << s.shift, run = cap / C, share = s.U * cap / sms;
   if (s.dtype == GRKV_F32)
     return rows <= 2 ? run <= 800 + share / 2 : rows <= 4 ? run <= 800 : rows <= 8 && run <= 400;
+  if (s.simt && rows > 2) return false;   // CUDA cores, and P in fp32
   return rows == 1   ? run <= 1700 + share
          : rows == 2 ? run <= 1000 + share / 2
          : rows <= 8 ? run <= 900 + share / 4

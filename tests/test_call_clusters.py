@@ -41,7 +41,7 @@ constexpr int kMaxSolo = 8;
 %(call)s
 constexpr int GRKV_F32 = 0, GRKV_BF16 = 1, kThreads = 256, kMmaThreads = 128, kMmaRows = 16;
 struct AttendArgs { int U, g, t, cols; int* status; };
-struct CacheShape { int U, g, t, cols, shift, dtype; };
+struct CacheShape { int U, g, t, cols, shift, dtype, simt; };
 struct __nv_bfloat16 {};
 template <class T, int R> void k_cross_few(const AttendArgs, int, bool) {}
 template <int NT> void k_cross_mma(const AttendArgs, int, bool) {}
@@ -73,9 +73,9 @@ extern "C" int call(long long blocks, long long bytes, int limit, int* out) {
   out[0] = cluster_used, out[1] = grid_used, out[2] = memsets, out[3] = clears, out[4] = beside_used, out[5] = launched;
   return rc;
 }
-extern "C" int cross(int U, int g, int t, int cols, int dtype, int limit, int* out) {
+extern "C" int cross(int U, int g, int t, int cols, int dtype, int limit, int simt, int* out) {
   reset(limit);
-  const CacheShape s{U, g, t, cols, 4, dtype};
+  const CacheShape s{U, g, t, cols, 4, dtype, simt};
   const AttendArgs a{U, g, t, cols, nullptr};
   out[6] = cross_is_few(s, 152);
   const int rc = out[6] ? launch_cross_few(s, a, 152, 0) : 0;
@@ -124,9 +124,9 @@ def test_status_of_a_call(lib):
     assert _call(lib, 9, 1 << 30) == dict(cluster=1, grid=9, memsets=0, clears=1, beside=1)
 
 
-def _cross(lib, u, g, t, cols, dtype=1, limit=8):
+def _cross(lib, u, g, t, cols, dtype=1, limit=8, simt=0):
     out = (ctypes.c_int * 7)()
-    assert lib.cross(u, g, t, cols, dtype, limit, out) == 0
+    assert lib.cross(u, g, t, cols, dtype, limit, simt, out) == 0
     if not out[6]:
         return None
     assert out[5] == 1
@@ -151,3 +151,5 @@ def test_calls_that_go_to_the_tiles(lib):
     assert _cross(lib, 8, 9, 1, 10, dtype=0) is None and _cross(lib, 128, 8, 1, 95, dtype=0) is None
     assert _cross(lib, 1 << 28, 1, 1, 1) == (1, 1 << 28, 1, 0)        # the largest number of units
     assert _cross(lib, 1, 64, 1 << 22, 1) is None
+    # the portable kernels' flag: CUDA cores only
+    assert _cross(lib, 8, 3, 1, 10, simt=1) is None and _cross(lib, 8, 2, 1, 10, simt=1) == (2, 18, 0, 0)
