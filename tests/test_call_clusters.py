@@ -103,7 +103,9 @@ def lib(tmp_path_factory):
     with open(src, "w") as f:
         f.write(code)
     cuda = os.path.dirname(os.path.dirname(build_mod.nvcc()))
-    subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", "-shared", "-w", "-I", os.path.join(cuda, "include"), "-o",
+    # (its own runtime calls, though another runtime may be loaded)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", "-shared", "-Wl,-Bsymbolic", "-w", "-I",
+                    os.path.join(cuda, "include"), "-o",
                     so, src], check=True)
     return ctypes.CDLL(so)
 

@@ -205,7 +205,7 @@ def test_one_token_sees_what_decoding_sees(grkv_lib, dtype, flags):
 
 
 @pytest.mark.parametrize("dtype,flags", TYPES)
-@pytest.mark.parametrize("g,t", [(1, 1), (4, 100)])
+@pytest.mark.parametrize("g,t", [(1, 1), (2, 1), (5, 1), (4, 3), (4, 100)])
 def test_what_lies_behind_the_length_stays_out(grkv_lib, dtype, flags, g, t):
     """Values of NaN and infinities behind the last slot of a page, pages that are not there."""
     c = R.Cache([301, 0, 640], 128, dtype, 11, extra_cols=2)
@@ -220,30 +220,47 @@ def test_what_lies_behind_the_length_stays_out(grkv_lib, dtype, flags, g, t):
 
 
 @pytest.mark.parametrize("dtype,flags", TYPES)
-def test_what_a_row_sees_reaches_it(grkv_lib, dtype, flags):
+@pytest.mark.parametrize("g,t", [(1, 1), (2, 1), (5, 1), (4, 3), (2, 70)])
+def test_what_a_row_sees_reaches_it(grkv_lib, dtype, flags, g, t):
     """A value that is not finite, in a whole tile and in the last one, reaches every row's element."""
     for slot in (3, 299):
         for what in (math.nan, math.inf):
             c = R.Cache([300], 16, dtype, 13)
             c.v[c.table[0, slot // 16], slot % 16, 9] = what
-            q, _ = queries(1, 2, 70, dtype, 14)
-            p = b.cache_params(1, 2, c.pages, 16, c.cols, tokens=70, dtype=dtype, flags=flags)
+            q, _ = queries(1, g, t, dtype, 14)
+            p = b.cache_params(1, g, c.pages, 16, c.cols, tokens=t, dtype=dtype, flags=flags)
             out, _, _ = run(c, p, q)
             assert not torch.isfinite(out[..., 9]).any()
             assert torch.isfinite(out[..., :9]).all() and torch.isfinite(out[..., 10:]).all()
+            c.v[c.table[0, slot // 16], slot % 16, 9] = 0.0
+            c.k[c.table[0, slot // 16], slot % 16, 5] = math.nan     # a key of NaN: every element
+            out, _, _ = run(c, p, q)
+            assert torch.isnan(out).all()
 
 
 @pytest.mark.parametrize("dtype,flags", TYPES)
-def test_large_logits(grkv_lib, dtype, flags):
+@pytest.mark.parametrize("g,t", [(4, 90), (1, 1), (2, 1), (7, 1), (4, 4)])
+def test_large_logits(grkv_lib, dtype, flags, g, t):
+    """Keys that grow along the cache; then logits of up to 2^40, which leave every row its largest one's value."""
     c = R.Cache([1500], 64, dtype, 22)
     grow = np.linspace(0.1, 40, 1500)
     for j in range(1500):
         r = c.table[0, j // 64], j % 64
         c.k[r] = c.rounded(c.k[r] * grow[j])
-    q, q64 = queries(1, 4, 90, dtype, 23)
-    p = b.cache_params(1, 4, c.pages, 64, c.cols, tokens=90, dtype=dtype, flags=flags)
+    q, q64 = queries(1, g, t, dtype, 23)
+    p = b.cache_params(1, g, c.pages, 64, c.cols, tokens=t, dtype=dtype, flags=flags)
     out, lse, _ = run(c, p, q)
-    check(c, q64, out, lse, [90])
+    check(c, q64, out, lse, [t])
+    p.scale = 2.0 ** 28
+    out, lse, _ = run(c, p, q)
+    k, v = c.slots(0)
+    x = q64[0] @ k.T                                          # the two largest are far apart in most rows
+    top = np.sort(x, -1)
+    clear = top[..., -1] - top[..., -2] > 1e-3 * np.abs(x).max()
+    best = v[x.argmax(-1)]
+    got = out[0].double().cpu().numpy()
+    assert clear.mean() > 0.5 and torch.isfinite(out).all() and torch.isfinite(lse).all()
+    assert np.abs(got - best)[clear].max() <= R.ROUND[dtype] * np.abs(best).max()
 
 
 @pytest.mark.parametrize("dtype,flags", TYPES)
