@@ -67,8 +67,9 @@ struct Status {
     if (threadIdx.x == 0) *word = *at;
   }
 };
+
 // The status of a call of one kernel.  `solo` blocks, up to kMaxSolo, are one cluster, of which the
-// first writes the word whole, without a memset in front (a decoding step's append 6.3 -> 3.9 us).  More
+// first writes the word whole, without a memset in front (a decoding step's append 3.8 us for 6.2).  More
 // blocks (solo 0) add their faults to a word that a memset has cleared, or that k_clear_status clears
 // while they run (launch_call).  Every thread of the block runs to end().
 constexpr int kMaxSolo = 8;
@@ -119,8 +120,8 @@ cudaError_t launch_clear_status(int* word, cudaStream_t st);
 
 // Launches a kernel of `blocks` blocks (a grid of one dimension) whose last parameters are the status
 // word and `solo`, for a call that moves `bytes`.  Long calls clear the word beside their kernel, 2 us less
-// on the GPU and 2 us more on the host, which they hide (appends of 50 MB 12.4 -> 10.3 us);
-// short ones, which wait for the host, by a memset (64 trees of 1024 units 9.3 us a call, else 10.2).
+// on the GPU (an append of 50 MB 8.6 us for 10.6) and 0.5 to 1 us more on the host, which they hide;
+// short ones, which wait for the host, by a memset (trees of 1024 units 9.0 us a call of the host for 9.9).
 constexpr size_t kLongCall = (size_t)16 << 20;
 template <typename... Params, typename... Args>
 cudaError_t launch_call(void (*kern)(Params...), int64_t blocks, int threads, size_t bytes, int* word,
