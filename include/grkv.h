@@ -411,7 +411,8 @@ int grkv_attend_cross(const grkv_cache_params* p, const void* q, const void* k_p
  * pos int32 and slot int64 [U][t]; entries of rows that a unit does not have are -1.  With first_row
  * (int64 [U + 1], written; U <= 2^20) rows are packed: unit u's entries start at first_row[u], the sum of
  * the counts before it, first_row[U] is the sum of all, and the entries (of U t) behind it are -1.
- * That is what grkv_cache_append and grkv_cache_append_rope take as first_row and pos. */
+ * That is what grkv_cache_append and grkv_cache_append_rope take as first_row and pos; slot is for a
+ * caller's own kernel that writes its rows to the pages itself. */
 int grkv_cache_map(const grkv_cache_params* p, const int32_t* count, const int32_t* parent,
                    const int32_t* offset, const int32_t* table, const int32_t* len,
                    int64_t* first_row, int32_t* pos, int64_t* slot, void* ws, size_t ws_bytes,
