@@ -640,6 +640,11 @@ cudaError_t launch_attend(const CacheShape& s, const AttendIo& io, char* ws, con
   const int sms = sm_count();
   if (sms <= 0 || sms > kMaxAttendSms) return cudaErrorInvalidDevice;
   if (io.cross && cross_is_few(s, sms)) return launch_cross_few(s, a, sms, st);
+  if (io.cross && cross_is_split(s)) {
+    split_rows(s, &a);
+    const cudaError_t e = launch_cross_split(a, sms, st);
+    return e != cudaSuccess ? e : launch_join<float>(a, sms, st);
+  }
   const int G = sms * ctas_per_sm(s, a.rows);
   const bool f32 = s.dtype == GRKV_F32;
   auto simt = [&](const auto& x) {
