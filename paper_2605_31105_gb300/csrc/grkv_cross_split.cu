@@ -9,10 +9,10 @@
 // kept in registers, where additions round to nearest (in the tensor cores' accumulator a long row's would
 // not), with its reference, which moves only when a tile's maximum passes it by 2^8.
 //
-// Roles.  Warps 0-3: softmax, a row (a TMEM lane) to a thread, and its output, 128 registers.  Warps 4-7: queries, K
-// and V, read from the pages, split, and stored to shared memory as the products want them.  Warp 8 issues the
-// products.  Numbers are split at half their size, so that none rounds up to infinity.  Of the block's 384 x 168
-// registers at launch the warpgroups take 128 x (240 + 192 + 72).
+// Roles.  Warps 0-3: softmax, a row (a TMEM lane) to a thread, and its output, 128 registers.  Warps 4-11: queries,
+// K and V, read from the pages, split, and stored to shared memory as the products want them.  Warp 12 issues the
+// products.  Numbers are split at half their size, so that none rounds up to infinity.  Of the block's 512 x 128
+// registers at launch the warpgroups take 128 x (240 + 104 + 104 + 64).
 #include <stddef.h>
 
 #include <algorithm>
@@ -25,7 +25,7 @@ namespace {
 using namespace sm100;
 
 constexpr int kSub = 64;                       // slots of a tile
-constexpr int kThreads = 384;
+constexpr int kThreads = 512, kLoaders = 256;   // kLoaders: of queries, K and V
 constexpr uint32_t kQPart = 128 * kD * 2;      // 32 KB: two halves of 64 dimensions
 constexpr uint32_t kKvPart = kSub * kD * 2;    // 16 KB
 constexpr uint32_t kOffQ = 0, kOffK = 3 * kQPart, kOffV = kOffK + 3 * kKvPart, kOffBar = kOffV + 3 * kKvPart,
@@ -36,9 +36,10 @@ constexpr long long kWaitBudget = 1ll << 32;   // cycles (~2 s)
 constexpr long long kTestWaitBudget = 1ll << 22;   // ~2 ms: GRKV_TEST_TIMEOUT's
 constexpr float kSlack = 8.f;                  // by which logits may pass their reference (log2)
 
-// Arrivals that complete a phase: 4 warps where warps write, 1 where products do.
+// Arrivals that complete a phase: 8 loading warps, 4 of the softmax, or 1 where products do.
 struct Bars {
-  uint64_t k_full, v_full, o_empty, p_full[2];                  // 4
+  uint64_t k_full, v_full;                                      // 8
+  uint64_t o_empty, p_full[2];                                  // 4
   uint64_t k_empty, v_empty, o_full, s_full[2], drain;          // 1
   uint32_t tmem;
   int abort;
@@ -102,9 +103,10 @@ __device__ __forceinline__ void store_split(uint8_t* tile, uint32_t part, uint32
   for (int i = 0; i < 3; ++i) *(uint4*)(at + i * part) = make_uint4(w[0][i], w[1][i], w[2][i], w[3][i]);
 }
 
-// A lane's part of a K or V tile: chunk c of rows r0 + 8 j.
+// A lane's part of a K or V tile: chunk c of rows r0 + 16 j.
+constexpr int kRowStep = kLoaders / 16, kChunks = kSub / kRowStep;
 struct Chunks {
-  float4 x[8], y[8];
+  float4 x[kChunks], y[kChunks];
 };
 // The pages of a tile's slots, one to a lane (four of 16 slots, or fewer).
 __device__ __forceinline__ int pages_of(const CrossArgs& a, const Cursor& cur, int lane, int* err) {
@@ -114,8 +116,8 @@ __device__ __forceinline__ int pages_of(const CrossArgs& a, const Cursor& cur, i
 __device__ __forceinline__ void load_chunks(const CrossArgs& a, const void* pool, int pages, int x0, int L, int r0, int c,
                                             Chunks* z) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int r = r0 + 8 * j, slot = x0 + r;
+  for (int j = 0; j < kChunks; ++j) {
+    const int r = r0 + kRowStep * j, slot = x0 + r;
     const int page = __shfl_sync(0xffffffffu, pages, (slot >> a.shift) - (x0 >> a.shift));
     const float4* p =
         (const float4*)pool + (((size_t)page << a.shift) + (slot & ((1 << a.shift) - 1))) * (kD / 4) + 2 * c;
@@ -128,7 +130,7 @@ __device__ __forceinline__ void load_chunks(const CrossArgs& a, const void* pool
 }
 __device__ __forceinline__ void store_chunks(uint8_t* tile, int r0, int c, const Chunks& z) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) store_split(tile, kKvPart, kKvPart / 2, r0 + 8 * j, c, z.x[j], z.y[j]);
+  for (int j = 0; j < kChunks; ++j) store_split(tile, kKvPart, kKvPart / 2, r0 + kRowStep * j, c, z.x[j], z.y[j]);
 }
 
 // The K = 16 steps of a product of parts, by one elected lane of a converged warp, whose descriptors advance inside.
@@ -186,11 +188,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   if (warp == 0) {
-    if (lane < kBars) mbar_init((uint64_t*)bars + lane, lane < 5 ? 4 : 1);
+    if (lane < kBars) mbar_init((uint64_t*)bars + lane, lane < 2 ? 8 : lane < 5 ? 4 : 1);
     if (lane == 0) bars->abort = 0;
     fence_mbar_init();
   }
-  if (warp == 8) {
+  if (warp == 12) {
     tmem_alloc(&bars->tmem, 512);
     tmem_relinquish();
   }
@@ -204,10 +206,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
   auto wait = [&](uint64_t* bar, uint32_t parity) { return wait_warp(bar, parity & 1, abort_flag, budget); };
   int err = 0;
 
-  if (warp >= 8) {
+  if (warp >= 12) {
     // ------------------------------------------------------------- the products
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (warp == 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == 12) {
     constexpr uint32_t id_s = idesc_bf16(128, kSub, 0, 0);   // both K-major
     constexpr uint32_t id_o = idesc_bf16(128, kD, 0, 1);     // V MN-major
     const uint64_t q_desc = sw128_desc(smem_u32(sm + kOffQ), 16, 1024);
@@ -247,7 +249,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
     }
   } else if (warp >= 4) {
     // -------------------------------------------- queries, K (a tile ahead) and V
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     const int t = tid - 128, c = t & 15, r0 = t >> 4;
     // K of tile n + 1 is stored once S of tile n has been formed, then V of tile n once O of the one before has;
     // both were asked for a tile earlier, their pages before that.
@@ -255,9 +257,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
     int v_pages = 0, v_slot = 0, v_len = 0;   // of the tile that kc is ahead of
     auto fill_q = [&]() {
       const Item& it = kc.sg.it;
-#pragma unroll 8
-      for (int j = 0; j < 16; ++j) {
-        const int r = r0 + 8 * j;
+#pragma unroll 2
+      for (int j = 0; j < 128 / kRowStep; ++j) {
+        const int r = r0 + kRowStep * j;
         int h, i;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
         if (row_of(a, it, 0, r, &h, &i)) {
@@ -344,8 +346,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
       if (!ok) break;
       tc_fence_after();
       float top = -INFINITY;
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
+#pragma unroll 1
+      for (int c = 0; c < 2; ++c) {   // (not unrolled: the roles' code shares what an SM holds of it)
         float v[32];
         tmem_ld32f(s_addr + 32 * c, v);
         tmem_wait32(v);
@@ -362,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
       }
       const float ref = m == -INFINITY ? 0.f : m;
       float sum = 0.f;
-#pragma unroll
+#pragma unroll 1
       for (int c = 0; c < 2; ++c) {
         float v[32];
         tmem_ld32f(s_addr + 32 * c, v);
@@ -389,30 +391,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
       tmem_st_wait();
       tc_fence_before();
       arrive_warp(&bars->p_full[n & 1], lane);
-      if (!cur.first()) {
-        ok = add_output(n - 1);
-        if (!ok) break;
-        if (__any_sync(0xffffffffu, f != 1.f)) {
+      // the outputs of the tile before, in the old reference, and, at a segment's end, of this one
+      const bool last = cur.last();
+      for (int x = cur.first() ? n : n - 1; ok && x <= (last ? n : n - 1); ++x) {
+        ok = add_output(x);
+        if (x < n && __any_sync(0xffffffffu, f != 1.f)) {
 #pragma unroll
-          for (int x = 0; x < kD; ++x) acc[x] *= f;
+          for (int y = 0; y < kD; ++y) acc[y] *= f;
         }
       }
-      if (cur.last()) {
-        ok = add_output(n);
-        if (!ok) break;
+      if (!ok) break;
+      if (last) {
         const Item& it = cur.sg.it;
         int h, i;
         if (row_of(a, it, 0, row, &h, &i)) {
           const bool whole = cur.sg.whole();
           const float to = !whole ? 2.f : l == 0.f ? 0.f : 2.f / l;   // the values were halved
-          const size_t dst = ((size_t)it.u * a.g + h) * a.t + i;
+          const size_t dst = ((size_t)it.u * a.g + h) * a.t + i, step = whole ? 1 : a.rows;
           const int slot = cur.sg.slot(blockIdx.x);
+          float4* p = whole ? (float4*)a.out + dst * (kD / 4) : part4(a, slot, 0, row);
 #pragma unroll
-          for (int x = 0; x < kD; x += 4) {
-            const float4 y = make_float4(acc[x] * to, acc[x + 1] * to, acc[x + 2] * to, acc[x + 3] * to);
-            if (whole) store_row4((float*)a.out + dst * kD + x, y);
-            else *part4(a, slot, x / 4, row) = y;
-          }
+          for (int x = 0; x < kD / 4; ++x)
+            p[x * step] = make_float4(acc[4 * x] * to, acc[4 * x + 1] * to, acc[4 * x + 2] * to, acc[4 * x + 3] * to);
           if (!whole) a.pml[(size_t)slot * a.rows + row] = make_float2(m, l);
           else if (a.lse) a.lse[dst] = row_lse(m, l);
         }
@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 8) tmem_dealloc(tmem, 512);
+  if (warp == 12) tmem_dealloc(tmem, 512);
   if (tid == 0) {
     AttendRec rec = plan->rec;
     rec.err = bars->abort ? GRKV_ERR_TIMEOUT : plan->err;
