@@ -417,7 +417,7 @@ __device__ __forceinline__ void store_row4(__nv_bfloat16* p, float4 x) {
 bool cross_is_few(const CacheShape& s, int sms);
 cudaError_t launch_cross_few(const CacheShape& s, const AttendArgs& a, int sms, cudaStream_t st);
 
-// ... in fp32 for many rows, on the tensor cores (grkv_cross_split.cu).
+// ... in fp32 for more rows, on the tensor cores (grkv_cross_split.cu).
 bool cross_is_split(const CacheShape& s);
 void split_rows(const CacheShape& s, AttendArgs* a);
 cudaError_t launch_cross_split(const AttendArgs& a, int G, cudaStream_t st);

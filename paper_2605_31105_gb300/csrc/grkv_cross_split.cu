@@ -1,18 +1,22 @@
-// Attention over encoder states in fp32 for many rows, on the 5th-generation tensor cores: every fp32 number is
-// three bf16 parts, x = x1 + x2 + x3 (each the nearest to what the ones before leave: 2^-27 of x is lost),
-// and a product of two is the six products of parts whose orders add up to four at most (the others are 2^-27
-// of it), summed in fp32 from the smallest on.
+// Attention over encoder states in fp32 for 9 rows a unit and more, on the 5th-generation tensor cores: every fp32
+// number is three bf16 parts, x = x1 + x2 + x3 (each the nearest to what the ones before leave: 2^-27 of x is
+// lost), and a product of two is the six products of parts whose orders add up to four at most (the others are
+// 2^-27 of it), summed in fp32 from the smallest on.  Numbers are halved before they are split, so that none
+// rounds up to infinity; parts below 2^-126 are lost, so numbers below 2^-100 are less exact.
 //
-// A row tile is up to 128 rows, a slot tile 64 slots: S = Q K^T in 48 products of K = 16 and 64 columns,
-// O = P V in 24 of 128 columns, 1.5 K cycles each.  S goes ahead of O by a tile, so that the tensor cores
-// work on one while the softmax does the other's (two S and two P buffers).  O is a tile's alone: the sum over tiles is
-// kept in registers, where additions round to nearest (in the tensor cores' accumulator a long row's would
-// not), with its reference, which moves only when a tile's maximum passes it by 2^8.
+// A row tile is up to 128 rows, a slot tile 64 slots: S = Q K^T in 48 products of K = 16 and 64 columns, 65 cycles
+// each, O = P V in 24 of 128 columns, 57 each.  S goes ahead of O by a tile, so that the tensor cores work on one
+// while the softmax does the other's (two S and two P buffers).  O is a tile's alone: the sum over tiles is kept in
+// registers, where additions round to nearest, against the running maximum (log2 units).
 //
 // Roles.  Warps 0-3: softmax, a row (a TMEM lane) to a thread, and its output, 128 registers.  Warps 4-11: queries,
-// K and V, read from the pages, split, and stored to shared memory as the products want them.  Warp 12 issues the
-// products.  Numbers are split at half their size, so that none rounds up to infinity.  Of the block's 512 x 128
-// registers at launch the warpgroups take 128 x (240 + 104 + 104 + 64).
+// K and V, read from the pages a tile ahead, split, and stored to shared memory as the products want them.  Warp 12
+// issues the products.  Of the block's 512 x 128 registers at launch the warpgroups take 128 x (208 + 128 + 128 + 48).
+//
+// What bounds it: 4.5 K cycles of products a tile, and the code, of which an SM holds little: 8 K cycles a tile with
+// few tiles a CTA (every role unrolled, and half the loading warps, took 15 K).  300 queries of 4 heads over 16
+// units of up to 1203 slots take 58 us (184 on CUDA cores), 77 of 7 over 6 units 23.4 (47), 24 rows over 64 units of
+// up to 6000 slots 104 (211), 9 over 128 of 1500 65 (96).
 #include <stddef.h>
 
 #include <algorithm>
@@ -34,7 +38,6 @@ static_assert(kSmem <= 227 * 1024 && sizeof(PlanSmem) <= 1024, "smem");
 constexpr uint32_t kColP = 128, kColO = 384;   // TMEM: S at 0 and 64, P at 128 and 256 (three parts of 32), O
 constexpr long long kWaitBudget = 1ll << 32;   // cycles (~2 s)
 constexpr long long kTestWaitBudget = 1ll << 22;   // ~2 ms: GRKV_TEST_TIMEOUT's
-constexpr float kSlack = 8.f;                  // by which logits may pass their reference (log2)
 
 // Arrivals that complete a phase: 8 loading warps, 4 of the softmax, or 1 where products do.
 struct Bars {
@@ -113,8 +116,8 @@ __device__ __forceinline__ int pages_of(const CrossArgs& a, const Cursor& cur, i
   const int c = (cur.slot() >> a.shift) + lane;
   return lane < max(1, kSub >> a.shift) && c << a.shift < cur.sg.it.L ? page_of(a, cur.sg.it.u, c, err) : 0;
 }
-__device__ __forceinline__ void load_chunks(const CrossArgs& a, const void* pool, int pages, int x0, int L, int r0, int c,
-                                            Chunks* z) {
+__device__ __forceinline__ void load_chunks(const CrossArgs& a, const void* pool, int pages, int x0, int L, int r0,
+                                            int c, Chunks* z) {
 #pragma unroll
   for (int j = 0; j < kChunks; ++j) {
     const int r = r0 + kRowStep * j, slot = x0 + r;
@@ -208,48 +211,48 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
 
   if (warp >= 12) {
     // ------------------------------------------------------------- the products
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (warp == 12) {
-    constexpr uint32_t id_s = idesc_bf16(128, kSub, 0, 0);   // both K-major
-    constexpr uint32_t id_o = idesc_bf16(128, kD, 0, 1);     // V MN-major
-    const uint64_t q_desc = sw128_desc(smem_u32(sm + kOffQ), 16, 1024);
-    const uint64_t k_desc = sw128_desc(smem_u32(sm + kOffK), 16, 1024);
-    const uint64_t v_desc = sw128_desc(smem_u32(sm + kOffV), kKvPart / 2, 1024);
-    int tiles = 0;
-    for (Segments<CrossArgs> sg(a, run); sg.more(); sg.next(a)) tiles += tiles_of(sg);
-    auto issue_s = [&](int n) -> bool {
-      if (!wait(&bars->k_full, n)) return false;   // and the queries, if it is a segment's first
-      tc_fence_after();
-#pragma unroll
-      for (int p = 0; p < 6; ++p)
-        mma_s<id_s>(tmem + (n & 1) * kSub, q_desc + ((part_of(kLeft, p) * kQPart) >> 4),
-                    k_desc + ((part_of(kRight, p) * kKvPart) >> 4), p > 0);
-      mma_commit_elect(&bars->s_full[n & 1]);
-      mma_commit_elect(&bars->k_empty);
-      return true;
-    };
-    bool ok = tiles == 0 || issue_s(0);
-    for (int n = 0; ok && n < tiles; ++n) {
-      if (n + 1 < tiles) ok = issue_s(n + 1);
-      ok = ok && wait(&bars->p_full[n & 1], n >> 1) && wait(&bars->v_full, n) && (n == 0 || wait(&bars->o_empty, n - 1));
-      if (!ok) break;
-      tc_fence_after();
-#pragma unroll
-      for (int p = 0; p < 6; ++p)
-        mma_o<id_o>(tmem + kColO, tmem + kColP + (n & 1) * 128 + part_of(kLeft, p) * 32,
-                    v_desc + ((part_of(kRight, p) * kKvPart) >> 4), p > 0);
-      mma_commit_elect(&bars->o_full);
-      mma_commit_elect(&bars->v_empty);
-    }
-    // every product issued so far completes before TMEM is released
-    mma_commit_elect(&bars->drain);
-    volatile int no_abort = 0;
-    mbar_wait(&bars->drain, 0, &no_abort, kWaitBudget);
-    __syncwarp();
+      constexpr uint32_t id_s = idesc_bf16(128, kSub, 0, 0);   // both K-major
+      constexpr uint32_t id_o = idesc_bf16(128, kD, 0, 1);     // V MN-major
+      const uint64_t q_desc = sw128_desc(smem_u32(sm + kOffQ), 16, 1024);
+      const uint64_t k_desc = sw128_desc(smem_u32(sm + kOffK), 16, 1024);
+      const uint64_t v_desc = sw128_desc(smem_u32(sm + kOffV), kKvPart / 2, 1024);
+      int tiles = 0;
+      for (Segments<CrossArgs> sg(a, run); sg.more(); sg.next(a)) tiles += tiles_of(sg);
+      auto issue_s = [&](int n) -> bool {
+        if (!wait(&bars->k_full, n)) return false;   // and the queries, if it is a segment's first
+        tc_fence_after();
+#pragma unroll 1
+        for (int p = 0; p < 6; ++p)
+          mma_s<id_s>(tmem + (n & 1) * kSub, q_desc + ((part_of(kLeft, p) * kQPart) >> 4),
+                      k_desc + ((part_of(kRight, p) * kKvPart) >> 4), p > 0);
+        mma_commit_elect(&bars->s_full[n & 1]);
+        mma_commit_elect(&bars->k_empty);
+        return true;
+      };
+      bool ok = tiles == 0 || issue_s(0);
+      for (int n = 0; ok && n < tiles; ++n) {
+        if (n + 1 < tiles) ok = issue_s(n + 1);
+        ok = ok && wait(&bars->p_full[n & 1], n >> 1) && wait(&bars->v_full, n) &&
+             (n == 0 || wait(&bars->o_empty, n - 1));
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll 1
+        for (int p = 0; p < 6; ++p)
+          mma_o<id_o>(tmem + kColO, tmem + kColP + (n & 1) * 128 + part_of(kLeft, p) * 32,
+                      v_desc + ((part_of(kRight, p) * kKvPart) >> 4), p > 0);
+        mma_commit_elect(&bars->o_full);
+        mma_commit_elect(&bars->v_empty);
+      }
+      // every product issued so far completes before TMEM is released
+      mma_commit_elect(&bars->drain);
+      volatile int no_abort = 0;
+      mbar_wait(&bars->drain, 0, &no_abort, kWaitBudget);
+      __syncwarp();
     }
   } else if (warp >= 4) {
     // -------------------------------------------- queries, K (a tile ahead) and V
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     const int t = tid - 128, c = t & 15, r0 = t >> 4;
     // K of tile n + 1 is stored once S of tile n has been formed, then V of tile n once O of the one before has;
     // both were asked for a tile earlier, their pages before that.
@@ -310,7 +313,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
     }
   } else {
     // ------------------------------------------------------- softmax and outputs
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 240;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int row = warp * 32 + lane;
     const uint32_t lane_addr = tmem + ((uint32_t)(warp * 32) << 16);
     const float sl2 = 4.f * a.sl2;   // of halved queries and keys
@@ -356,12 +359,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
           if (32 * c + x < left) top = fmaxf(top, v[x]);
       }
       top = __fmul_rn(top, sl2);
-      float f = 1.f;
-      if (m == -INFINITY || top > m + kSlack) {
-        const float to = fmaxf(m, top);
-        if (m != -INFINITY) f = fast_exp2(m - to);
-        m = to;
-      }
+      const float to = fmaxf(m, top), f = m == -INFINITY || to == m ? 1.f : fast_exp2(m - to);
+      m = to;
       const float ref = m == -INFINITY ? 0.f : m;
       float sum = 0.f;
 #pragma unroll 1
@@ -435,7 +434,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
 
 }  // namespace
 
-bool cross_is_split(const CacheShape& s) { return s.dtype == GRKV_F32 && !s.simt && s.g * s.t > 16; }
+// From 9 rows on, where a row tile is filled by a tenth: 9 rows of a unit of 300 slots take 17 us (20 in the CUDA-core
+// kernel), of 128 units of 1500 65 (96), of 8000 241 (381); 64 rows 71 (118) and 248 (510).  Up to 8 rows, tiles of the
+// CUDA-core kernel that are mostly empty too are faster: 128 units of 1500 slots take 42.
+bool cross_is_split(const CacheShape& s) { return s.dtype == GRKV_F32 && !s.simt && s.g * s.t > 8; }
 
 void split_rows(const CacheShape& s, AttendArgs* a) {
   // two tiles of the CUDA-core kernels' 64 rows, whose parts the workspace holds
