@@ -191,12 +191,13 @@ def test_scale(grkv_lib, dtype, flags):
     case([200, 90], 2, 3, 16, dtype, flags, seed=8, scale=0.25)
 
 
-@pytest.mark.parametrize("dtype,flags", TYPES)
-def test_one_token_sees_what_decoding_sees(grkv_lib, dtype, flags):
+@pytest.mark.parametrize("dtype,flags,g", [("bf16", 0, 20), ("bf16", b.GRKV_FORCE_SIMT, 20),
+                                           ("f32", b.GRKV_FORCE_SIMT, 20), ("f32", 0, 7)])
+def test_one_token_sees_what_decoding_sees(grkv_lib, dtype, flags, g):
     """The last slot's own token sees every slot: bit for bit grkv_attend, where its kernels run."""
     c = R.Cache([1, 77, 4000, 333], 32, dtype, 9)
-    q, _ = queries(4, 20, 1, dtype, 10)
-    p = b.cache_params(4, 20, c.pages, 32, c.cols, dtype=dtype, flags=flags)
+    q, _ = queries(4, g, 1, dtype, 10)
+    p = b.cache_params(4, g, c.pages, 32, c.cols, dtype=dtype, flags=flags)
     out, lse, _ = run(c, p, q)
     kd, vd = c.dev()
     o, l, ws = torch.zeros_like(out), torch.zeros_like(lse), workspace(p)
@@ -283,14 +284,15 @@ def test_faults_are_reported(grkv_lib, dtype, flags):
     check(c, q64, out, lse, [3, 3])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("g,t", [(20, 1), (50, 2), (4, 200)])
-def test_a_wait_that_runs_out_ends_the_call(grkv_lib, g, t):
+def test_a_wait_that_runs_out_ends_the_call(grkv_lib, dtype, g, t):
     gen = torch.Generator(device="cuda").manual_seed(g)
-    rnd = lambda *s: torch.randn(*s, dtype=torch.float32, device="cuda", generator=gen).bfloat16()
+    rnd = lambda *s: torch.randn(*s, dtype=torch.float32, device="cuda", generator=gen).to(R.TORCH[dtype])
     k, v, q = rnd(60, 64, D), rnd(60, 64, D), rnd(300, g, t, D)
     table = torch.arange(60, device="cuda").int().repeat(300, 1)
     lens = torch.full((300,), 60 * 64 - 5, dtype=torch.int32, device="cuda")
-    p = b.cache_params(300, g, 60, 64, 60, tokens=t)
+    p = b.cache_params(300, g, 60, 64, 60, tokens=t, dtype=dtype)
     ws, outs = workspace(p), []
     for flags in (0, b.GRKV_TEST_TIMEOUT, 0):
         p.flags = flags
@@ -300,6 +302,40 @@ def test_a_wait_that_runs_out_ends_the_call(grkv_lib, g, t):
         if not flags:
             outs.append(out)
     assert outs[0].abs().max() > 0 and torch.equal(*outs)
+
+
+# fp32 rows of 9 and more are products of bf16 parts; of the other kernels, for comparison
+@pytest.mark.parametrize("flags", [0, b.GRKV_FORCE_SIMT])
+@pytest.mark.parametrize("g,t", [(9, 1), (4, 70), (33, 4), (64, 3), (1, 129)])
+@pytest.mark.parametrize("power_k,power_v", [(0, 100), (0, -100), (40, 0), (-40, 60)])
+def test_numbers_of_any_size(grkv_lib, flags, g, t, power_k, power_v):
+    """Values near the ends of fp32's range, one at its very end; keys that the queries' size makes up for."""
+    c = R.Cache([300, 77, 64, 0], 16, "f32", 50)
+    q, q64 = queries(4, g, t, "f32", 51)
+    q, q64 = q * 2.0 ** -power_k, q64 * 2.0 ** -power_k
+    c.k, c.v = c.k * 2.0 ** power_k, c.v * 2.0 ** power_v
+    if power_v > 0:
+        c.v[c.table[1, 3], 9, 17] = float(np.finfo(np.float32).max)
+    p = b.cache_params(4, g, c.pages, 16, c.cols, tokens=t, dtype="f32", flags=flags)
+    out, lse, status = run(c, p, q)
+    assert status == b.GRKV_OK
+    check(c, q64, out, lse, [t] * 4)
+
+
+@pytest.mark.parametrize("g,t", [(9, 1), (7, 77), (4, 200)])
+def test_fp32_runs_are_equal(grkv_lib, g, t):
+    """Many units, so that a CTA has several segments, whole ones and parts; twice the same to the bit."""
+    rng = np.random.default_rng(60)
+    lens = [int(x) for x in rng.integers(0, 700, 60)]
+    c = R.Cache(lens, 32, "f32", 61)
+    q, q64 = queries(60, g, t, "f32", 62)
+    q_lens = [int(x) for x in rng.integers(0, t + 1, 60)]
+    p = b.cache_params(60, g, c.pages, 32, c.cols, tokens=t, dtype="f32")
+    o1, l1, status = run(c, p, q, q_lens=q_lens)
+    assert status == b.GRKV_OK
+    check(c, q64, o1, l1, q_lens)
+    o2, l2, _ = run(c, p, q, q_lens=q_lens)
+    assert torch.equal(o1, o2) and torch.equal(l1, l2)
 
 
 # ---------------------------------------------------------------- a decoder's steps
