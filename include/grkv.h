@@ -395,8 +395,12 @@ int grkv_attend_tree(const grkv_cache_params* p, const void* q, const void* k_pa
  * several sequences read, a cache compressed with causal = 0.  Row i < q_len[u] (NULL: t) of unit u
  * sees every slot j < len[u]; queries are no slots of the cache, so that q_len and len have nothing
  * to do with each other.  window and n_sink are not read.  The rest, errors and roundings too (up to 8
- * rows g t of bf16 may be rounded less), is grkv_attend's: a unit of length 0 gives out = 0 and lse = -inf, rows from q_len[u] on are left as
- * they were.  Beams of a sequence, whose caches are one, go into the group. */
+ * rows g t of bf16 may be rounded less), is grkv_attend's: a unit of length 0 gives out = 0 and
+ * lse = -inf, rows from q_len[u] on are left as they were.  Beams of a sequence, whose caches are
+ * one, go into the group.  With 9 rows g t of fp32 and more, queries, keys, values and probabilities
+ * are multiplied as three bf16 parts each, which leave 2^-27 of a number, or 2^-125 where that is
+ * more (GRKV_FORCE_SIMT: fp32 as they are); a key or value that is not finite then makes every
+ * element that it reaches NaN. */
 int grkv_attend_cross(const grkv_cache_params* p, const void* q, const void* k_pages,
                       const void* v_pages, const int32_t* table, const int32_t* len,
                       const int32_t* q_len, void* out, float* lse, void* ws, size_t ws_bytes,
