@@ -485,7 +485,8 @@ typedef struct {
  * pos[s][i] (int32 [S][t]), or start[s] + i (start int32 [S], NULL: 0); not both arrays.  Rows at negative
  * positions, padding, are left as they were.  out may be in, with the same strides; otherwise
  * they must not overlap, nor out's rows each other (GRKV_ERR_INVALID_ARG for strides that step into
- * their own rows; an input's may be 0).  Takes no workspace and reports no status. */
+ * their own rows, an input's may be 0, or reach over more than 2^40 elements).  Takes no workspace
+ * and reports no status. */
 int grkv_rope_rows(const grkv_rope* rope, const grkv_rows* rows, const void* in, void* out,
                    const int32_t* pos, const int32_t* start, void* stream);
 

@@ -1,4 +1,4 @@
-// Attention over encoder states for few rows (up to 8 a unit: single tokens) of caches that are small
+// Attention over encoder states for few rows (up to 16 a unit: single tokens) of caches that are small
 // enough for a call to be a matter of latency.
 //
 // A cluster of CTAs takes a unit, its warps the unit's slots, 16 or 8 to a step, in turn: there is

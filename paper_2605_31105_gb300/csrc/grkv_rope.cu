@@ -131,12 +131,13 @@ __global__ void __launch_bounds__(kRowThreads)
     if (j < heads) store_pair<T, H>(out + j * a.os[1], at, rotate<T, H>(x[j], at, an));
 }
 
-// Whether rows of the strides (elements) are whole vectors apart, and, for outputs, apart at all.
+// Whether rows of the strides (elements) are whole vectors apart, reach over 2^40 elements at most, and, for outputs,
+// are apart at all.
 int check_strides(const int64_t* stride, const int64_t* n, int vec, bool apart) {
   for (int x = 0; x < 3; ++x)
     if (n[x] > 1 && stride[x] % vec) return GRKV_ERR_MISALIGNED;
   for (int x = 0; x < 3; ++x)
-    if (n[x] > 1 && (stride[x] < 0 || stride[x] > (int64_t)1 << 40)) return GRKV_ERR_INVALID_ARG;
+    if (n[x] > 1 && (stride[x] < 0 || stride[x] > ((int64_t)1 << 40) / (n[x] - 1))) return GRKV_ERR_INVALID_ARG;
   if (!apart) return GRKV_OK;
   int order[3] = {0, 1, 2};
   std::sort(order, order + 3, [&](int x, int y) { return stride[x] < stride[y]; });

@@ -100,7 +100,8 @@ def rows(seqs=2, heads=3, tokens=4, d=128, dtype=b.GRKV_BF16, flags=0, ins=(1536
     (dict(ins=(1538, 512, 128), dtype=b.GRKV_F32), -4), (dict(ins=(-1536, 512, 128)), -1),
     (dict(outs=(1536, 512, 120)), -1), (dict(outs=(1536, 0, 128)), -1), (dict(outs=(128, 512, 128)), -1),
     (dict(outs=(1536, 384, 128)), -1), (dict(outs=(1408, 512, 128)), -1),
-    (dict(out=FAKE, outs=(1536, 128, 384)), -1), (dict(out=FAKE, ins=(0, 512, 128)), -1)])
+    (dict(out=FAKE, outs=(1536, 128, 384)), -1), (dict(out=FAKE, ins=(0, 512, 128)), -1),
+    (dict(outs=(1536, (1 << 39) + 8, 128)), -1), (dict(ins=(1536, 1 << 40, 128)), -1)])
 def test_rows_that_are_refused(lib, kw, code):  # noqa: F811
     assert rows(**kw) == code
 
