@@ -41,6 +41,8 @@ struct AttendArgs {
   int* status;
   int withhold;   // GRKV_TEST_TIMEOUT: CTA 0 withholds one arrive (tensor cores)
   static constexpr bool cross = false;
+  static constexpr int tile = kSlotTile;
+  __device__ int extra_of(long long) const { return extra; }   // of a call of so many tiles
   __device__ bool tree() const { return parent != nullptr; }
 };
 
@@ -50,6 +52,12 @@ struct AttendArgs {
 struct CrossArgs : AttendArgs {
   static constexpr bool cross = true;
   __device__ bool tree() const { return false; }
+};
+// ... in slot tiles of 64 (grkv_cross_split.cu).
+struct SplitArgs : CrossArgs {
+  static constexpr int tile = 64;
+  // where CTAs have one tile each, there is nothing to even out
+  __device__ int extra_of(long long all) const { return all > gridDim.x ? extra : 0; }
 };
 
 // One item: tokens [tok0, tok0 + ntok) of unit u; the slots that its rows see are in
@@ -75,9 +83,9 @@ __device__ __forceinline__ Item make_item(const A& a, int u, int qb, int L, int 
   it.hi = A::cross ? L : max(0, it.base + it.tok0 + it.ntok);
   it.lo = !A::cross && a.W ? min(max(0, p0 - a.W + 1), it.hi) : 0;
   it.sink_end = !A::cross && a.W ? min(a.s, it.lo) : 0;
-  it.lo_tile = it.lo / kSlotTile;
-  it.ns = min((it.sink_end + kSlotTile - 1) / kSlotTile, it.lo_tile);
-  it.nt = it.ns + (it.hi + kSlotTile - 1) / kSlotTile - it.lo_tile;
+  it.lo_tile = it.lo / A::tile;
+  it.ns = min((it.sink_end + A::tile - 1) / A::tile, it.lo_tile);
+  it.nt = it.ns + (it.hi + A::tile - 1) / A::tile - it.lo_tile;
   if (it.ntok == 0) it.nt = 0;
   else if (it.nt < 1) it.nt = 1;   // rows that see nothing are written by a tile without slots
   return it;
@@ -287,10 +295,11 @@ __device__ __forceinline__ Run plan_run_of(const A& a, PlanSmem* ps, int n) {
   const int all_live = warp_total(cnt), front = warp_total(lane < warp ? cnt : 0) + scan_live - live;
   I tiles = tiles_before + scan - mine;
   if (all > 0) {
-    const Split<I> sp(all + (I)a.extra * all_live, (int)min((I)gridDim.x, all));
+    const I extra = a.extra_of(all);
+    const Split<I> sp(all + extra * all_live, (int)min((I)gridDim.x, all));
     const int c = blockIdx.x;
-    I at = tiles + (I)a.extra * front;
-    const I end = at + mine + (I)a.extra * live;
+    I at = tiles + extra * front;
+    const I end = at + mine + extra * live;
     const I t0 = sp.start(c), t1 = sp.start(c + 1);
     // each end of the run is in the items of one thread
     const bool first = at <= t0 && t0 < end, last = at < t1 && t1 <= end;
@@ -298,7 +307,7 @@ __device__ __forceinline__ Run plan_run_of(const A& a, PlanSmem* ps, int n) {
       for (int i = i0, u = first_u, qb = first_qb; i < i1; ++i) {
         const int nt = i == i0 ? nt0 : make_item(a, u, qb).nt;
         if (nt > 0) {
-          const I from = at + a.extra, to = from + nt;   // its tiles
+          const I from = at + extra, to = from + nt;   // its tiles
           if (at <= t0 && t0 < to) {
             const int off = (int)max((I)0, t0 - from);
             ps->run = Run{u, qb, off, 0};
@@ -353,7 +362,7 @@ struct Segments {
   }
   __device__ bool more() const { return left > 0; }
   __device__ bool whole() const { return off == 0 && cnt == it.nt; }
-  __device__ int end() const { return (it.tile(off + cnt - 1) + 1) * kSlotTile; }
+  __device__ int end() const { return (it.tile(off + cnt - 1) + 1) * A::tile; }
   __device__ int slot(int cta) const { return off == 0 ? 2 * cta + 1 : 2 * cta; }
   __device__ void next(const A& a) {
     left -= cnt;

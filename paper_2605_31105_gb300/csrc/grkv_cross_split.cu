@@ -13,10 +13,13 @@
 // K and V, read from the pages a tile ahead, split, and stored to shared memory as the products want them.  Warp 12
 // issues the products.  Of the block's 512 x 128 registers at launch the warpgroups take 128 x (208 + 128 + 128 + 48).
 //
-// What bounds it: 4.5 K cycles of products a tile, and the code, of which an SM holds little: 8 K cycles a tile with
-// few tiles a CTA (every role unrolled, and half the loading warps, took 15 K).  300 queries of 4 heads over 16
-// units of up to 1203 slots take 58 us (184 on CUDA cores), 77 of 7 over 6 units 23.4 (47), 24 rows over 64 units of
-// up to 6000 slots 104 (211), 9 over 128 of 1500 65 (96).
+// What bounds it: 4.5 K cycles of products a tile, and the code, of which an SM holds little: 7.5 K cycles a tile
+// (every role unrolled, and half the loading warps, took 15 K).  Runs are planned in tiles of 64 slots and an item's
+// start and end as one more (in tiles of 128, 9 rows of one unit of 300 slots took 17.8 us for 14.9).  300 queries of
+// 4 heads over 16 units of up to 1203 slots take 55 us (184 on CUDA cores), 77 of 7 over 6 units 22.5 (47), 24 rows
+// over 64 units of up to 6000 slots 97 (211), 9 over 128 of 1500 60 (96).  Q in TMEM, with K and V in two buffers or
+// copied two tiles ahead, was slower (128 units of 8000 slots 243 us for 226), as were parts formed before there is
+// room for them (285).
 #include <stddef.h>
 
 #include <algorithm>
@@ -28,7 +31,7 @@ namespace {
 
 using namespace sm100;
 
-constexpr int kSub = 64;                       // slots of a tile
+constexpr int kSub = SplitArgs::tile;
 constexpr int kThreads = 512, kLoaders = 256;   // kLoaders: of queries, K and V
 constexpr uint32_t kQPart = 128 * kD * 2;      // 32 KB: two halves of 64 dimensions
 constexpr uint32_t kKvPart = kSub * kD * 2;    // 16 KB
@@ -50,26 +53,19 @@ struct Bars {
 constexpr int kBars = 11;
 static_assert(sizeof(Bars) <= 256 && offsetof(Bars, tmem) == 8 * kBars, "barriers");
 
-// Slot tiles of a segment: from its first slot on, those that hold slots.
-__device__ __forceinline__ int tiles_of(const Segments<CrossArgs>& sg) {
-  return max(1, min(2 * sg.cnt, (sg.it.L - sg.off * kSlotTile + kSub - 1) / kSub));
-}
 // A CTA's slot tiles in order.
 struct Cursor {
-  Segments<CrossArgs> sg;
-  int sub = 0, subs = 0;
-  __device__ Cursor(const CrossArgs& a, const Run& run) : sg(a, run) {
-    if (sg.more()) subs = tiles_of(sg);
-  }
+  Segments<SplitArgs> sg;
+  int sub = 0;
+  __device__ Cursor(const SplitArgs& a, const Run& run) : sg(a, run) {}
   __device__ bool more() const { return sg.more(); }
   __device__ bool first() const { return sub == 0; }
-  __device__ bool last() const { return sub + 1 == subs; }
-  __device__ int slot() const { return sg.off * kSlotTile + sub * kSub; }
-  __device__ void next(const CrossArgs& a) {
-    if (++sub < subs) return;
+  __device__ bool last() const { return sub + 1 == sg.cnt; }
+  __device__ int slot() const { return (sg.off + sub) * kSub; }
+  __device__ void next(const SplitArgs& a) {
+    if (++sub < sg.cnt) return;
     sg.next(a);
     sub = 0;
-    if (sg.more()) subs = tiles_of(sg);
   }
 };
 
@@ -112,11 +108,11 @@ struct Chunks {
   float4 x[kChunks], y[kChunks];
 };
 // The pages of a tile's slots, one to a lane (four of 16 slots, or fewer).
-__device__ __forceinline__ int pages_of(const CrossArgs& a, const Cursor& cur, int lane, int* err) {
+__device__ __forceinline__ int pages_of(const SplitArgs& a, const Cursor& cur, int lane, int* err) {
   const int c = (cur.slot() >> a.shift) + lane;
   return lane < max(1, kSub >> a.shift) && c << a.shift < cur.sg.it.L ? page_of(a, cur.sg.it.u, c, err) : 0;
 }
-__device__ __forceinline__ void load_chunks(const CrossArgs& a, const void* pool, int pages, int x0, int L, int r0,
+__device__ __forceinline__ void load_chunks(const SplitArgs& a, const void* pool, int pages, int x0, int L, int r0,
                                             int c, Chunks* z) {
 #pragma unroll
   for (int j = 0; j < kChunks; ++j) {
@@ -183,7 +179,7 @@ __device__ __forceinline__ void mma_o(uint32_t d, uint32_t p, uint64_t v, bool a
 constexpr uint32_t kLeft = 0x001102, kRight = 0x010120;
 __host__ __device__ constexpr uint32_t part_of(uint32_t parts, int p) { return (parts >> (4 * p)) & 15; }
 
-__global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_constant__ CrossArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_constant__ SplitArgs a) {
   extern __shared__ __align__(1024) uint8_t smraw[];
   uint8_t* sm = (uint8_t*)(((uintptr_t)smraw + 1023) & ~(uintptr_t)1023);
   Bars* bars = (Bars*)(sm + kOffBar);
@@ -218,8 +214,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
       const uint64_t q_desc = sw128_desc(smem_u32(sm + kOffQ), 16, 1024);
       const uint64_t k_desc = sw128_desc(smem_u32(sm + kOffK), 16, 1024);
       const uint64_t v_desc = sw128_desc(smem_u32(sm + kOffV), kKvPart / 2, 1024);
-      int tiles = 0;
-      for (Segments<CrossArgs> sg(a, run); sg.more(); sg.next(a)) tiles += tiles_of(sg);
+      const int tiles = run.left;
       auto issue_s = [&](int n) -> bool {
         if (!wait(&bars->k_full, n)) return false;   // and the queries, if it is a segment's first
         tc_fence_after();
@@ -434,8 +429,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
 
 }  // namespace
 
-// From 9 rows on, where a row tile is filled by a tenth: 9 rows of a unit of 300 slots take 17 us (20 in the CUDA-core
-// kernel), of 128 units of 1500 65 (96), of 8000 241 (381); 64 rows 71 (118) and 248 (510).  Up to 8 rows, tiles of the
+// From 9 rows on, where a row tile is filled by a tenth: 9 rows of a unit of 300 slots take 15 us (20 in the CUDA-core
+// kernel), of 128 units of 1500 60 (96), of 8000 226 (381); 64 rows 63 (118) and 233 (510).  Up to 8 rows, tiles of the
 // CUDA-core kernel that are mostly empty too are faster: 128 units of 1500 slots take 42.
 bool cross_is_split(const CacheShape& s) { return s.dtype == GRKV_F32 && !s.simt && s.g * s.t > 8; }
 
@@ -446,13 +441,15 @@ void split_rows(const CacheShape& s, AttendArgs* a) {
   a->nq = 1;
   a->QB = (s.t + a->T - 1) / a->T;
   a->rows = a->T * s.g;
+  a->extra = 1;   // queries and output
+  a->wide = 2 * attend_tiles(s) + (int64_t)s.U * a->QB * a->extra >= 1 << 30;   // tiles of half the slots
 }
 
 cudaError_t launch_cross_split(const AttendArgs& a, int G, cudaStream_t st) {
   const cudaError_t e = cudaFuncSetAttribute(k_cross_split, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
   if (e != cudaSuccess) return e;
   count_launches(1);
-  return launch_kernel(false, 1, k_cross_split, dim3((unsigned)G), kThreads, kSmem, st, CrossArgs{a});
+  return launch_kernel(false, 1, k_cross_split, dim3((unsigned)G), kThreads, kSmem, st, SplitArgs{a});
 }
 
 }  // namespace grkv
