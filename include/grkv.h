@@ -466,7 +466,8 @@ typedef struct {
 
 /* Fills `p` with the defaults above (half layout, every dimension, no scaling). */
 void grkv_rope_params_init(grkv_rope_params* p);
-/* factors: HOST array [rotary / 2] by which the frequencies are divided as well, or NULL. */
+/* factors: HOST array [rotary / 2] by which the frequencies are divided as well, or NULL.  Frequencies from
+ * 1024 radians a position on (factors far below 1) are GRKV_ERR_INVALID_ARG. */
 int grkv_rope_make(const grkv_rope_params* p, const double* factors, grkv_rope* rope);
 
 #define GRKV_ROPE_TRANSPOSE 0x1u /* the angles' signs turned: the gradient of the rotation's input from

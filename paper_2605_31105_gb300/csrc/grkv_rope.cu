@@ -15,6 +15,10 @@ using namespace grkv;
 namespace {
 
 // ---------------------------------------------------------------------- the plan
+// Radians a position from which a plan is refused.  fp64 leaves 2^-53 of a frequency's turns: less than 2^-45 turns below
+// this, nothing of the fraction from 2^53 on; factors far below 1 overflow, too.
+constexpr double kMostRadians = 1024;
+
 int make_rope(const grkv_rope_params* p, const double* factors, grkv_rope* rope) {
   if (!p || !rope) return GRKV_ERR_INVALID_ARG;
   if (p->d < 1 || p->rotary < 2 || p->rotary > p->d || p->rotary % 2) return GRKV_ERR_INVALID_ARG;
@@ -62,6 +66,7 @@ int make_rope(const grkv_rope_params* p, const double* factors, grkv_rope* rope)
       if (!positive(factors[i])) return GRKV_ERR_INVALID_ARG;
       f /= factors[i];
     }
+    if (!(f < kMostRadians)) return GRKV_ERR_INVALID_ARG;   // infinities and NaN too
     double t = f / pi2;
     t = std::ldexp(t - std::floor(t), 64);   // at most 2^64 - 2^11: the fraction has 53 bits
     out.turns[i] = (uint64_t)std::round(t);
