@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int row = warp * 32 + lane;
     const uint32_t lane_addr = tmem + ((uint32_t)(warp * 32) << 16);
-    const float sl2 = 4.f * a.sl2;   // of halved queries and keys
+    const float sl2 = a.sl2;   // of halved queries and keys: logits are four times its products, which may pass fp32 first
     float acc[kD];
     float m = -INFINITY, l = 0.f;
     bool ok = true;
@@ -353,10 +353,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
         for (int x = 0; x < 32; ++x)
           if (32 * c + x < left) top = fmaxf(top, v[x]);
       }
-      top = __fmul_rn(top, sl2);
+      top = 4.f * __fmul_rn(top, sl2);
       const float to = fmaxf(m, top), f = m == -INFINITY || to == m ? 1.f : fast_exp2(m - to);
       m = to;
-      const float ref = m == -INFINITY ? 0.f : m;
+      // (an infinite logit makes its row NaN: against infinity, exact products would all weigh nothing)
+      const float ref = m == -INFINITY ? 0.f : m == INFINITY ? NAN : m;
       float sum = 0.f;
 #pragma unroll 1
       for (int c = 0; c < 2; ++c) {
@@ -366,8 +367,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
         uint32_t p[3][16];
 #pragma unroll
         for (int x = 0; x < 32; ++x) {
-          // rounded product and difference: a fused one would be off by what rounding took from the reference
-          v[x] = 32 * c + x < left ? fast_exp2(__fsub_rn(__fmul_rn(v[x], sl2), ref)) : 0.f;
+          // the product rounded, as the reference's was: an exact one would be off by what rounding took from that
+          v[x] = 32 * c + x < left ? fast_exp2(__fmaf_rn(4.f, __fmul_rn(v[x], sl2), -ref)) : 0.f;
           sum += v[x];
         }
 #pragma unroll
