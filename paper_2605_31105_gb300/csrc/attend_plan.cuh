@@ -404,6 +404,12 @@ __device__ __forceinline__ float4* part4(const AttendArgs& a, int slot, int c4, 
   return (float4*)a.po + ((size_t)slot * (kD / 4) + c4) * a.rows + r;
 }
 
+// A product q k as a logit in log2 units, and what a logit weighs against a reference, itself a logit.  Each step is
+// rounded by itself: where a compiler fused them, the product would be exact and the reference not, 2^-25 of it
+// apart, which for logits of 2^33 is more than an exponent holds.
+__device__ __forceinline__ float logit_of(float product, float sl2) { return __fmul_rn(product, sl2); }
+__device__ __forceinline__ float prob_of(float logit, float ref) { return sm100::fast_exp2(__fsub_rn(logit, ref)); }
+
 // What a partial result with reference m weighs against reference M.
 __device__ __forceinline__ float weight_of(float m, float M) {
   return m == -INFINITY ? 0.f : sm100::fast_exp2(m - M);

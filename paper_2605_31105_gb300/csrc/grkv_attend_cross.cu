@@ -208,13 +208,13 @@ __global__ void __launch_bounds__(kThreads, R <= 4 ? 2 : 1)
     }
     const float dot = sum_lanes<R * kLoad, kLanes>(x, lane);
     const bool see = F::kSide * my_slot < L - k * F::kSlots - side;
-    const float logit = see ? dot * a.sl2 : -INFINITY;
+    const float logit = see ? logit_of(dot, a.sl2) : -INFINITY;
     float top = logit;
 #pragma unroll
     for (int d = kLoad / 2; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d * F::kStep));
     if (F::kSide == 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, kLanes));
     const float M = fmaxf(m, top), ref = M == -INFINITY ? 0.f : M;
-    const float keep = fast_exp2(m - ref), p = see ? fast_exp2(logit - ref) : 0.f;
+    const float keep = fast_exp2(m - ref), p = see ? prob_of(logit, ref) : 0.f;
     m = M;
     l = l * keep + p;
     const bool scale = __any_sync(0xffffffffu, keep != 1.f);
@@ -458,15 +458,16 @@ __global__ void __launch_bounds__(kMmaThreads, NT == 1 ? 4 : 3)
       float keep[2], p[4];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float x0 = i < n ? s[x][e] * a.sl2 : -INFINITY, x1 = i + 8 < n ? s[x][2 + e] * a.sl2 : -INFINITY;
+        const float x0 = i < n ? logit_of(s[x][e], a.sl2) : -INFINITY;
+        const float x1 = i + 8 < n ? logit_of(s[x][2 + e], a.sl2) : -INFINITY;
         float top = fmaxf(x0, x1);
 #pragma unroll
         for (int d = 4; d <= 16; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
         const float M = fmaxf(m[x][e], top), ref = M == -INFINITY ? 0.f : M;
         keep[e] = fast_exp2(m[x][e] - ref);
         m[x][e] = M;
-        p[e] = i < n ? fast_exp2(x0 - ref) : 0.f;
-        p[2 + e] = i + 8 < n ? fast_exp2(x1 - ref) : 0.f;
+        p[e] = i < n ? prob_of(x0, ref) : 0.f;
+        p[2 + e] = i + 8 < n ? prob_of(x1, ref) : 0.f;
         l[x][e] = l[x][e] * keep[e] + (p[e] + p[2 + e]);
       }
       if (__any_sync(0xffffffffu, keep[0] != 1.f || keep[1] != 1.f)) {

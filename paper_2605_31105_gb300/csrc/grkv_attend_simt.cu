@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_simt(A a) {
         for (int j = 0; j < 4; ++j) {
           const uint32_t w = j < 2 ? w0 : w1;
           const bool see = (w >> ((tx + 16 * j) & 31)) & 1;
-          sc[r][j] = see ? sc[r][j] * a.sl2 : -INFINITY;
+          sc[r][j] = see ? logit_of(sc[r][j], a.sl2) : -INFINITY;
           top = fmaxf(top, sc[r][j]);
         }
 #pragma unroll
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_simt(A a) {
         for (int j = 0; j < 4; ++j) {
           const uint32_t w = j < 2 ? w0 : w1;
           const bool see = (w >> ((tx + 16 * j) & 31)) & 1;
-          const float p = fast_exp2(sc[r][j] - ref);
+          const float p = prob_of(sc[r][j], ref);
           if (see) l[r] += p;
           sc[r][j] = see ? p : -1.f;
         }
@@ -325,12 +325,12 @@ __global__ void __launch_bounds__(kFewThreads, R <= 8 ? 2 : 1) k_attend_few(A a)
             x[e] = (up ? x[e + d] : x[e]) + __shfl_xor_sync(0xffffffffu, send, d);
           }
         }
-        const float logit = see ? x[0] * a.sl2 : -INFINITY;
+        const float logit = see ? logit_of(x[0], a.sl2) : -INFINITY;
         float top = logit;
 #pragma unroll
         for (int d = S / 2; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
         const float M = fmaxf(m, top), ref = M == -INFINITY ? 0.f : M;
-        const float keep = fast_exp2(m - ref), p = see ? fast_exp2(logit - ref) : 0.f;
+        const float keep = fast_exp2(m - ref), p = see ? prob_of(logit, ref) : 0.f;
         m = M;
         l = l * keep + p;
         const bool scale = __any_sync(0xffffffffu, keep != 1.f);

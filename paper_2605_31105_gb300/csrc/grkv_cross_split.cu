@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int row = warp * 32 + lane;
     const uint32_t lane_addr = tmem + ((uint32_t)(warp * 32) << 16);
-    const float sl2 = a.sl2;   // of halved queries and keys: logits are four times its products, which may pass fp32 first
+    const float sl2 = a.sl2;   // halved queries and keys: a logit is four times the product with it (4 sl2 may pass fp32)
     float acc[kD];
     float m = -INFINITY, l = 0.f;
     bool ok = true;
