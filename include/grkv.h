@@ -394,9 +394,10 @@ int grkv_attend_tree(const grkv_cache_params* p, const void* q, const void* k_pa
 /* Attention over the whole cache of a unit, whatever it holds: an encoder's states, a document that
  * several sequences read, a cache compressed with causal = 0.  Row i < q_len[u] (NULL: t) of unit u
  * sees every slot j < len[u]; queries are no slots of the cache, so that q_len and len have nothing
- * to do with each other.  window and n_sink are not read.  The rest, errors and roundings too (up to 8
- * rows g t of bf16 may be rounded less), is grkv_attend's: a unit of length 0 gives out = 0 and
- * lse = -inf, rows from q_len[u] on are left as they were.  Beams of a sequence, whose caches are
+ * to do with each other.  window and n_sink are not read (negative ones are refused).  The rest, errors and
+ * roundings too, is grkv_attend's: a unit of length 0 gives out = 0 and lse = -inf, rows from q_len[u] on
+ * are left as they were.  (bf16 over short caches: probabilities keep 16 bits and more with up to 8 rows g t,
+ * and are rounded to bf16 in every tile with 9 to 16.)  Beams of a sequence, whose caches are
  * one, go into the group.  With 9 rows g t of fp32 and more, queries, keys, values and probabilities
  * are multiplied as three bf16 parts each, which leave 2^-27 of a number, or 2^-125 where that is
  * more (GRKV_FORCE_SIMT: fp32 as they are); a key or value that is not finite then makes every
@@ -429,9 +430,10 @@ int grkv_cache_map(const grkv_cache_params* p, const int32_t* count, const int32
  *
  * Pair i < rotary / 2 of a row at position p becomes
  *   (x, y) -> a (x cos p f_i - y sin p f_i, x sin p f_i + y cos p f_i)
- * and the dimensions from rotary on go through bit for bit.  Angles are off by 2^-28 turns
- * at most (what fp32 leaves of an eighth of a turn) at every position, frequencies by some 2^-51 of
- * themselves and 2^-65 turns; products and sums are fp32, rounded once to the row's type. */
+ * and the dimensions from rotary on go through bit for bit.  Frequencies are off by some 2^-51 of
+ * themselves and 2^-65 turns; p f_i as a fraction of a turn by 2^-33 turns, at every position; its
+ * cosine and sine by 2^-23 at most for fp32 rows and 2^-20 for bf16 ones.  Products and sums are fp32,
+ * rounded once to the row's type. */
 #define GRKV_ROPE_HALF  0   /* pair i: dimensions i and i + rotary / 2 */
 #define GRKV_ROPE_PAIRS 1   /* pair i: dimensions 2 i and 2 i + 1 (interleaved) */
 

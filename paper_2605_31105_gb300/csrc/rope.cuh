@@ -67,9 +67,10 @@ __device__ __forceinline__ Turn turn_by(int64_t p, float amp, float sign) {
 }
 
 // Cosine and sine of the fraction f 2^-32 of a turn.  fp32: the nearest quarter, and a rest of at most an
-// eighth of a turn, which fp32 holds to 2^-28, through the Taylor polynomials of both to the 9th
-// and 10th power (the next terms are below 2^-28): off by 2^-23 at most.  (sincospif over the whole turn, of
-// which fp32 holds 2^-25, takes as long: 5.6 us for 5.8 over 25000 rows.)
+// eighth of a turn, through the Taylor polynomials of both to the 9th and 10th power (the next terms are below
+// 2^-28).  The rest is off by 2^-26.3 turns (2^-28 as an fp32 number, as much again from 2 pi 2^-32, 2^-27.6 from their
+// product), cosine and sine by 2^-23.2 (the largest over all 2^32 fractions).  (sincospif over the whole turn, of which
+// fp32 holds 2^-25, takes as long: 5.6 us for 5.8 over 25000 rows.)
 __device__ __forceinline__ void cos_sin(uint32_t f, float* c, float* s) {
   const uint32_t quarter = (f + (1u << 29)) >> 30;   // 0..3
   const float x = (float)(int32_t)(f - (quarter << 30)) * 1.46291807926715968e-9f;   // 2 pi 2^-32
@@ -87,9 +88,10 @@ __device__ __forceinline__ void cos_sin(uint32_t f, float* c, float* s) {
   *c = __uint_as_float(__float_as_uint(odd ? a : b) ^ (((quarter + 1) & 2) << 30));
   *s = __uint_as_float(__float_as_uint(odd ? b : a) ^ ((quarter & 2) << 30));
 }
-// bf16: the special function unit's, over one turn around 0, off by 2^-20 at most (2^-21.2 of its own, the rest
-// the angle's rounding), a 2000th of the output's: with the polynomials an appended chunk takes 9.8 us for 9.1, a
-// streamed one 27.2 for 25.5, 524288 kept rows 88.1 for 87.1.
+// bf16: the special function unit's, over one turn around 0.  Its documented errors are 2^-21.4 and 2^-21.2; the angle is
+// off by 2^-25 turns as an fp32 number, 2^-26.1 from 2 pi 2^-32 and 2^-25.7 from their product: 2^-20.2 together at
+// most (2^-21.1 is the largest over all 2^32 fractions), a 2000th of the output's.  With the polynomials an appended chunk takes 9.8 us
+// for 9.1, a streamed one 27.2 for 25.5, 524288 kept rows 88.1 for 87.1.
 __device__ __forceinline__ void cos_sin_bf16(uint32_t f, float* c, float* s) {
   __sincosf((float)(int32_t)f * 1.46291807926715968e-9f, s, c);
 }
