@@ -189,7 +189,8 @@ __global__ void __launch_bounds__(kThreads, R <= 4 ? 2 : 1)
       page = 0;
     }
     entry = look_up(k + stride);
-    // (the next step's K asked for here already: 12.2 us -> 13.1 for one row of 128 units)
+    // (the next step's K asked for here already: 12.2 us -> 13.1 for one row of 128 units, two sets of inputs in turn, which
+    // L2 holds in part)
     uint4 kk[kLoad], vv[kLoad];
     load(a.k, k, page, kk);
     load(a.v, k, page, vv);
@@ -612,7 +613,9 @@ cudaError_t launch_few(const AttendArgs& a, bool f32, int C, cudaStream_t st) {
 
 }  // namespace
 
-// CTAs of a unit: three to an SM in all (four of those with four warps), 128 slots each at least.
+// CTAs of a unit, 128 slots each at least: up to three times the SMs in all, four times those of four warps.  An SM
+// holds two of k_cross_few's at once (one of fp32 with 5 to 8 rows), four of k_cross_mma's (three with 9 rows and more),
+// so a call of the most CTAs takes more than a wave; the rule below was measured with it.
 static int few_ctas(const CacheShape& s, int sms) {
   const int most = (s.dtype == GRKV_BF16 && s.g * s.t > 2 ? 4 : 3) * sms;
   int C = 1;
@@ -622,8 +625,8 @@ static int few_ctas(const CacheShape& s, int sms) {
 
 // Whether a cluster a unit is faster than runs that are even over the SMs, by the slots that units can have (the
 // host does not know their lengths): a CTA's run of them may be longer than an SM's even share by what planning
-// and joining take, 10 us, less where rows make a slot dearer; many rows are bound by the products.  us, the other
-// kernels' behind the slash (`n`: units of n / 16 to n slots, `n-`: all of n):
+// and joining take, 10 us, less where rows make a slot dearer; many rows are bound by the products.  us in a
+// graph, three sets of inputs in turn, the other kernels' behind the slash (`n`: units of n / 16 to n slots, `n-`: all of n):
 //   bf16, 1 row    128 x 1500 14.5/24.5, 1 x 8000 9.5/12.0, 1 x 20000 18.5/13.3, 128 x 16000 108/107, 128 x 30000- 281/329
 //         2 rows   128 x 1500 16.0/25.3, 64 x 6000 24.8/33.5, 128 x 16000 121/107
 //         4        128 x 1500 16.3/24.9, 8 x 8000 14.6/20.5, 1 x 8000 14.5/13.3, 128 x 16000- 163/183, 512 x 8000 240/202

@@ -13,13 +13,14 @@
 // K and V, read from the pages a tile ahead, split, and stored to shared memory as the products want them.  Warp 12
 // issues the products.  Of the block's 512 x 128 registers at launch the warpgroups take 128 x (208 + 128 + 128 + 48).
 //
-// What bounds it: 4.5 K cycles of products a tile, and the code, of which an SM holds little: 7.5 K cycles a tile
-// (every role unrolled, and half the loading warps, took 15 K).  Runs are planned in tiles of 64 slots and an item's
+// What bounds it: 4.5 K cycles of products a tile, and the code, of which an SM holds little: 7.2 K cycles a tile
+// (every role unrolled, and half the loading warps, took 15 K).  The loading warps keep a tile's K and V in 64 of
+// the launch's 128 registers, for which the compiler spills 68 bytes stored and 152 loaded (-Xptxas -v).  Runs are planned in tiles of 64 slots and an item's
 // start and end as one more (in tiles of 128, 9 rows of one unit of 300 slots took 17.8 us for 14.9).  300 queries of
-// 4 heads over 16 units of up to 1203 slots take 55 us (184 on CUDA cores), 77 of 7 over 6 units 22.5 (47), 24 rows
-// over 64 units of up to 6000 slots 97 (211), 9 over 128 of 1500 60 (96).  Q in TMEM, with K and V in two buffers or
-// copied two tiles ahead, was slower (128 units of 8000 slots 243 us for 226), as were parts formed before there is
-// room for them (285).
+// 4 heads over 16 units of up to 1203 slots take 55 us (184 on CUDA cores), 77 of 7 over 6 units 22.4 (47), 24 rows
+// over 64 units of up to 6000 slots 94 (211), 9 over 128 of 1500 58 (96).  Q in TMEM, with K and V in two buffers or
+// copied two tiles ahead, was slower (9 rows over 128 units of 8000 slots 243 us, where this took 226 then and 217 now),
+// as were parts formed before there is room for them (285).
 #include <stddef.h>
 
 #include <algorithm>
@@ -431,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_split(const __grid_consta
 }  // namespace
 
 // From 9 rows on, where a row tile is filled by a tenth: 9 rows of a unit of 300 slots take 15 us (20 in the CUDA-core
-// kernel), of 128 units of 1500 60 (96), of 8000 226 (381); 64 rows 63 (118) and 233 (510).  Up to 8 rows, tiles of the
+// kernel), of 128 units of 1500 58 (96), of 8000 217 (381); 64 rows 63 (118) and 226 (510).  Up to 8 rows, tiles of the
 // CUDA-core kernel that are mostly empty too are faster: 128 units of 1500 slots take 42.
 bool cross_is_split(const CacheShape& s) { return s.dtype == GRKV_F32 && !s.simt && s.g * s.t > 8; }
 

@@ -169,8 +169,8 @@ struct AppendRopeArgs {
 
 // kThreads threads a token's new key and value and up to kPartHeads of its queries' heads, two in flight; more
 // heads are parts of their own.  Rows are asked for before the table's entry that says where they go.  Memory:
-// 32768 tokens of 4 heads, 100 MB, 16.8 us; a chunk of 16384 8.6, with four heads in flight 10.4, with keys and
-// queries in blocks of their own 10.0.
+// 32768 tokens of 4 heads, 100 MB, 19.0 us; a chunk of 16384 8.4 to 9.3 (8.6 where four heads in flight took 10.4, and
+// keys and queries in blocks of their own 10.0).
 constexpr int kAppendThreads = 128, kAppendHeads = 2, kPartHeads = 4;
 template <typename T, Hold H>
 __global__ void __launch_bounds__(kAppendThreads)
