@@ -25,7 +25,7 @@ def test_the_largest_slot_takes_all(grkv_lib, dtype, flags, g, t, cross):
     dq, table, lens, ws = q.cuda(), R.int_dev(c.table), R.int_dev(c.lens), workspace(p)
     for power in (24, 30, 40, 70, 120):
         p.scale = 2.0 ** power
-        out, lse = torch.zeros_like(dq), torch.zeros(q.shape[:3], device="cuda")
+        out, lse = torch.zeros_like(dq), torch.zeros(q.shape[:3], dtype=torch.float32, device="cuda")
         (b.grkv_attend_cross if cross else b.grkv_attend)(p, dq, kd, vd, table, lens, out, ws, lse=lse)
         assert b.grkv_status(ws) == b.GRKV_OK and torch.isfinite(out).all() and torch.isfinite(lse).all()
         for u, n in enumerate(c.lens):
