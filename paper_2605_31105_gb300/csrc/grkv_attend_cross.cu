@@ -189,8 +189,8 @@ __global__ void __launch_bounds__(kThreads, R <= 4 ? 2 : 1)
       page = 0;
     }
     entry = look_up(k + stride);
-    // (the next step's K asked for here already: 12.2 us -> 13.1 for one row of 128 units, two sets of inputs in turn, which
-    // L2 holds in part)
+    // (the next step's K asked for here already: 12.2 us -> 13.1 for one row of 128 units, two sets of inputs in
+    // turn, which L2 holds in part)
     uint4 kk[kLoad], vv[kLoad];
     load(a.k, k, page, kk);
     load(a.v, k, page, vv);
@@ -626,7 +626,8 @@ static int few_ctas(const CacheShape& s, int sms) {
 // Whether a cluster a unit is faster than runs that are even over the SMs, by the slots that units can have (the
 // host does not know their lengths): a CTA's run of them may be longer than an SM's even share by what planning
 // and joining take, 10 us, less where rows make a slot dearer; many rows are bound by the products.  us in a
-// graph, three sets of inputs in turn, the other kernels' behind the slash (`n`: units of n / 16 to n slots, `n-`: all of n):
+// graph, three sets of inputs in turn, the other kernels' behind the slash (`n`: units of n / 16 to n slots, `n-`: all
+// of n):
 //   bf16, 1 row    128 x 1500 14.5/24.5, 1 x 8000 9.5/12.0, 1 x 20000 18.5/13.3, 128 x 16000 108/107, 128 x 30000- 281/329
 //         2 rows   128 x 1500 16.0/25.3, 64 x 6000 24.8/33.5, 128 x 16000 121/107
 //         4        128 x 1500 16.3/24.9, 8 x 8000 14.6/20.5, 1 x 8000 14.5/13.3, 128 x 16000- 163/183, 512 x 8000 240/202

@@ -14,13 +14,13 @@
 // issues the products.  Of the block's 512 x 128 registers at launch the warpgroups take 128 x (208 + 128 + 128 + 48).
 //
 // What bounds it: 4.5 K cycles of products a tile, and the code, of which an SM holds little: 7.2 K cycles a tile
-// (every role unrolled, and half the loading warps, took 15 K).  The loading warps keep a tile's K and V in 64 of
-// the launch's 128 registers, for which the compiler spills 68 bytes stored and 152 loaded (-Xptxas -v).  Runs are planned in tiles of 64 slots and an item's
-// start and end as one more (in tiles of 128, 9 rows of one unit of 300 slots took 17.8 us for 14.9).  300 queries of
-// 4 heads over 16 units of up to 1203 slots take 55 us (184 on CUDA cores), 77 of 7 over 6 units 22.4 (47), 24 rows
-// over 64 units of up to 6000 slots 94 (211), 9 over 128 of 1500 58 (96).  Q in TMEM, with K and V in two buffers or
-// copied two tiles ahead, was slower (9 rows over 128 units of 8000 slots 243 us, where this took 226 then and 217 now),
-// as were parts formed before there is room for them (285).
+// (every role unrolled, and half the loading warps, took 15 K).  The loading warps keep a tile's K and V in 64 of the
+// launch's 128 registers, for which the compiler spills 68 bytes stored and 152 loaded (-Xptxas -v).  Runs are planned
+// in tiles of 64 slots and an item's start and end as one more (in tiles of 128, 9 rows of one unit of 300 slots took
+// 17.8 us for 14.9).  300 queries of 4 heads over 16 units of up to 1203 slots take 55 us (184 on CUDA cores), 77 of 7
+// over 6 units 22.4 (47), 24 rows over 64 units of up to 6000 slots 94 (211), 9 over 128 of 1500 58 (96).  Q in TMEM,
+// with K and V in two buffers or copied two tiles ahead, was slower (9 rows over 128 units of 8000 slots 243 us, where
+// this took 226 then and 217 now), as were parts formed before there is room for them (285).
 #include <stddef.h>
 
 #include <algorithm>

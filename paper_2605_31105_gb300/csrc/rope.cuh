@@ -90,8 +90,8 @@ __device__ __forceinline__ void cos_sin(uint32_t f, float* c, float* s) {
 }
 // bf16: the special function unit's, over one turn around 0.  Its documented errors are 2^-21.4 and 2^-21.2; the angle is
 // off by 2^-25 turns as an fp32 number, 2^-26.1 from 2 pi 2^-32 and 2^-25.7 from their product: 2^-20.2 together at
-// most (2^-21.1 is the largest over all 2^32 fractions), a 2000th of the output's.  With the polynomials an appended chunk takes 9.8 us
-// for 9.1, a streamed one 27.2 for 25.5, 524288 kept rows 88.1 for 87.1.
+// most (2^-21.1 is the largest over all 2^32 fractions), a 2000th of the output's.  With the polynomials an appended
+// chunk takes 9.8 us for 9.1, a streamed one 27.2 for 25.5, 524288 kept rows 88.1 for 87.1.
 __device__ __forceinline__ void cos_sin_bf16(uint32_t f, float* c, float* s) {
   __sincosf((float)(int32_t)f * 1.46291807926715968e-9f, s, c);
 }
